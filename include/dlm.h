@@ -240,6 +240,65 @@ int dlm_gemm_nt(const void* x, const void* w, void* y, int M, int N, int K, int 
 int dlm_attention(const void* q, const void* k, const void* v, void* out, int A, int T, int n_q, int n_kv,
                   int head_dim, int dtype, void* stream);
 
+/* ---- an 8-bit KV cache, and what feeds and reads it -------------------------------------------------
+ * For callers that keep a cache of their own beside (or instead of) a dlm_state's half-precision one: queries and keys
+ * normalised and rotated, K and V quantised as they are written, read back, and the attention of packed rows over them.
+ * Sequences are packed as in dlm_step: sequence b owns rows [row_offsets[b], row_offsets[b+1]) of every per-row array (a
+ * sequence may have none), host arrays have n_seqs entries (row_offsets one more; row_offsets[0] == 0), slot NULL means
+ * 0, 1, ...; at most 32 sequences.  Rows are row-major with a stride in elements, so that they can be columns of a wider
+ * matrix (the fused QKV product); DEVICE pointers are 16-byte aligned and strides multiples of 16 bytes (DLM_EINVAL
+ * otherwise).  head_dim in {32, 64, 128}; dtype DLM_F32 or DLM_BF16.  None of the calls allocates or synchronises: all can
+ * be captured into a graph, with the host arrays as they were at capture. */
+
+/* Queries and keys as an attention reads them.  A row of x holds n_q query heads and then n_kv key heads of head_dim values (either
+ * count may be 0; what lies behind them is neither read nor written).  Per head:
+ *   y = x * rsqrt(mean(x^2) + eps) * gain          (q_gain / k_gain DEVICE [head_dim] of dtype; NULL: y = x)
+ *   out_i = y_i cos a - y_j sin a, out_j = y_j cos a + y_i sin a,   j = i + head_dim/2, a = position * theta^(-2 i / head_dim)
+ * positions DEVICE [rows], any int32; the angle is computed in 64 bits, sums are fp32, values are rounded once.  out may be x (with
+ * the same stride); else the two must not overlap.  Errors: DLM_EINVAL (null pointer, alignment, stride shorter than a row, overlap,
+ * eps or theta not positive and finite, bad dtype), DLM_ESHAPE (rows < 0, heads, head_dim), DLM_EHIP. */
+int dlm_qk_norm_rope(const void* x, int64_t x_stride, int rows, int n_q, int n_kv, int head_dim, int dtype, const void* q_gain,
+                     const void* k_gain, float eps, float theta, const int32_t* positions, void* out, int64_t out_stride, void* stream);
+
+/* A cache of n_slots sequences of up to max_len positions, in caller-owned DEVICE memory of dlm_kv8_bytes(...) bytes (0: an
+ * unsupported shape) at a multiple of 16, zero-filled before its first use.  Each vector (K or V of one position and kv head) is held
+ * as 8-bit codes and a scale 2^E: E is the smallest integer in [-60, 60] with max|x| <= M 2^E, a code is x 2^-E rounded to the
+ * format (ties to even, saturated where E = 60 is not enough).  DLM_KV8_E4M3: 8-bit floating point with 3 fraction bits, M = 448;
+ * DLM_KV8_I8: integers, M = 127.  A vector with a NaN or an infinity reads as all NaN; a position never written reads as 0. */
+enum { DLM_KV8_E4M3 = 0, DLM_KV8_I8 = 1 };
+typedef struct {
+  int32_t n_slots, max_len, n_kv, head_dim, format;
+  void* data; /* DEVICE */
+} dlm_kv8_cache;
+size_t dlm_kv8_bytes(int n_slots, int max_len, int n_kv, int head_dim);
+
+/* Row r of sequence b (k and v: [rows, n_kv * head_dim] at row_stride) becomes position start[b] + r of its slot; a slot may be given
+ * once.  dlm_kv8_read writes the values the positions stand for (exact in both dtypes) to k and v; slots may repeat, k and v must
+ * not overlap.  Positions outside the spans, and rows behind the last sequence, are left as they are.
+ * Errors: DLM_EINVAL (null pointer, alignment, stride, bad dtype or format, offsets, slot), DLM_ESHAPE (cache shape),
+ * DLM_ECAPACITY (n_seqs > 32, a span beyond max_len), DLM_EHIP. */
+int dlm_kv8_write(const dlm_kv8_cache* c, const void* k, const void* v, int64_t row_stride, int dtype, const int32_t* row_offsets,
+                  const int32_t* start, const int32_t* slot, int n_seqs, void* stream);
+int dlm_kv8_read(const dlm_kv8_cache* c, void* k, void* v, int64_t row_stride, int dtype, const int32_t* row_offsets, const int32_t* start,
+                 const int32_t* slot, int n_seqs, void* stream);
+
+/* out[rows, n_q, head_dim] (contiguous) = softmax(q K^T / sqrt(head_dim)) V per row and head; query head h reads kv head
+ * h / (n_q / n_kv).  mask NULL: every row of sequence b sees positions [0, n_keys[b]) of its slot.  mask DEVICE [rows, mask_words]
+ * uint32: the last positions of the n_keys[b] (at least the sequence's row count nr) are its rows' own; a row sees the n_keys[b] - nr
+ * before them and position n_keys[b] - nr + j where bit j % 32 of word j / 32 of its mask is set (32 mask_words >= nr): a tree of
+ * drafted tokens sets its ancestors' bits and its own, a causal span the bits up to its own.  A row that sees nothing (or n_keys 0)
+ * gives zeros; NaN or infinite keys and values that a row does not see do not touch it, those that it sees make it NaN.  Slots may repeat.
+ * q is read as it is (fp32: products to 22 bits of it); out must not overlap q.
+ * workspace: DEVICE scratch of dlm_kv8_attention_workspace(rows, n_q, head_dim) bytes (16-byte aligned; NULL where that is 0),
+ * used until the call's work is done: calls that may overlap need one each.
+ * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, bad dtype or format, offsets, slot, n_keys < 0 or, with a mask, < nr),
+ * DLM_ESHAPE (cache shape, n_q), DLM_ECAPACITY (n_seqs > 32, n_keys > max_len, mask_words or workspace too small, too many rows for
+ * one launch), DLM_EHIP. */
+size_t dlm_kv8_attention_workspace(int rows, int n_q, int head_dim);
+int dlm_kv8_attention(const dlm_kv8_cache* c, const void* q, int64_t q_stride, void* out, int dtype, int n_q, const int32_t* row_offsets,
+                      const int32_t* n_keys, const int32_t* slot, int n_seqs, const uint32_t* mask, int mask_words, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
 /* ---- what the GPU achieves on the resources the rooflines are drawn against -------------------
  * For callers that report measurements (bench.py): kernels that do nothing but the one thing, timed
  * with events on `stream`, which is synchronised before the call returns.

@@ -26,4 +26,6 @@ Parity status of each function against something other than itself
                                          in the schedule arithmetic fail that check.  The schedule itself is this
                                          build's reading of Sec. 4.2 / App. A.3: "parity unpinned" against the
                                          authors' behaviour
+  kv8 (8-bit cache and its operators)    pinned (the formats' codes against torch's e4m3, quantisation by brute force, midpoints,
+                                         attention and masks by closed forms)
 """

@@ -38,6 +38,10 @@ class dlm_weights(C.Structure):
                 ("norm2", C.POINTER(C.c_void_p)), ("final_norm", C.c_void_p), ("lm_head", C.c_void_p)]
 
 
+class dlm_kv8_cache(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_slots", "max_len", "n_kv", "head_dim", "format")] + [("data", C.c_void_p)]
+
+
 _I32P = C.POINTER(C.c_int32)
 
 
@@ -59,7 +63,8 @@ EXPORTS = ["dlm_last_error", "dlm_model_create", "dlm_model_destroy", "dlm_state
            "dlm_state_kv_len", "dlm_step", "block_boundary", "select_parallel", "dlm_vocab_stats_workspace", "dlm_vocab_stats",
            "dlm_gemm_nt", "dlm_attention", "dlm_profile_enable", "dlm_profile_read", "dlm_probe_hbm_read", "dlm_probe_mfma",
            "dlm_state_fuse_stats", "dlm_vocab_stats_static", "dlm_plan_attention",
-           "dlm_plan_vocab_stats", "dlm_plan_gemm"]
+           "dlm_plan_vocab_stats", "dlm_plan_gemm", "dlm_qk_norm_rope", "dlm_kv8_bytes", "dlm_kv8_write", "dlm_kv8_read",
+           "dlm_kv8_attention_workspace", "dlm_kv8_attention"]
 
 
 def lib():
@@ -98,6 +103,15 @@ def lib():
         L.dlm_state_fuse_stats.argtypes = [C.c_void_p, C.c_int]
         L.dlm_profile_enable.argtypes = [C.c_void_p, C.c_uint]
         L.dlm_profile_read.argtypes = [C.c_void_p, C.c_int, C.POINTER(C.c_double), C.POINTER(C.c_int64), C.c_int]
+        L.dlm_qk_norm_rope.argtypes = [C.c_void_p, C.c_int64] + [C.c_int] * 5 + [C.c_void_p] * 2 + [C.c_float] * 2 + [C.c_void_p] * 2 + [C.c_int64, C.c_void_p]
+        L.dlm_kv8_bytes.argtypes = [C.c_int] * 4
+        L.dlm_kv8_bytes.restype = C.c_size_t
+        for f in (L.dlm_kv8_write, L.dlm_kv8_read):
+            f.argtypes = [C.c_void_p] * 3 + [C.c_int64, C.c_int] + [C.c_void_p] * 3 + [C.c_int, C.c_void_p]
+        L.dlm_kv8_attention_workspace.argtypes = [C.c_int] * 3
+        L.dlm_kv8_attention_workspace.restype = C.c_size_t
+        L.dlm_kv8_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int] + [C.c_void_p] * 3 + \
+                                       [C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -379,6 +393,163 @@ def dlm_attention(q, k, v):
     T, n_kv, _ = k.shape
     out = torch.empty_like(q)
     _check(lib().dlm_attention(_ptr(q), _ptr(k), _ptr(v), _ptr(out), A, T, n_q, n_kv, hd, dtype_code(q), _stream()))
+    return out
+
+
+# ---- the 8-bit KV cache, and what feeds and reads it (include/dlm.h) ---------------------------------------------------------------
+
+KV8_FORMATS = ("e4m3", "i8")
+
+
+def _int32s(name, v, n):
+    """A host list as the bytes of 32-bit integers, at least n of them; what is none is refused."""
+    if v is None:
+        return None
+    if len(v) < n:
+        raise ValueError(f"{name}: {len(v)} entries where {n} are read")
+    try:
+        return _int_packer(len(v))(*v)
+    except (struct.error, TypeError):
+        pass
+    whole = [int(x) if not isinstance(x, str) and x == int(x) else None for x in v]
+    if any(x is None or not -2**31 <= x < 2**31 for x in whole):
+        raise ValueError(f"{name}: {v} are not 32-bit integers")
+    return _int_packer(len(v))(*whole)
+
+
+def _on_gpu(name, t):
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: not on the current GPU")
+
+
+def _row_stride(name, t, shape, dtypes):
+    """The stride between the rows (first axis) of a device tensor whose rows are contiguous; shape: None for an axis of any size."""
+    _on_gpu(name, t)
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name}: {t.dtype}, not one of {dtypes}")
+    have, strides = t.shape, t.stride()
+    if len(have) != len(shape):
+        raise ValueError(f"{name}: shape {tuple(have)} where {shape} is read")
+    width = 1
+    for i in range(len(shape) - 1, 0, -1):
+        if strides[i] != width and have[i] != 1:
+            raise ValueError(f"{name}: strides {strides}: a row is not contiguous")
+        width *= have[i]
+    for n, m in zip(shape, have):
+        if n is not None and n != m:
+            raise ValueError(f"{name}: shape {tuple(have)} where {shape} is read")
+    return strides[0] if have[0] > 1 else width
+
+
+_FLOATS = (torch.float32, torch.bfloat16)
+
+
+class Kv8Cache:
+    """A cache of K and V at 8 bits (dlm_kv8_cache) with its memory: `slots` sequences of up to max_len positions.
+    format: "e4m3" or "i8"."""
+
+    def __init__(self, slots, max_len, n_kv, head_dim, format="e4m3", device="cuda"):
+        n = lib().dlm_kv8_bytes(slots, max_len, n_kv, head_dim)
+        if n == 0:
+            raise DlmError(-2, f"a cache of {slots} slots x {max_len} positions x {n_kv} heads of {head_dim}")
+        self.slots, self.max_len, self.n_kv, self.head_dim, self.format = slots, max_len, n_kv, head_dim, format
+        code = KV8_FORMATS.index(format)
+        self.data = torch.zeros(n, dtype=torch.uint8, device=device)
+        self._desc = dlm_kv8_cache(slots, max_len, n_kv, head_dim, code, self.data.data_ptr())
+        self._ref = C.addressof(self._desc)
+
+
+def _kv8_spans(cache, k, v, row_offsets, start, slot):
+    n = len(start)
+    off = _int32s("row_offsets", row_offsets, n + 1)
+    shape = (None, cache.n_kv, cache.head_dim)
+    stride = _row_stride("k", k, shape, _FLOATS)
+    if _row_stride("v", v, shape, (k.dtype,)) != stride:
+        raise ValueError("k and v have different strides between rows")
+    if k.shape[0] != v.shape[0] or row_offsets[n] > k.shape[0]:
+        raise ValueError(f"{k.shape[0]} rows of k and {v.shape[0]} of v where {row_offsets[n]} are read")
+    _on_gpu("cache", cache.data)
+    return cache._ref, k.data_ptr(), v.data_ptr(), stride, _DTYPE_CODES[k.dtype], off, _int32s("start", start, n), _int32s("slot", slot, n), n, _stream()
+
+
+def dlm_kv8_write(cache, k, v, row_offsets, start, slot=None):
+    """k, v: device tensors [rows, n_kv, head_dim] (rows may be strided: columns of a wider matrix); the rest: host int lists."""
+    args = _kv8_spans(cache, k, v, row_offsets, start, slot)
+    if k.shape[0]:  # (a tensor without rows has no address)
+        _check(lib().dlm_kv8_write(*args))
+
+
+def dlm_kv8_read(cache, row_offsets, start, slot=None, k=None, v=None, dtype=torch.bfloat16):
+    """The values of cached positions, (k, v): into the given tensors [rows, n_kv, head_dim], or into new ones of `dtype`."""
+    if (k is None) != (v is None):
+        raise ValueError("k and v are given together")
+    if k is None:
+        rows = int(row_offsets[len(start)])
+        k, v = (torch.empty((rows, cache.n_kv, cache.head_dim), dtype=dtype, device=cache.data.device) for _ in "kv")
+    args = _kv8_spans(cache, k, v, row_offsets, start, slot)
+    if k.shape[0]:
+        _check(lib().dlm_kv8_read(*args))
+    return k, v
+
+
+def dlm_kv8_attention(cache, q, row_offsets, n_keys, slot=None, mask=None, out=None, workspace=None):
+    """q: device tensor [rows, n_q, head_dim] (rows may be strided); mask: device int32 [rows, words], bits as in include/dlm.h; out:
+    contiguous, of q's shape and dtype (None: a new one); workspace: a contiguous device tensor of at least
+    dlm_kv8_attention_workspace bytes that nothing else uses meanwhile (None: a new one); the rest: host int lists.  Returns out."""
+    n = len(n_keys)
+    stride = _row_stride("q", q, (None, None, cache.head_dim), _FLOATS)
+    rows, n_q = q.shape[0], q.shape[1]
+    off = _int32s("row_offsets", row_offsets, n + 1)
+    packed = int(row_offsets[n])
+    if packed > rows:
+        raise ValueError(f"{rows} rows of q where {packed} are read")
+    if out is None:
+        out = torch.empty((rows, n_q, cache.head_dim), dtype=q.dtype, device=q.device)
+    elif _row_stride("out", out, (rows, n_q, cache.head_dim), (q.dtype,)) != n_q * cache.head_dim:
+        raise ValueError("out is not contiguous")
+    words = 0
+    if mask is not None:
+        words = mask.shape[-1]
+        if _row_stride("mask", mask, (None, None), (torch.int32,)) != words or mask.shape[0] < packed:
+            raise ValueError(f"mask: {tuple(mask.shape)} for {packed} rows, or not contiguous")
+    _on_gpu("cache", cache.data)
+    if rows == 0:
+        return out
+    L = lib()
+    size = L.dlm_kv8_attention_workspace(packed, n_q, cache.head_dim)
+    if workspace is None:
+        workspace = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
+    else:
+        _on_gpu("workspace", workspace)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace is not contiguous")
+        size = workspace.numel() * workspace.element_size()
+    _check(L.dlm_kv8_attention(cache._ref, q.data_ptr(), stride, out.data_ptr(), _DTYPE_CODES[q.dtype], n_q, off, _int32s("n_keys", n_keys, n),
+                               _int32s("slot", slot, n), n, _ptr(mask), words, _ptr(workspace), size, _stream()))
+    return out
+
+
+def dlm_qk_norm_rope(x, positions, n_q, n_kv, head_dim, q_gain=None, k_gain=None, eps=1e-5, theta=10000.0, out=None):
+    """x: device tensor [rows, columns] whose first (n_q + n_kv) * head_dim columns are the query and key heads (rows may be
+    strided); positions: device int32 [rows]; gains: [head_dim] of x's dtype, or None; out: as x (x itself: in place; None: a new
+    tensor of those columns alone).  Returns out."""
+    width = (n_q + n_kv) * head_dim
+    stride = _row_stride("x", x, (None, None), _FLOATS)
+    rows, dtype = x.shape[0], (x.dtype,)
+    if out is None:
+        out = torch.empty((rows, width), dtype=x.dtype, device=x.device)
+    out_stride = _row_stride("out", out, (rows, None), dtype)
+    if x.shape[1] < width or out.shape[1] < width:
+        raise ValueError(f"rows of {x.shape[1]} and {out.shape[1]} columns where {width} are read and written")
+    if _row_stride("positions", positions, (rows,), (torch.int32,)) != 1:
+        raise ValueError("positions are not contiguous")
+    for name, gain in (("q_gain", q_gain), ("k_gain", k_gain)):
+        if gain is not None and _row_stride(name, gain, (head_dim,), dtype) != 1:
+            raise ValueError(f"{name} is not contiguous")
+    if rows == 0:
+        return out
+    _check(lib().dlm_qk_norm_rope(x.data_ptr(), stride, rows, n_q, n_kv, head_dim, _DTYPE_CODES[x.dtype], _ptr(q_gain), _ptr(k_gain), eps, theta,
+                                  positions.data_ptr(), out.data_ptr(), out_stride, _stream()))
     return out
 
 

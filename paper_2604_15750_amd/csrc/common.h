@@ -29,6 +29,10 @@ typedef f16x4 op4;
 #define DLM_WAVE 64
 
 int dlm_fail(int code, const char* fmt, ...);
+#define REQUIRE(cond, code, ...) \
+  do {                           \
+    if (!(cond)) return dlm_fail(code, __VA_ARGS__); \
+  } while (0)
 #define DLM_HIP(expr)                                                                        \
   do {                                                                                       \
     hipError_t e_ = (expr);                                                                  \

@@ -22,11 +22,6 @@ int dlm_fail(int code, const char* fmt, ...) {
 }
 extern "C" const char* dlm_last_error(void) { return g_err; }
 
-#define REQUIRE(cond, code, ...) \
-  do {                           \
-    if (!(cond)) return dlm_fail(code, __VA_ARGS__); \
-  } while (0)
-
 // ---- file-scope scratch of the entry point that allocates nothing (dlm_vocab_stats_static) -------------
 // The partial online-softmax states of the vocabulary reduction, one per (row, chunk): what dlm_vocab_stats takes as its
 // workspace argument.  Every GPU the library runs on holds its own copy of the array, at its own address, until the process
