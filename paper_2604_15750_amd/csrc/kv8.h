@@ -5,12 +5,12 @@
 // arithmetic), costs e4m3 nothing (its steps are relative) and i8 half a bit on average, and takes one byte.
 //
 // Memory: per (slot, kv head) blocks of 32 positions, each one run of 64 * head_dim + 64 bytes, in the order in which the attention
-// feeds the matrix cores:
-//   K codes   operand fragments (16 positions x 32 dims, 8 bytes a lane) paired into 1 KiB pieces of 16 bytes a lane
-//   V codes   operand fragments (16 dims x 32 positions), paired the same way; a lane's 8 bytes hold positions {4g..4g+3, 16+4g..16+4g+3}:
-//             the order in which the first product leaves the keys in a lane's registers
-//   scales    for g = 0..3 the bytes of K at positions 4g.., 16+4g.., then of V: what lane group g needs is 16 bytes
-// so a wavefront reads a block of 32 positions in HD / 16 loads of 1 KiB and one of 64 bytes, all from one run of memory.
+// feeds the matrix cores (32x32x16 products; h = 0, 1: the half of a wavefront):
+//   K codes   per 32 dims 1 KiB: 16 bytes a lane, position lane % 32, dims 16h .. 16h + 15
+//   V codes   per 32 dims 1 KiB: 16 bytes a lane, dim lane % 32, positions 8j + 4h + i at byte 4j + i (j, i = 0..3): the order in which
+//             the first product leaves the keys in a lane's registers
+//   scales    32 bytes of K, 32 of V, by position
+// so a wavefront reads a block of 32 positions in HD / 16 loads of 1 KiB and two of a byte a lane, all from one run of memory.
 #pragma once
 #include "common.h"
 
@@ -20,15 +20,11 @@ typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 
 __host__ __device__ constexpr int kv8_block_bytes(int hd) { return 64 * hd + 64; }
 // byte offsets inside a block (p: position in it)
-__host__ __device__ inline int kv8_k_index(int p, int d, int hd) {
-  const int f = (p >> 4) * (hd >> 5) + (d >> 5), lane = (p & 15) + 16 * ((d & 31) >> 3);
-  return (f >> 1) * 1024 + lane * 16 + (f & 1) * 8 + (d & 7);
-}
+__host__ __device__ inline int kv8_k_index(int p, int d, int) { return (d >> 5) * 1024 + (p + (d & 16) * 2) * 16 + (d & 15); }
 __host__ __device__ inline int kv8_v_index(int p, int d, int hd) {
-  const int f = d >> 4, lane = (d & 15) + 16 * ((p & 15) >> 2);
-  return 32 * hd + (f >> 1) * 1024 + lane * 16 + (f & 1) * 8 + (p & 3) + 4 * (p >> 4);
+  return 32 * hd + (d >> 5) * 1024 + ((d & 31) + (p & 4) * 8) * 16 + (p >> 3) * 4 + (p & 3);
 }
-__host__ __device__ inline int kv8_scale_index(int p, int is_v, int hd) { return 64 * hd + ((p & 15) >> 2) * 16 + is_v * 8 + (p >> 4) * 4 + (p & 3); }
+__host__ __device__ inline int kv8_scale_index(int p, int is_v, int hd) { return 64 * hd + 32 * is_v + p; }
 
 // Scales: a byte E + 127, E in [-60, 60]; 255 marks a vector that had a NaN or an infinity (its codes are zero, it reads as NaN); 0 is
 // a position that was never written (it reads as zero).  The range of E is what lets the attention keep the V scale inside the
@@ -65,8 +61,7 @@ __device__ inline int seq_of(const int32_t* off, int n_seqs, int i) {
 void launch_kv8_write(const Kv8View& c, int format, int hd, const void* k, const void* v, int64_t stride, int dtype, const Kv8Meta& m, hipStream_t st);
 void launch_kv8_read(const Kv8View& c, int format, int hd, void* k, void* v, int64_t stride, int dtype, const Kv8Meta& m, hipStream_t st);
 struct Kv8AttnPlan {
-  int tiles;    // 16-query tiles of a workgroup
-  int waves;    // its wavefronts
+  int queries;  // of a workgroup
   int chunk;    // 32-position blocks of a split's share of the keys
   int splits;   // most shares of a sequence (1: the workgroups write the output)
   int64_t items;

@@ -166,7 +166,7 @@ extern "C" int dlm_kv8_attention(const dlm_kv8_cache* c, const void* q, int64_t 
   for (int b = 0; b < n_seqs; ++b) {
     const int64_t queries = (int64_t)(row_offsets[b + 1] - row_offsets[b]) * (n_q / c->n_kv);
     const int splits = ((n_keys[b] + 31) / 32 + p.chunk - 1) / p.chunk;
-    p.items += (queries + 16 * p.tiles - 1) / (16 * p.tiles) * (splits > 1 ? splits : 1);
+    p.items += (queries + p.queries - 1) / p.queries * (splits > 1 ? splits : 1);
     REQUIRE(queries <= INT32_MAX && p.items * c->n_kv < INT32_MAX, DLM_ECAPACITY, "dlm_kv8_attention: too many rows for one launch");
     m.item_off[b + 1] = (int32_t)p.items;
   }

@@ -1,63 +1,56 @@
 // Attention of packed rows over the 8-bit cache on the matrix cores: one pass over the keys with the running maximum and sum of a softmax.
 //
 // The queries of a kv head are the rows of a sequence times the query heads that share it (a group's heads read K and V together); a
-// workgroup has up to 16 TILES of them, its wavefronts take every NWV-th block of 32 positions and are merged through LDS.  S^T = K Q^T
-// leaves 8 keys of one query in a lane, in the order in which the cache holds V, so the probabilities feed O^T = V^T P^T from registers.
+// wavefront has 32 of them and takes blocks of 32 positions.  S^T = K Q^T leaves 16 keys of one query in a lane, in the order in which
+// the cache holds V, so the probabilities feed O^T = V^T P^T from registers.
 //
 // 8-bit codes are exact in IEEE half, so what the matrix cores lose is what the other operand loses:
 //   q  a power of two brings a query's largest magnitude to [2^14, 2^15); then one half term (bf16 queries: exact down to 2^-29 of the
 //      largest) or two, high and low (fp32 queries: 22 bits)
 //   p  one half term (bf16 outputs: 11 bits against the output's 8) or two (fp32: 22 bits)
 // The scales: with K_j = 2^a_j code_j and V_j = 2^b_j code_j,
-//   s'_j = (q . code_j) 2^a_j log2(e) / sqrt(hd) + b_j,   p'_j = 2^(s'_j - m'),   l = sum_j p'_j 2^-b_j,   o = sum_j p'_j code_j / l
-// so V's scale costs no instruction: it is the addend of the multiply-add that applies K's, and the sum's addition becomes a
-// multiply-add.  p' is at most 1 whatever the scales; b in [-60, 60] keeps every p' that weighs in l within 32 bits.  p' is kept times
-// 2^15, the top of half's range, where it keeps 11 bits down to 2^-29 of the largest.
-// A vector marked NaN: a key's scale byte 255 makes its score infinity times zero, a value's makes l minus infinity or NaN.
+//   s'_j = (q . K_j) log2(e) / sqrt(hd) + b_j,   p'_j = 2^(s'_j - m),   l = sum_j p'_j 2^-b_j,   o = sum_j p'_j code_j / l
+//   a  goes in where codes become half (the conversion scales; i8 takes it in the multiply-add that takes its offset off), relative to a
+//      wavefront's `ref`, which is raised where a block's keys would leave half's range; keys 2^-24 below it lose bits
+//   b  is the addend of the multiply-add that applies the softmax's scale, and the sum's addition becomes a multiply-add.  p' stays
+//      bounded whatever the scales; b in [-60, 60] keeps every p' that weighs in l within 32 bits.
+// The softmax's instructions weigh as much as the products (16 scores a lane against 512 cycles of them for 32 x 32 scores), so each
+// score costs a multiply-add, half a maximum, an exponential, a multiply-add and half a conversion: the products start from -m, and m
+// moves only where a score would leave half's range: the largest p' is brought to 2^8 (fp32: 2^13) and may grow to 2^15 before that.
 #include <type_traits>
 
 #include "kv8.h"
 
 namespace {
 
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
 constexpr float NEG_BIG = -3.0e38f;
-constexpr int P_BITS = 15;
+constexpr float P_LIMIT = 15.f;  // log2 of where the largest p' may go
 
-struct Pair { float a, b; };
-__device__ inline Pair across16(float v) {
-  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return Pair{__uint_as_float(r[0]), __uint_as_float(r[1])};
-}
-__device__ inline Pair across32(float v) {
+__device__ inline float halves_max(float v) {  // over the two lanes of a query
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return Pair{__uint_as_float(r[0]), __uint_as_float(r[1])};
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ inline float query_max(float v) {  // over the four lanes of a query
-  Pair t = across16(v);
-  t = across32(fmaxf(t.a, t.b));
-  return fmaxf(t.a, t.b);
-}
-__device__ inline float query_sum(float v) {
-  Pair t = across16(v);
-  t = across32(t.a + t.b);
-  return t.a + t.b;
+__device__ inline float halves_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// 8 codes (8 bytes) as half
+// 8 codes (8 bytes) as half, times 2^e (e4m3: `scale`; i8: `mul`, and `add` = -1152 mul)
 template <int FMT>
-__device__ inline f16x8 halves(unsigned lo, unsigned hi) {
+__device__ inline f16x8 halves(unsigned lo, unsigned hi, float scale, f16x2 mul, f16x2 add) {
   f16x2 h[4];
   if (FMT == DLM_KV8_E4M3) {
-    h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, false);
-    h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, 1.f, true);
-    h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, false);
-    h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, 1.f, true);
+    h[0] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, scale, false);
+    h[1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)lo, scale, true);
+    h[2] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, scale, false);
+    h[3] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)hi, scale, true);
   } else {  // a stored byte c + 128 behind 0x64 is 1024 + c + 128 as half
-    const f16x2 bias = {(f16_t)1152.f, (f16_t)1152.f};
-    h[0] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)) - bias;
-    h[1] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)) - bias;
-    h[2] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)) - bias;
-    h[3] = __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)) - bias;
+    h[0] = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04010400u)), mul, add);
+    h[1] = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, lo, 0x04030402u)), mul, add);
+    h[2] = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04010400u)), mul, add);
+    h[3] = __builtin_elementwise_fma(__builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, hi, 0x04030402u)), mul, add);
   }
   return f16x8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
 }
@@ -72,195 +65,368 @@ __device__ inline void load8(const float* p, float (&x)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
 }
+__device__ inline void store4(bf16_t* p, f32x4 v) { *(bf16x4*)p = bf16x4{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]}; }
+__device__ inline void store4(float* p, f32x4 v) { *(f32x4*)p = v; }
 
-template <int HD, int NWV>
-struct MergeLds {
-  float m[NWV][16], l[NWV][16];
-  float o[NWV][16][HD + 4];  // (rows 16 bytes apart from a multiple of the banks)
+// what an output is multiplied with: a row that sees nothing gives 0, one whose sum is not a positive number NaN
+__device__ inline float reciprocal(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : __uint_as_float(0x7FC00000u); }
+
+// What a workgroup works on
+struct Work {
+  int head, b, row0, nq, group, q0, split, blk0, blk1, n_keys, first;  // first: positions from here on are visible to whom the mask says
+  const unsigned char* region;
 };
+// (the heads of an item are neighbours: where their number is a multiple of 8 all items of a head are on one XCD, and its L2 has the head's K and V)
+__device__ inline Work work_of(const Kv8AttnArgs& a, const Kv8View& cache, const Kv8AttnMeta& meta, int queries) {
+  Work w;
+  w.head = blockIdx.x % cache.n_kv;
+  const int item = blockIdx.x / cache.n_kv;
+  w.b = seq_of(meta.item_off, meta.n_seqs, item);
+  w.row0 = meta.row_off[w.b];
+  w.n_keys = meta.n_keys[w.b];
+  w.group = a.n_q / cache.n_kv;
+  const int nr = meta.row_off[w.b + 1] - w.row0;
+  w.nq = nr * w.group;
+  const int qtiles = (w.nq + queries - 1) / queries, rel = item - meta.item_off[w.b];
+  w.split = rel / qtiles;
+  w.q0 = (rel - w.split * qtiles) * queries;
+  w.blk0 = w.split * meta.chunk;
+  w.blk1 = min((w.n_keys + 31) >> 5, w.blk0 + meta.chunk);
+  w.first = a.mask ? w.n_keys - nr : w.n_keys;
+  w.region = cache.data + ((int64_t)meta.slot[w.b] * cache.n_kv + w.head) * cache.head_bytes;
+  return w;
+}
 
-__device__ inline float finish(float o, float l) { return l > 0.f ? o / l : l == 0.f ? 0.f : __uint_as_float(0x7FC00000u); }
+// 32 queries of a wavefront and their running softmax
+template <typename T, int HD, int FMT>
+struct Tile {
+  static constexpr bool F32 = std::is_same<T, float>::value;
+  static constexpr float P_TOP = F32 ? 13.f : 8.f;  // log2 of where the largest p' is put: half ends 25 bits below 1
+  static constexpr int PIECES = HD / 32, KF = HD / 16, TERMS = F32 ? 2 : 1;
+  f16x8 qf[TERMS][KF];
+  f32x16 o[PIECES], from_m;        // from_m: -m / cq in every element, what the products start from
+  float qs, cq, m, l, limit;       // limit: minus infinity until the query has seen a key
+  int ref;                         // biased exponent that K's scales are relative to
+  const uint32_t* words;           // of the query's row in the mask
 
-template <typename T, int HD, int FMT, int TILES, int NWV>
-__global__ __launch_bounds__(NWV * 64) void kv8_attention_kernel(Kv8AttnArgs a, Kv8View cache, Kv8AttnMeta meta, int split_out) {
-  constexpr bool F32 = std::is_same<T, float>::value;
-  constexpr int KS = HD / 32, DT = HD / 16, TERMS = F32 ? 2 : 1;
-  __shared__ MergeLds<HD, NWV> L;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, c = lane & 15;
-  // (the heads of an item are neighbours: where their number is a multiple of 8 all items of a head are on one XCD, and its L2 has the head's K and V)
-  const int head = blockIdx.x % cache.n_kv, item = blockIdx.x / cache.n_kv;
-  const int b = seq_of(meta.item_off, meta.n_seqs, item);
-  const int row0 = meta.row_off[b], nr = meta.row_off[b + 1] - row0, n_keys = meta.n_keys[b], group = a.n_q / cache.n_kv;
-  const int nq = nr * group, qtiles = (nq + 16 * TILES - 1) / (16 * TILES);
-  const int rel = item - meta.item_off[b], split = rel / qtiles, q0 = (rel - split * qtiles) * (16 * TILES);
-  const int nblk = (n_keys + 31) >> 5, blk0 = split * meta.chunk, blk1 = min(nblk, blk0 + meta.chunk);
-  const unsigned char* region = cache.data + ((int64_t)meta.slot[b] * cache.n_kv + head) * cache.head_bytes;
-
-  // ---- queries: normalised by a power of two, in one or two half terms
-  f16x8 qf[TILES][TERMS][KS];
-  float qs[TILES];
-  const uint32_t* words[TILES];
-#pragma unroll
-  for (int u = 0; u < TILES; ++u) {
-    const int x = q0 + 16 * u + c, r = x / group;
-    const bool there = x < nq;
-    const T* from = (const T*)a.q + (int64_t)(row0 + (there ? r : 0)) * a.q_stride + (head * group + (there ? x - r * group : 0)) * HD + 8 * g;
-    words[u] = a.mask + (int64_t)(row0 + (there ? r : 0)) * a.mask_words;
-    float v[KS][8];
+  __device__ inline void start(const Kv8AttnArgs& a, const Work& w, int q0, int lane) {
+    const int h = lane >> 5, x = q0 + (lane & 31), r = x < w.nq ? x / w.group : 0, hq = x < w.nq ? x - r * w.group : 0;
+    const T* from = (const T*)a.q + (int64_t)(w.row0 + r) * a.q_stride + (w.head * w.group + hq) * HD + 16 * h;
+    words = a.mask + (int64_t)(w.row0 + r) * a.mask_words;
+    float v[KF][8];
     unsigned top = 0;
 #pragma unroll
-    for (int t = 0; t < KS; ++t) {
-      load8(from + 32 * t, v[t]);
+    for (int f = 0; f < KF; ++f) load8(from + 32 * (f >> 1) + 8 * (f & 1), v[f]);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[t][i]) & 0x7FFFFFFFu);
-    }
-    const int e = min(max((int)(__float_as_uint(query_max(__uint_as_float(top & 0x7F800000u))) >> 23) - 127, -100), 127);
+    for (int f = 0; f < KF; ++f)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[f][i]) & 0x7FFFFFFFu);
+    const int e = min(max((int)(__float_as_uint(halves_max(__uint_as_float(top & 0x7F800000u))) >> 23) - 127, -100), 127);
     const float up = __uint_as_float((unsigned)(127 + 14 - e) << 23);
-    qs[u] = __uint_as_float((unsigned)(127 - 14 + e) << 23) * (1.44269504088896340736f / sqrtf((float)HD));
+    qs = __uint_as_float((unsigned)(127 - 14 + e) << 23) * (float)(1.44269504088896340736 / (HD == 128 ? 11.3137084989847603904 : HD == 64 ? 8.0 : 5.65685424949238019521));
 #pragma unroll
-    for (int t = 0; t < KS; ++t)
+    for (int f = 0; f < KF; ++f)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float y = v[t][i] * up;
+        const float y = v[f][i] * up;
         const f16_t hi = (f16_t)y;
-        qf[u][0][t][i] = hi;
-        if (F32) qf[u][TERMS - 1][t][i] = (f16_t)(y - (float)hi);
+        qf[0][f][i] = hi;
+        if (F32) qf[TERMS - 1][f][i] = (f16_t)(y - (float)hi);
       }
+    m = l = cq = 0.f;
+    limit = -__builtin_inff();
+    ref = -1000;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) from_m[i] = 0.f;
+#pragma unroll
+    for (int d = 0; d < PIECES; ++d) o[d] = from_m;
   }
 
-  float m[TILES], l[TILES];
-  f32x4 o[TILES][DT];
-#pragma unroll
-  for (int u = 0; u < TILES; ++u) {
-    m[u] = NEG_BIG;
-    l[u] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) o[u][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // which of a block's positions the lane's query sees, from bit 4h on
+  __device__ inline unsigned visible(const Kv8AttnArgs& a, const Work& w, int blk, int h) const {
+    unsigned see = 0xFFFFFFFFu;
+    const int left = w.n_keys - 32 * blk, ofs = 32 * blk - w.first;  // ofs: of the block in the masked positions
+    if (left < 32) see = left > 0 ? (1u << left) - 1u : 0u;
+    if (a.mask) {
+      const int i = ofs >> 5, sh = ofs & 31;  // (floors: a block that starts in front of them takes its upper bits from word 0)
+      const unsigned lo = i >= 0 ? words[i] : 0xFFFFFFFFu, hi = sh && i + 1 < a.mask_words ? words[i + 1] : 0u;
+      see &= sh ? lo >> sh | hi << (32 - sh) : lo;
+    }
+    return see >> 4 * h;
   }
 
-  // ---- blocks of 32 positions; the next one is in flight while this one is worked on
-  constexpr int KP = HD / 32, VP = HD / 32;  // 1 KiB pieces of K and of V
-  u32x4 raw[KP + VP + 1];
-  auto load = [&](u32x4 (&w)[KP + VP + 1], int blk) __attribute__((always_inline)) {
-    const u32x4* p = (const u32x4*)(region + (int64_t)blk * kv8_block_bytes(HD));
+  __device__ inline void start_from_m() {
+    const float t = -m / cq;
 #pragma unroll
-    for (int i = 0; i < KP + VP; ++i) w[i] = p[i * 64 + lane];
-    w[KP + VP] = p[(KP + VP) * 64 + g];
+    for (int i = 0; i < 16; ++i) from_m[i] = t;
+  }
+
+  // One block of 32 positions.  kb: K's scale byte of position lane % 32; nan_keys: bits of positions marked NaN in K or V (the same
+  // in all lanes); vb, inv: LDS, V's exponents and what undoes them; k(i), v(i): the lane's 16 bytes of piece i; after_k, after_v: run
+  // when they are used up.
+  template <typename K, typename V, typename AK, typename AV>
+  __device__ __attribute__((always_inline)) inline void block(const Kv8AttnArgs& a, const Work& w, int blk, int h, unsigned kb, unsigned nan_keys, const float* vb,
+                                                              const float* inv, K k, V v, AK after_k, AV after_v) {
+    if (__builtin_amdgcn_ballot_w64((int)kb > ref + 5 && kb != KV8_NAN)) {  // (5: 1152 2^5 and 448 2^5 are below half's largest)
+      unsigned t = kb == KV8_NAN ? 1u : kb;
+      t = row_butterfly(t, [](unsigned p, unsigned q) { return p > q ? p : q; });
+      const auto r = __builtin_amdgcn_permlane16_swap(t, t, false, false);
+      ref = __builtin_amdgcn_readfirstlane(r[0] > r[1] ? r[0] : r[1]);
+      cq = fmaxf(qs * __uint_as_float((unsigned)ref << 23), 7.8886090522101181e-31f);  // (2^-100: scores that far below 1 are zero beside anything)
+      start_from_m();
+    }
+    const float k_scale = __uint_as_float((unsigned)max((int)kb - ref + 127, 0) << 23);
+    const f16x2 k_mul = {(f16_t)k_scale, (f16_t)k_scale}, k_add = k_mul * f16x2{(f16_t)-1152.f, (f16_t)-1152.f};
+    const f16x2 v_mul = {(f16_t)1.f, (f16_t)1.f}, v_add = {(f16_t)-1152.f, (f16_t)-1152.f};
+    f32x16 s = from_m;
+#pragma unroll
+    for (int f = 0; f < KF; ++f) {
+      const u32x4 raw = k(f >> 1);
+      const f16x8 kf = halves<FMT>(raw[f % 2 * 2], raw[f % 2 * 2 + 1], k_scale, k_mul, k_add);
+#pragma unroll
+      for (int x = 0; x < TERMS; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[x][f], s, 0, 0, 0);
+    }
+    after_k();
+    float p[16];  // of the lane's keys 8j + 4h + i
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 t = *(const f32x4*)&vb[8 * j + 4 * h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_fmaf(s[4 * j + i], cq, t[i]);
+    }
+    if (nan_keys) {
+      asm volatile("; keys marked NaN");  // (keeps the branch: the compiler would make 48 instructions of every block out of it)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (nan_keys >> (8 * (i >> 2) + 4 * h + (i & 3)) & 1u) p[i] = __uint_as_float(0x7FC00000u);
+    }
+    if (32 * blk + 32 > w.first) {  // (uniform)
+      const unsigned see = visible(a, w, blk, h);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(see >> (8 * (i >> 2) + (i & 3)) & 1u)) p[i] = -__builtin_inff();
+    }
+    float mx = p[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, p[i]);
+    if (__builtin_amdgcn_ballot_w64(mx > limit)) {  // some query's maximum moves
+      mx = halves_max(mx);
+      const bool up = mx > limit;
+      const float by = up ? mx - P_TOP : 0.f, corr = !up ? 1.f : limit > 0.f ? __builtin_amdgcn_exp2f(-by) : 0.f;
+      m += by;
+      if (up) limit = P_LIMIT;
+      l *= corr;
+#pragma unroll
+      for (int d = 0; d < PIECES; ++d) o[d] *= corr;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] -= by;
+      start_from_m();
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const f32x4 t = *(const f32x4*)&inv[8 * j + 4 * h];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[4 * j + i] = __builtin_amdgcn_exp2f(p[4 * j + i]);
+        l = __builtin_fmaf(p[4 * j + i], t[i], l);
+      }
+    }
+    f16x8 ph[TERMS][2];
+#pragma unroll
+    for (int x = 0; x < TERMS; ++x)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        ph[x][i >> 3][i & 7] = (f16_t)p[i];
+        if (F32) p[i] -= (float)ph[x][i >> 3][i & 7];
+      }
+#pragma unroll
+    for (int f = 0; f < KF; ++f) {
+      const u32x4 raw = v(f >> 1);
+      const f16x8 vf = halves<FMT>(raw[f % 2 * 2], raw[f % 2 * 2 + 1], 1.f, v_mul, v_add);
+#pragma unroll
+      for (int x = 0; x < TERMS; ++x) o[f >> 1] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf, ph[x][f & 1], o[f >> 1], 0, 0, 0);
+    }
+    after_v();
+  }
+
+  __device__ inline float top() const { return limit > 0.f ? m : NEG_BIG; }
+};
+
+__device__ inline float exponent_of(unsigned vb) { return (float)vb - 127.f; }
+__device__ inline float undo_of(unsigned vb) { return vb == KV8_NAN ? 0.f : __uint_as_float((254u - vb) << 23); }
+
+// where a query's four dims from d on go: the output, or the workspace if the keys are split
+template <typename T, int HD>
+__device__ inline void put(const Kv8AttnArgs& a, const Work& w, int split_out, int x, int d, f32x4 v, float top, float sum_or_inv) {
+  const int r = x / w.group;
+  const int64_t at = (int64_t)(w.row0 + r) * a.n_q + w.head * w.group + (x - r * w.group);
+  if (!split_out) {
+    store4((T*)a.out + at * HD + d, v * sum_or_inv);
+    return;
+  }
+  const int64_t part = (int64_t)w.split * a.rows * a.n_q + at;
+  *(f32x4*)(a.part + part * HD + d) = v;
+  if (d == 0) { a.part_ml[2 * part] = top; a.part_ml[2 * part + 1] = sum_or_inv; }
+}
+
+// ---- few queries (up to 32 of a sequence and kv head): the wavefronts share the keys and are merged through LDS ---------------------
+
+template <int HD, int NWV>
+struct alignas(16) FewLds {
+  float b[NWV][32], inv[NWV][32];  // of a block's keys: V's exponent, and what undoes its scale
+  float m[NWV][32], l[NWV][32];    // the wavefronts' maxima and sums
+  float o[NWV][32][HD + 4];        // ... and outputs (a query's 16 bytes apart from a multiple of the banks)
+};
+
+template <typename T, int HD, int FMT, int NWV>
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 128 && sizeof(T) == 4 ? 1 : 2))) void kv8_attention_few_kernel(Kv8AttnArgs a, Kv8View cache, Kv8AttnMeta meta, int split_out) {
+  constexpr int PIECES = HD / 32;
+  __shared__ FewLds<HD, NWV> L;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, c = lane & 31;
+  const Work w = work_of(a, cache, meta, 32);
+  // the next block is in flight while this one is worked on
+  u32x4 kr[PIECES], vr[PIECES];
+  unsigned kb = 0, vb = 0;  // scale bytes of position c
+  auto load_k = [&](int blk) __attribute__((always_inline)) {
+    const unsigned char* p = w.region + (int64_t)blk * kv8_block_bytes(HD);
+    kb = p[64 * HD + c];
+    vb = p[64 * HD + 32 + c];
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) kr[i] = ((const u32x4*)p)[i * 64 + lane];
   };
-  const int first = a.mask ? n_keys - nr : n_keys;  // positions from here on are visible to whom the mask says
-  if (blk0 + wave < blk1) load(raw, blk0 + wave);
-  for (int blk = blk0 + wave; blk < blk1; blk += NWV) {
-    f16x8 kf[2 * KS], vf[DT];
+  auto load_v = [&](int blk) __attribute__((always_inline)) {
+    const u32x4* p = (const u32x4*)(w.region + (int64_t)blk * kv8_block_bytes(HD));
 #pragma unroll
-    for (int f = 0; f < 2 * KS; ++f) kf[f] = halves<FMT>(raw[f / 2][f % 2 * 2], raw[f / 2][f % 2 * 2 + 1]);
-#pragma unroll
-    for (int f = 0; f < DT; ++f) vf[f] = halves<FMT>(raw[KP + f / 2][f % 2 * 2], raw[KP + f / 2][f % 2 * 2 + 1]);
-    float ks[8], vb[8], vi[8];  // 2^a, b, 2^-b of the lane's keys 4g + i (i < 4) and 16 + 4g + i - 4
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const unsigned kb = raw[KP + VP][i / 4] >> 8 * (i % 4) & 255u, vbyte = raw[KP + VP][2 + i / 4] >> 8 * (i % 4) & 255u;
-      ks[i] = __uint_as_float(kb << 23);
-      vb[i] = (float)vbyte - 127.f;
-      vi[i] = __uint_as_float((254u - vbyte) << 23);
-    }
-    if (blk + NWV < blk1) load(raw, blk + NWV);
-    const bool masked = 32 * blk + 32 > first;  // (uniform)
-#pragma unroll
-    for (int u = 0; u < TILES; ++u) {
-      f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int x = 0; x < TERMS; ++x)
-#pragma unroll
-        for (int t = 0; t < KS; ++t) {
-          s0 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[t], qf[u][x][t], s0, 0, 0, 0);
-          s1 = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[KS + t], qf[u][x][t], s1, 0, 0, 0);
-        }
-      float sv[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) sv[i] = __builtin_fmaf((i < 4 ? s0[i] : s1[i - 4]) * qs[u], ks[i], vb[i]);
-      unsigned see = 0xFFFFFFFFu;
-      if (masked) {
-        const int left = n_keys - 32 * blk, ofs = 32 * blk - first;  // ofs: of the block in the masked positions
-        if (left < 32) see = (1u << left) - 1u;
-        if (a.mask) {
-          const int w = ofs >> 5, sh = ofs & 31;  // (floors: a block that starts in front of them takes its upper bits from word 0)
-          const unsigned lo = w >= 0 ? words[u][w] : 0xFFFFFFFFu, hi = sh && w + 1 < a.mask_words ? words[u][w + 1] : 0u;
-          see &= sh ? lo >> sh | hi << (32 - sh) : lo;
-        }
-        see = see >> 4 * g;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (!(see >> (i < 4 ? i : 12 + i) & 1u)) sv[i] = -__builtin_inff();
-      }
-      float mx = fmaxf(fmaxf(fmaxf(sv[0], sv[1]), fmaxf(sv[2], sv[3])), fmaxf(fmaxf(sv[4], sv[5]), fmaxf(sv[6], sv[7])));
-      const float mn = fmaxf(m[u], query_max(mx) - (float)P_BITS);
-      if (__builtin_amdgcn_ballot_w64(mn != m[u])) {
-        const float corr = __builtin_amdgcn_exp2f(m[u] - mn);
-        l[u] *= corr;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[u][dt] *= corr;
-        m[u] = mn;
-      }
-      float p[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(sv[i] - mn);
-      if (masked) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if (see >> (i < 4 ? i : 12 + i) & 1u) l[u] = __builtin_fmaf(p[i], vi[i], l[u]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) l[u] = __builtin_fmaf(p[i], vi[i], l[u]);
-      }
-      f16x8 ph, pl;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        ph[i] = (f16_t)p[i];
-        if (F32) pl[i] = (f16_t)(p[i] - (float)ph[i]);
-      }
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        o[u][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[dt], ph, o[u][dt], 0, 0, 0);
-        if (F32) o[u][dt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf[dt], pl, o[u][dt], 0, 0, 0);
-      }
-    }
+    for (int i = 0; i < PIECES; ++i) vr[i] = p[(PIECES + i) * 64 + lane];
+  };
+  if (w.blk0 + wave < w.blk1) {
+    load_k(w.blk0 + wave);
+    load_v(w.blk0 + wave);
   }
+  Tile<T, HD, FMT> t;
+  t.start(a, w, w.q0, lane);
+  for (int blk = w.blk0 + wave; blk < w.blk1; blk += NWV) {
+    const unsigned nan_keys = (unsigned)__builtin_amdgcn_ballot_w64(max(kb, vb) == KV8_NAN), k_now = kb;
+    if (h == 0) L.b[wave][c] = exponent_of(vb);
+    else L.inv[wave][c] = undo_of(vb);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const bool more = blk + NWV < w.blk1;
+    t.block(a, w, blk, h, k_now, nan_keys, L.b[wave], L.inv[wave], [&](int i) { return kr[i]; }, [&](int i) { return vr[i]; },
+            [&] { if (more) load_k(blk + NWV); }, [&] { if (more) load_v(blk + NWV); });
+    __builtin_amdgcn_wave_barrier();
+  }
+  // each wavefront brings its own part to the common maximum
+  const float ls = halves_sum(t.l), mw = t.top();
+  if (h == 0) { L.m[wave][c] = mw; L.l[wave][c] = ls; }
+  __syncthreads();
+  float M = L.m[0][c];
+#pragma unroll
+  for (int v = 1; v < NWV; ++v) M = fmaxf(M, L.m[v][c]);
+  const float f = __builtin_amdgcn_exp2f(mw - M);
+#pragma unroll
+  for (int d = 0; d < PIECES; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *(f32x4*)&L.o[wave][c][32 * d + 8 * j + 4 * h] = f32x4{t.o[d][4 * j] * f, t.o[d][4 * j + 1] * f, t.o[d][4 * j + 2] * f, t.o[d][4 * j + 3] * f};
+  if (wave == 0) {
+    float all = 0.f;
+#pragma unroll
+    for (int v = 0; v < NWV; ++v) all += __builtin_amdgcn_exp2f(L.m[v][c] - M) * L.l[v][c];
+    if (h == 0) L.inv[0][c] = split_out ? all : reciprocal(all);
+    else L.b[0][c] = M;
+  }
+  __syncthreads();
+  for (int i = tid; i < 32 * HD / 4; i += NWV * 64) {
+    const int x = i / (HD / 4), d = i % (HD / 4) * 4;
+    if (w.q0 + x >= w.nq) break;
+    f32x4 acc = *(const f32x4*)&L.o[0][x][d];
+#pragma unroll
+    for (int v = 1; v < NWV; ++v) acc += *(const f32x4*)&L.o[v][x][d];
+    put<T, HD>(a, w, split_out, w.q0 + x, d, acc, L.b[0][x], L.inv[0][x]);
+  }
+}
 
-  // ---- merge the wavefronts, a tile at a time
+// ---- many queries: a wavefront has 32 of its own, and the workgroup's four share K and V through LDS --------------------------------
+// (With the keys shared between the wavefronts instead, 32 queries a workgroup, half of the instructions are queries' and merges', and
+// every 32 queries read all of K and V: 1280 rows x 1280 keys x 32 heads 52 us.)
+
+constexpr int STAGE = 2;  // blocks fetched at a time
+template <int HD>
+struct alignas(16) ManyLds {
+  u32x4 codes[2][STAGE][4 * HD];
+  float b[2][STAGE][32], inv[2][STAGE][32];
+  unsigned kb[2][STAGE][32], nan_keys[2][STAGE];
+};
+
+template <typename T, int HD, int FMT>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 && sizeof(T) == 4 ? 1 : 2))) void kv8_attention_many_kernel(Kv8AttnArgs a, Kv8View cache, Kv8AttnMeta meta, int split_out) {
+  constexpr int PIECES = HD / 32, PER = STAGE * 4 * HD / 256;
+  __shared__ ManyLds<HD> L;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, c = lane & 31;
+  const Work w = work_of(a, cache, meta, 128);
+  u32x4 raw[PER];
+  unsigned kb = 0, vb = 0;
+  const int sb = tid >> 5;  // threads below 32 STAGE: a block's scale bytes, position c
+  auto load = [&](int blk) __attribute__((always_inline)) {
 #pragma unroll
-  for (int u = 0; u < TILES; ++u) {
-    if (q0 + 16 * u >= nq) break;  // (uniform)
-    if (u) __syncthreads();
-    const float ls = query_sum(l[u]);
-    if (g == 0) { L.m[wave][c] = m[u]; L.l[wave][c] = ls; }
-#pragma unroll
-    for (int dt = 0; dt < DT; ++dt) *(f32x4*)&L.o[wave][c][16 * dt + 4 * g] = o[u][dt];
-    __syncthreads();
-    for (int i = tid; i < 16 * HD / 4; i += NWV * 64) {
-      const int x = i / (HD / 4), d = i % (HD / 4) * 4, qi = q0 + 16 * u + x, r = qi / group;
-      if (qi >= nq) continue;
-      float M = L.m[0][x], ls = 0.f;
-#pragma unroll
-      for (int w = 1; w < NWV; ++w) M = fmaxf(M, L.m[w][x]);
-      f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int w = 0; w < NWV; ++w) {
-        const float f = __builtin_amdgcn_exp2f(L.m[w][x] - M);
-        ls += f * L.l[w][x];
-        acc += *(const f32x4*)&L.o[w][x][d] * f;
-      }
-      const int64_t at = (int64_t)(row0 + r) * a.n_q + head * group + (qi - r * group);
-      if (split_out) {
-        const int64_t part = (int64_t)split * a.rows * a.n_q + at;
-        *(f32x4*)(a.part + part * HD + d) = acc;
-        if (d == 0) { a.part_ml[2 * part] = M; a.part_ml[2 * part + 1] = ls; }
-      } else {
-        T* to = (T*)a.out + at * HD + d;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) to[j] = (T)finish(acc[j], ls);
-      }
+    for (int i = 0; i < PER; ++i) {
+      const int n = i * 256 + tid, s = n / (4 * HD);
+      raw[i] = ((const u32x4*)(w.region + (int64_t)min(blk + s, w.blk1 - 1) * kv8_block_bytes(HD)))[n % (4 * HD)];
     }
+    if (tid < 32 * STAGE) {
+      const unsigned char* p = w.region + (int64_t)min(blk + sb, w.blk1 - 1) * kv8_block_bytes(HD) + 64 * HD;
+      kb = p[c];
+      vb = p[32 + c];
+    }
+  };
+  auto keep = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) (&L.codes[buf][0][0])[i * 256 + tid] = raw[i];
+    if (tid < 32 * STAGE) {
+      const unsigned long long nan = __builtin_amdgcn_ballot_w64(max(kb, vb) == KV8_NAN);
+      L.b[buf][sb][c] = exponent_of(vb);
+      L.inv[buf][sb][c] = undo_of(vb);
+      L.kb[buf][sb][c] = kb;
+      if (c == 0) L.nan_keys[buf][sb] = (unsigned)(nan >> (lane & 32));
+    }
+  };
+  if (w.blk0 < w.blk1) load(w.blk0);
+  Tile<T, HD, FMT> t;
+  const int q0 = w.q0 + 32 * wave;
+  t.start(a, w, q0, lane);
+  if (w.blk0 < w.blk1) keep(0);
+  __syncthreads();
+  if (q0 >= w.nq) {  // no queries: only the fetching
+    for (int blk = w.blk0, buf = 0; blk < w.blk1; blk += STAGE, buf ^= 1) {
+      if (blk + STAGE < w.blk1) {
+        load(blk + STAGE);
+        keep(buf ^ 1);
+      }
+      __syncthreads();
+    }
+    return;
   }
+  for (int blk = w.blk0, buf = 0; blk < w.blk1; blk += STAGE, buf ^= 1) {
+    const bool more = blk + STAGE < w.blk1;
+    if (more) load(blk + STAGE);
+#pragma unroll
+    for (int s = 0; s < STAGE; ++s) {  // (blocks behind the last one, whose codes are read again, are seen by nobody)
+      const unsigned nan_keys = __builtin_amdgcn_readfirstlane(L.nan_keys[buf][s]);
+      t.block(a, w, blk + s, h, L.kb[buf][s][c], nan_keys, L.b[buf][s], L.inv[buf][s], [&](int i) { return L.codes[buf][s][i * 64 + lane]; },
+              [&](int i) { return L.codes[buf][s][(PIECES + i) * 64 + lane]; }, [] {}, [] {});
+    }
+    if (more) keep(buf ^ 1);
+    __syncthreads();
+  }
+  const int x = q0 + c;
+  const float ls = halves_sum(t.l), f = split_out ? ls : reciprocal(ls);
+  if (x >= w.nq) return;
+#pragma unroll
+  for (int d = 0; d < PIECES; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      put<T, HD>(a, w, split_out, x, 32 * d + 8 * j + 4 * h, f32x4{t.o[d][4 * j], t.o[d][4 * j + 1], t.o[d][4 * j + 2], t.o[d][4 * j + 3]}, t.top(), f);
 }
 
 // the shares of a sequence's keys joined: a wavefront a (row, head)
@@ -283,9 +449,10 @@ __global__ __launch_bounds__(256) void kv8_attention_join_kernel(Kv8AttnArgs a, 
     for (int j = 0; j < N; ++j)
       if (lane * N < HD) acc[j] += f * a.part[i * HD + lane * N + j];
   }
+  const float inv = reciprocal(ls);
 #pragma unroll
   for (int j = 0; j < N; ++j)
-    if (lane * N < HD) ((T*)a.out)[at * HD + lane * N + j] = (T)finish(acc[j], ls);
+    if (lane * N < HD) ((T*)a.out)[at * HD + lane * N + j] = (T)(acc[j] * inv);
 }
 
 constexpr int64_t MAX_PARTIALS = 1 << 16;
@@ -307,10 +474,9 @@ Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, in
     if (nr && n_keys[b] > longest) longest = n_keys[b];
   }
   const int64_t queries = (int64_t)rows_max * (n_q / n_kv);
-  p.tiles = queries <= 16 ? 1 : queries <= 32 || dtype == DLM_F32 ? 2 : 4;
-  p.waves = 4;
+  p.queries = queries <= 32 ? 32 : 128;
   int64_t wgs = 0;
-  for (int b = 0; b < n_seqs; ++b) wgs += ((int64_t)(row_off[b + 1] - row_off[b]) * (n_q / n_kv) + 16 * p.tiles - 1) / (16 * p.tiles) * n_kv;
+  for (int b = 0; b < n_seqs; ++b) wgs += ((int64_t)(row_off[b + 1] - row_off[b]) * (n_q / n_kv) + p.queries - 1) / p.queries * n_kv;
   const int blocks = (longest + 31) / 32;
   p.splits = 1;
   p.chunk = blocks ? blocks : 1;
@@ -322,6 +488,7 @@ Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, in
     if (s > 1) {
       int chunk = (int)((blocks + s - 1) / s);
       if (chunk < 8) chunk = 8;
+      chunk += chunk & 1;
       if (chunk < blocks) { p.chunk = chunk; p.splits = (blocks + chunk - 1) / chunk; }
     }
   }
@@ -333,10 +500,8 @@ namespace {
 template <typename T, int HD, int FMT>
 void launch_shape(const Kv8View& c, const Kv8AttnArgs& a, const Kv8AttnMeta& m, const Kv8AttnPlan& p, hipStream_t st) {
   const int grid = (int)(p.items * c.n_kv), sp = p.splits > 1;
-  constexpr int MOST = std::is_same<T, float>::value ? 2 : 4;
-  if (p.tiles == 1) kv8_attention_kernel<T, HD, FMT, 1, 4><<<grid, 256, 0, st>>>(a, c, m, sp);
-  else if (p.tiles == 2) kv8_attention_kernel<T, HD, FMT, 2, 4><<<grid, 256, 0, st>>>(a, c, m, sp);
-  else kv8_attention_kernel<T, HD, FMT, MOST, 4><<<grid, 256, 0, st>>>(a, c, m, sp);
+  if (p.queries == 32) kv8_attention_few_kernel<T, HD, FMT, 4><<<grid, 256, 0, st>>>(a, c, m, sp);
+  else kv8_attention_many_kernel<T, HD, FMT><<<grid, 256, 0, st>>>(a, c, m, sp);
   if (sp) kv8_attention_join_kernel<T, HD><<<(int)(((int64_t)a.rows * a.n_q + 3) / 4), 256, 0, st>>>(a, m);
 }
 template <typename T, int HD>

@@ -150,14 +150,9 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(const T* __restrict__ k,
   const unsigned here = (unsigned)((1ull << w.hi) - (1ull << w.lo));
   for (int i = threadIdx.x; i < kv8_block_bytes(HD) / 4; i += 256) {
     unsigned bits;  // which of the word's bytes
-    if (i < 8 * HD) {  // K: one position's, f = 2 (i / 256) + half
-      const int f = i / 256 * 2 + (i >> 1 & 1), p = f / (HD / 32) * 16 + (i >> 2 & 15);
-      bits = here >> p & 1 ? 15u : 0u;
-    } else if (i < 16 * HD) {  // V: four positions'
-      bits = here >> ((i >> 2 & 63) / 16 * 4 + (i & 1) * 16) & 15u;
-    } else {
-      bits = here >> ((i - 16 * HD) / 4 * 4 + (i & 1) * 16) & 15u;
-    }
+    if (i < 8 * HD) bits = here >> (i >> 2 & 31) & 1 ? 15u : 0u;                      // K: one position's
+    else if (i < 16 * HD) bits = here >> ((i & 3) * 8 + (i >> 2 & 32) / 8) & 15u;     // V: four positions'
+    else bits = here >> (i & 7) * 4 & 15u;
     const unsigned word = ((const unsigned*)img)[i];
     if (bits == 15u) ((unsigned*)out)[i] = word;
     else

@@ -8,10 +8,10 @@ Tolerances, derived before the first run (u = 2^-24, half a step of fp32; a roun
                  roundings of a log2 score plus V's exponent: d_j = (hd + 4) u sum|q_i K_ji| / sqrt(hd) + 8 u (|s_j| + 60 ln 2); a
                  probability is off by 2 d of itself (its own and the sum's) and by its rounding to half (2^-11 bf16, two terms 2^-21
                  fp32); sums over n keys 2 n u.  So (2 max d + r + (2 n + 64) u) sum_j p_j |V_j|, then the output's rounding.  Half ends:
-                 what multiplies the codes is p_j 2^b_j (b: the exponent of V_j's scale) with its largest at 2^15, and below 2^-14
-                 half's steps are 2^-24, so each is off by up to 2^-25 = 2^-40 of the largest: 2^-40 max_j(p_j 2^b_j) sum_i |code_i|.
-                 With t the largest magnitude of a vector and M the largest code, 2^b <= 2 t / M and |code| <= M |V| / t: at most
-                 2^-39 max_j(p_j t_j) sum_i |V_i| / t_i
+                 what multiplies the codes is p_j 2^b_j (b: the exponent of V_j's scale) with its largest at 2^P or above (P = 8 with bf16,
+                 13 with fp32 outputs), and below 2^-14 half's steps are 2^-24, so each is off by up to 2^-25 = 2^-(25+P) of the
+                 largest: 2^-(25+P) max_j(p_j 2^b_j) sum_i |code_i|.  With t the largest magnitude of a vector and M the largest code,
+                 2^b <= 2 t / M and |code| <= M |V| / t: at most 2^-(24+P) max_j(p_j t_j) sum_i |V_i| / t_i
 """
 import math
 
@@ -181,7 +181,7 @@ def _bound(q, k, v, see, dtype):
         d = ((hd + 4) * U + (2.0 ** -21 if dtype == F32 else 0.0)) * size + 8 * U * (np.abs(s) + 60 * math.log(2))
         rel = 2 * np.where(see, d, 0.0).max(-1, initial=0.0) + (2.0 ** -21 if dtype == F32 else 2.0 ** -11) + (2 * seen + 64) * U
         p, t = o_kv8.probabilities(s, see), np.abs(V).max(-1, initial=0.0)
-        out[:, h] = rel[:, None] * (p @ np.abs(V)) + 2.0 ** -39 * (p * t).max(-1, initial=0.0)[:, None] * (see @ (np.abs(V) / np.maximum(t, 1e-300)[:, None]))
+        out[:, h] = rel[:, None] * (p @ np.abs(V)) + 2.0 ** (-37 if dtype == F32 else -32) * (p * t).max(-1, initial=0.0)[:, None] * (see @ (np.abs(V) / np.maximum(t, 1e-300)[:, None]))
     return out
 
 
