@@ -417,28 +417,45 @@ def _int32s(name, v, n):
     return _int_packer(len(v))(*whole)
 
 
-def _on_gpu(name, t):
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+def _gpu_of(name, t):
+    """The index of the current GPU, which t is on."""
+    dev = t.get_device()  # (-1: on none)
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"{name}: not on the current GPU")
+    return dev
+
+
+def _on_gpu(name, t, dev):
+    if t.get_device() != dev:
         raise ValueError(f"{name}: not on the current GPU")
 
 
-def _row_stride(name, t, shape, dtypes):
-    """The stride between the rows (first axis) of a device tensor whose rows are contiguous; shape: None for an axis of any size."""
-    _on_gpu(name, t)
+def _row_stride(name, t, dev, tail, dtypes):
+    """The stride between the rows (first axis) of a tensor on GPU `dev` whose rows are contiguous; tail: their shape, None for any."""
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: not on the current GPU")
     if t.dtype not in dtypes:
         raise ValueError(f"{name}: {t.dtype}, not one of {dtypes}")
-    have, strides = t.shape, t.stride()
-    if len(have) != len(shape):
-        raise ValueError(f"{name}: shape {tuple(have)} where {shape} is read")
-    width = 1
-    for i in range(len(shape) - 1, 0, -1):
-        if strides[i] != width and have[i] != 1:
+    have = t.shape
+    if len(have) != len(tail) + 1:
+        raise ValueError(f"{name}: {len(have)} dimensions where {len(tail) + 1} are read")
+    width, dense = 1, t.is_contiguous()
+    strides = None if dense else t.stride()
+    for i in range(len(tail), 0, -1):
+        n = have[i]
+        if tail[i - 1] is not None and tail[i - 1] != n:
+            raise ValueError(f"{name}: rows of shape {tuple(have[1:])} where {tail} is read")
+        if not dense and strides[i] != width and n != 1:
             raise ValueError(f"{name}: strides {strides}: a row is not contiguous")
-        width *= have[i]
-    for n, m in zip(shape, have):
-        if n is not None and n != m:
-            raise ValueError(f"{name}: shape {tuple(have)} where {shape} is read")
-    return strides[0] if have[0] > 1 else width
+        width *= n
+    return width if dense or have[0] < 2 else strides[0]
+
+
+def _vector(name, t, dev, n, dtype):
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: not on the current GPU")
+    if t.dtype is not dtype or t.dim() != 1 or t.size(0) != n or not t.is_contiguous():
+        raise ValueError(f"{name}: not a contiguous vector of {n} x {dtype}")
 
 
 _FLOATS = (torch.float32, torch.bfloat16)
@@ -460,15 +477,15 @@ class Kv8Cache:
 
 
 def _kv8_spans(cache, k, v, row_offsets, start, slot):
-    n = len(start)
+    n, dev, tail = len(start), _gpu_of("k", k), (cache.n_kv, cache.head_dim)
     off = _int32s("row_offsets", row_offsets, n + 1)
-    shape = (None, cache.n_kv, cache.head_dim)
-    stride = _row_stride("k", k, shape, _FLOATS)
-    if _row_stride("v", v, shape, (k.dtype,)) != stride:
+    stride = _row_stride("k", k, dev, tail, _FLOATS)
+    if _row_stride("v", v, dev, tail, (k.dtype,)) != stride:
         raise ValueError("k and v have different strides between rows")
-    if k.shape[0] != v.shape[0] or row_offsets[n] > k.shape[0]:
-        raise ValueError(f"{k.shape[0]} rows of k and {v.shape[0]} of v where {row_offsets[n]} are read")
-    _on_gpu("cache", cache.data)
+    rows = k.shape[0]
+    if rows != v.shape[0] or row_offsets[n] > rows:
+        raise ValueError(f"{rows} rows of k and {v.shape[0]} of v where {row_offsets[n]} are read")
+    _on_gpu("cache", cache.data, dev)
     return cache._ref, k.data_ptr(), v.data_ptr(), stride, _DTYPE_CODES[k.dtype], off, _int32s("start", start, n), _int32s("slot", slot, n), n, _stream()
 
 
@@ -496,31 +513,31 @@ def dlm_kv8_attention(cache, q, row_offsets, n_keys, slot=None, mask=None, out=N
     """q: device tensor [rows, n_q, head_dim] (rows may be strided); mask: device int32 [rows, words], bits as in include/dlm.h; out:
     contiguous, of q's shape and dtype (None: a new one); workspace: a contiguous device tensor of at least
     dlm_kv8_attention_workspace bytes that nothing else uses meanwhile (None: a new one); the rest: host int lists.  Returns out."""
-    n = len(n_keys)
-    stride = _row_stride("q", q, (None, None, cache.head_dim), _FLOATS)
-    rows, n_q = q.shape[0], q.shape[1]
+    n, dev = len(n_keys), _gpu_of("q", q)
+    stride = _row_stride("q", q, dev, (None, cache.head_dim), _FLOATS)
+    rows, n_q, hd = q.shape
     off = _int32s("row_offsets", row_offsets, n + 1)
     packed = int(row_offsets[n])
     if packed > rows:
         raise ValueError(f"{rows} rows of q where {packed} are read")
     if out is None:
-        out = torch.empty((rows, n_q, cache.head_dim), dtype=q.dtype, device=q.device)
-    elif _row_stride("out", out, (rows, n_q, cache.head_dim), (q.dtype,)) != n_q * cache.head_dim:
-        raise ValueError("out is not contiguous")
+        out = torch.empty((rows, n_q, hd), dtype=q.dtype, device=q.device)
+    elif _row_stride("out", out, dev, (n_q, hd), (q.dtype,)) != n_q * hd or out.shape[0] != rows:
+        raise ValueError("out is not contiguous, or has not q's rows")
     words = 0
     if mask is not None:
         words = mask.shape[-1]
-        if _row_stride("mask", mask, (None, None), (torch.int32,)) != words or mask.shape[0] < packed:
+        if _row_stride("mask", mask, dev, (words,), (torch.int32,)) != words or mask.shape[0] < packed:
             raise ValueError(f"mask: {tuple(mask.shape)} for {packed} rows, or not contiguous")
-    _on_gpu("cache", cache.data)
+    _on_gpu("cache", cache.data, dev)
     if rows == 0:
         return out
     L = lib()
-    size = L.dlm_kv8_attention_workspace(packed, n_q, cache.head_dim)
+    size = L.dlm_kv8_attention_workspace(packed, n_q, hd)
     if workspace is None:
         workspace = torch.empty(size, dtype=torch.uint8, device=q.device) if size else None
     else:
-        _on_gpu("workspace", workspace)
+        _on_gpu("workspace", workspace, dev)
         if not workspace.is_contiguous():
             raise ValueError("workspace is not contiguous")
         size = workspace.numel() * workspace.element_size()
@@ -533,19 +550,19 @@ def dlm_qk_norm_rope(x, positions, n_q, n_kv, head_dim, q_gain=None, k_gain=None
     """x: device tensor [rows, columns] whose first (n_q + n_kv) * head_dim columns are the query and key heads (rows may be
     strided); positions: device int32 [rows]; gains: [head_dim] of x's dtype, or None; out: as x (x itself: in place; None: a new
     tensor of those columns alone).  Returns out."""
-    width = (n_q + n_kv) * head_dim
-    stride = _row_stride("x", x, (None, None), _FLOATS)
-    rows, dtype = x.shape[0], (x.dtype,)
+    width, dev, dtype = (n_q + n_kv) * head_dim, _gpu_of("x", x), x.dtype
+    stride = _row_stride("x", x, dev, (None,), _FLOATS)
+    rows, columns = x.shape
     if out is None:
-        out = torch.empty((rows, width), dtype=x.dtype, device=x.device)
-    out_stride = _row_stride("out", out, (rows, None), dtype)
-    if x.shape[1] < width or out.shape[1] < width:
-        raise ValueError(f"rows of {x.shape[1]} and {out.shape[1]} columns where {width} are read and written")
-    if _row_stride("positions", positions, (rows,), (torch.int32,)) != 1:
-        raise ValueError("positions are not contiguous")
-    for name, gain in (("q_gain", q_gain), ("k_gain", k_gain)):
-        if gain is not None and _row_stride(name, gain, (head_dim,), dtype) != 1:
-            raise ValueError(f"{name} is not contiguous")
+        out = torch.empty((rows, width), dtype=dtype, device=x.device)
+    out_stride = stride if out is x else _row_stride("out", out, dev, (None,), (dtype,))
+    if columns < width or out.shape[1] < width or out.shape[0] != rows:
+        raise ValueError(f"rows of {columns} and {out.shape[1]} columns where {width} are read and written, or not as many rows of out")
+    _vector("positions", positions, dev, rows, torch.int32)
+    if q_gain is not None:
+        _vector("q_gain", q_gain, dev, head_dim, dtype)
+    if k_gain is not None:
+        _vector("k_gain", k_gain, dev, head_dim, dtype)
     if rows == 0:
         return out
     _check(lib().dlm_qk_norm_rope(x.data_ptr(), stride, rows, n_q, n_kv, head_dim, _DTYPE_CODES[x.dtype], _ptr(q_gain), _ptr(k_gain), eps, theta,

@@ -61,12 +61,11 @@ __device__ inline int seq_of(const int32_t* off, int n_seqs, int i) {
 void launch_kv8_write(const Kv8View& c, int format, int hd, const void* k, const void* v, int64_t stride, int dtype, const Kv8Meta& m, hipStream_t st);
 void launch_kv8_read(const Kv8View& c, int format, int hd, void* k, void* v, int64_t stride, int dtype, const Kv8Meta& m, hipStream_t st);
 struct Kv8AttnPlan {
-  int queries;  // of a workgroup
-  int chunk;    // 32-position blocks of a split's share of the keys
+  int chunk;    // 32-position blocks of a workgroup's share of the keys
   int splits;   // most shares of a sequence (1: the workgroups write the output)
-  int64_t items;
+  int64_t items, item_off[DLM_MAX_SEQS + 1];  // (32-query tile, share) pairs: all, and of the sequences before each
 };
-Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, int n_seqs, int n_q, int n_kv, int hd, int dtype);
+Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, int n_seqs, int n_q, int n_kv);
 size_t kv8_attention_partials(int64_t rows, int n_q);  // most (split, row, head) triples a plan for that many rows has
 struct Kv8AttnArgs {
   const void* q;

@@ -161,15 +161,10 @@ extern "C" int dlm_kv8_attention(const dlm_kv8_cache* c, const void* q, int64_t 
   const size_t need = dlm_kv8_attention_workspace(rows, n_q, c->head_dim);
   REQUIRE(workspace_bytes >= need && (workspace || !need), DLM_ECAPACITY, "dlm_kv8_attention: workspace of %zu bytes < %zu", workspace ? workspace_bytes : 0, need);
   if (rows == 0) return DLM_OK;
-  Kv8AttnPlan p = kv8_attention_plan(row_offsets, n_keys, n_seqs, n_q, c->n_kv, c->head_dim, dtype);
+  const Kv8AttnPlan p = kv8_attention_plan(row_offsets, n_keys, n_seqs, n_q, c->n_kv);
+  REQUIRE((int64_t)rows * (n_q / c->n_kv) <= INT32_MAX && p.items * c->n_kv < INT32_MAX, DLM_ECAPACITY, "dlm_kv8_attention: too many rows for one launch");
   m.chunk = p.chunk;
-  for (int b = 0; b < n_seqs; ++b) {
-    const int64_t queries = (int64_t)(row_offsets[b + 1] - row_offsets[b]) * (n_q / c->n_kv);
-    const int splits = ((n_keys[b] + 31) / 32 + p.chunk - 1) / p.chunk;
-    p.items += (queries + p.queries - 1) / p.queries * (splits > 1 ? splits : 1);
-    REQUIRE(queries <= INT32_MAX && p.items * c->n_kv < INT32_MAX, DLM_ECAPACITY, "dlm_kv8_attention: too many rows for one launch");
-    m.item_off[b + 1] = (int32_t)p.items;
-  }
+  for (int b = 0; b <= n_seqs; ++b) m.item_off[b] = (int32_t)p.item_off[b];
   Kv8AttnArgs a{q, q_stride, out, mask, mask_words, n_q, rows, nullptr, nullptr};
   a.part = (float*)workspace;
   a.part_ml = a.part + (size_t)p.splits * rows * n_q * c->head_dim;

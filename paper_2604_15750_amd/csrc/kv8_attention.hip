@@ -73,29 +73,9 @@ __device__ inline float reciprocal(float l) { return l > 0.f ? 1.f / l : l == 0.
 
 // What a workgroup works on
 struct Work {
-  int head, b, row0, nq, group, q0, split, blk0, blk1, n_keys, first;  // first: positions from here on are visible to whom the mask says
+  int head, row0, nq, group, q0, split, blk0, blk1, n_keys, first;  // first: positions from here on are visible to whom the mask says
   const unsigned char* region;
 };
-// (the heads of an item are neighbours: where their number is a multiple of 8 all items of a head are on one XCD, and its L2 has the head's K and V)
-__device__ inline Work work_of(const Kv8AttnArgs& a, const Kv8View& cache, const Kv8AttnMeta& meta, int queries) {
-  Work w;
-  w.head = blockIdx.x % cache.n_kv;
-  const int item = blockIdx.x / cache.n_kv;
-  w.b = seq_of(meta.item_off, meta.n_seqs, item);
-  w.row0 = meta.row_off[w.b];
-  w.n_keys = meta.n_keys[w.b];
-  w.group = a.n_q / cache.n_kv;
-  const int nr = meta.row_off[w.b + 1] - w.row0;
-  w.nq = nr * w.group;
-  const int qtiles = (w.nq + queries - 1) / queries, rel = item - meta.item_off[w.b];
-  w.split = rel / qtiles;
-  w.q0 = (rel - w.split * qtiles) * queries;
-  w.blk0 = w.split * meta.chunk;
-  w.blk1 = min((w.n_keys + 31) >> 5, w.blk0 + meta.chunk);
-  w.first = a.mask ? w.n_keys - nr : w.n_keys;
-  w.region = cache.data + ((int64_t)meta.slot[w.b] * cache.n_kv + w.head) * cache.head_bytes;
-  return w;
-}
 
 // 32 queries of a wavefront and their running softmax
 template <typename T, int HD, int FMT>
@@ -109,9 +89,9 @@ struct Tile {
   int ref;                         // biased exponent that K's scales are relative to
   const uint32_t* words;           // of the query's row in the mask
 
-  __device__ inline void start(const Kv8AttnArgs& a, const Work& w, int q0, int lane) {
-    const int h = lane >> 5, x = q0 + (lane & 31), r = x < w.nq ? x / w.group : 0, hq = x < w.nq ? x - r * w.group : 0;
-    const T* from = (const T*)a.q + (int64_t)(w.row0 + r) * a.q_stride + (w.head * w.group + hq) * HD + 16 * h;
+  __device__ inline void start(const T* q, int64_t q_stride, const Kv8AttnArgs& a, const Work& w, int lane) {
+    const int h = lane >> 5, x = w.q0 + (lane & 31), r = x < w.nq ? x / w.group : 0, hq = x < w.nq ? x - r * w.group : 0;
+    const T* from = q + (int64_t)(w.row0 + r) * q_stride + (w.head * w.group + hq) * HD + 16 * h;
     words = a.mask + (int64_t)(w.row0 + r) * a.mask_words;
     float v[KF][8];
     unsigned top = 0;
@@ -269,21 +249,44 @@ __device__ inline void put(const Kv8AttnArgs& a, const Work& w, int split_out, i
   if (d == 0) { a.part_ml[2 * part] = top; a.part_ml[2 * part + 1] = sum_or_inv; }
 }
 
-// ---- few queries (up to 32 of a sequence and kv head): the wavefronts share the keys and are merged through LDS ---------------------
+constexpr int NWV = 4;  // wavefronts of a workgroup, which share its keys
 
-template <int HD, int NWV>
-struct alignas(16) FewLds {
+template <int HD>
+struct alignas(16) AttnLds {
   float b[NWV][32], inv[NWV][32];  // of a block's keys: V's exponent, and what undoes its scale
   float m[NWV][32], l[NWV][32];    // the wavefronts' maxima and sums
   float o[NWV][32][HD + 4];        // ... and outputs (a query's 16 bytes apart from a multiple of the banks)
 };
 
-template <typename T, int HD, int FMT, int NWV>
-__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 128 && sizeof(T) == 4 ? 1 : 2))) void kv8_attention_few_kernel(Kv8AttnArgs a, Kv8View cache, Kv8AttnMeta meta, int split_out) {
+template <typename T, int HD, int FMT>
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 128 && sizeof(T) == 4 ? 1 : 2))) void kv8_attention_kernel(
+    const unsigned char* __restrict__ data, int head_blocks, int n_kv, const T* __restrict__ q, int64_t q_stride, int n_q, int rows, int chunk, int one_keys, int one_slot,
+    int split_out, Kv8AttnArgs a, Kv8AttnMeta meta) {
   constexpr int PIECES = HD / 32;
-  __shared__ FewLds<HD, NWV> L;
+  __shared__ AttnLds<HD> L;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, c = lane & 31;
-  const Work w = work_of(a, cache, meta, 32);
+  // (the heads of an item are neighbours: where their number is a multiple of 8 all items of a head are on one XCD, and its L2 has the head's K and V)
+  Work w;
+  w.head = blockIdx.x % n_kv;
+  w.group = n_q / n_kv;
+  int item = blockIdx.x / n_kv, nr = rows, slot = one_slot;
+  w.row0 = 0;
+  w.n_keys = one_keys;
+  if (one_slot < 0) {  // (a single sequence's figures arrive in registers instead of by two trips to memory)
+    const int b = seq_of(meta.item_off, meta.n_seqs, item);
+    w.row0 = meta.row_off[b];
+    nr = meta.row_off[b + 1] - w.row0;
+    w.n_keys = meta.n_keys[b];
+    slot = meta.slot[b];
+    item -= meta.item_off[b];
+  }
+  w.nq = nr * w.group;
+  const int qtiles = (w.nq + 31) >> 5;
+  w.split = item / qtiles;
+  w.q0 = (item - w.split * qtiles) * 32;
+  w.blk0 = w.split * chunk;
+  w.blk1 = min((w.n_keys + 31) >> 5, w.blk0 + chunk);
+  w.region = data + ((int64_t)slot * n_kv + w.head) * head_blocks * kv8_block_bytes(HD);
   // the next block is in flight while this one is worked on
   u32x4 kr[PIECES], vr[PIECES];
   unsigned kb = 0, vb = 0;  // scale bytes of position c
@@ -303,8 +306,9 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 
     load_k(w.blk0 + wave);
     load_v(w.blk0 + wave);
   }
+  w.first = a.mask ? w.n_keys - nr : w.n_keys;
   Tile<T, HD, FMT> t;
-  t.start(a, w, w.q0, lane);
+  t.start(q, q_stride, a, w, lane);
   for (int blk = w.blk0 + wave; blk < w.blk1; blk += NWV) {
     const unsigned nan_keys = (unsigned)__builtin_amdgcn_ballot_w64(max(kb, vb) == KV8_NAN), k_now = kb;
     if (h == 0) L.b[wave][c] = exponent_of(vb);
@@ -347,152 +351,81 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 
   }
 }
 
-// ---- many queries: a wavefront has 32 of its own, and the workgroup's four share K and V through LDS --------------------------------
-// (With the keys shared between the wavefronts instead, 32 queries a workgroup, half of the instructions are queries' and merges', and
-// every 32 queries read all of K and V: 1280 rows x 1280 keys x 32 heads 52 us.)
-
-constexpr int STAGE = 2;  // blocks fetched at a time
-template <int HD>
-struct alignas(16) ManyLds {
-  u32x4 codes[2][STAGE][4 * HD];
-  float b[2][STAGE][32], inv[2][STAGE][32];
-  unsigned kb[2][STAGE][32], nan_keys[2][STAGE];
-};
-
-template <typename T, int HD, int FMT>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(HD == 128 && sizeof(T) == 4 ? 1 : 2))) void kv8_attention_many_kernel(Kv8AttnArgs a, Kv8View cache, Kv8AttnMeta meta, int split_out) {
-  constexpr int PIECES = HD / 32, PER = STAGE * 4 * HD / 256;
-  __shared__ ManyLds<HD> L;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, c = lane & 31;
-  const Work w = work_of(a, cache, meta, 128);
-  u32x4 raw[PER];
-  unsigned kb = 0, vb = 0;
-  const int sb = tid >> 5;  // threads below 32 STAGE: a block's scale bytes, position c
-  auto load = [&](int blk) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int n = i * 256 + tid, s = n / (4 * HD);
-      raw[i] = ((const u32x4*)(w.region + (int64_t)min(blk + s, w.blk1 - 1) * kv8_block_bytes(HD)))[n % (4 * HD)];
-    }
-    if (tid < 32 * STAGE) {
-      const unsigned char* p = w.region + (int64_t)min(blk + sb, w.blk1 - 1) * kv8_block_bytes(HD) + 64 * HD;
-      kb = p[c];
-      vb = p[32 + c];
-    }
-  };
-  auto keep = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < PER; ++i) (&L.codes[buf][0][0])[i * 256 + tid] = raw[i];
-    if (tid < 32 * STAGE) {
-      const unsigned long long nan = __builtin_amdgcn_ballot_w64(max(kb, vb) == KV8_NAN);
-      L.b[buf][sb][c] = exponent_of(vb);
-      L.inv[buf][sb][c] = undo_of(vb);
-      L.kb[buf][sb][c] = kb;
-      if (c == 0) L.nan_keys[buf][sb] = (unsigned)(nan >> (lane & 32));
-    }
-  };
-  if (w.blk0 < w.blk1) load(w.blk0);
-  Tile<T, HD, FMT> t;
-  const int q0 = w.q0 + 32 * wave;
-  t.start(a, w, q0, lane);
-  if (w.blk0 < w.blk1) keep(0);
-  __syncthreads();
-  if (q0 >= w.nq) {  // no queries: only the fetching
-    for (int blk = w.blk0, buf = 0; blk < w.blk1; blk += STAGE, buf ^= 1) {
-      if (blk + STAGE < w.blk1) {
-        load(blk + STAGE);
-        keep(buf ^ 1);
-      }
-      __syncthreads();
-    }
-    return;
-  }
-  for (int blk = w.blk0, buf = 0; blk < w.blk1; blk += STAGE, buf ^= 1) {
-    const bool more = blk + STAGE < w.blk1;
-    if (more) load(blk + STAGE);
-#pragma unroll
-    for (int s = 0; s < STAGE; ++s) {  // (blocks behind the last one, whose codes are read again, are seen by nobody)
-      const unsigned nan_keys = __builtin_amdgcn_readfirstlane(L.nan_keys[buf][s]);
-      t.block(a, w, blk + s, h, L.kb[buf][s][c], nan_keys, L.b[buf][s], L.inv[buf][s], [&](int i) { return L.codes[buf][s][i * 64 + lane]; },
-              [&](int i) { return L.codes[buf][s][(PIECES + i) * 64 + lane]; }, [] {}, [] {});
-    }
-    if (more) keep(buf ^ 1);
-    __syncthreads();
-  }
-  const int x = q0 + c;
-  const float ls = halves_sum(t.l), f = split_out ? ls : reciprocal(ls);
-  if (x >= w.nq) return;
-#pragma unroll
-  for (int d = 0; d < PIECES; ++d)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      put<T, HD>(a, w, split_out, x, 32 * d + 8 * j + 4 * h, f32x4{t.o[d][4 * j], t.o[d][4 * j + 1], t.o[d][4 * j + 2], t.o[d][4 * j + 3]}, t.top(), f);
-}
-
-// the shares of a sequence's keys joined: a wavefront a (row, head)
+// the shares of a sequence's keys joined: a wavefront a (row, head); a lane holds a share's weight, then the shares' outputs are added
+// (one share after the other, with the weights computed on the way: 48 rows x 28 heads x 17 shares 10.8 us)
 template <typename T, int HD>
 __global__ __launch_bounds__(256) void kv8_attention_join_kernel(Kv8AttnArgs a, Kv8AttnMeta meta) {
-  constexpr int N = HD / 64 ? HD / 64 : 1;
-  const int lane = threadIdx.x & 63;
+  constexpr int N = HD / 64 ? HD / 64 : 1, AHEAD = 8;
+  typedef float vec __attribute__((ext_vector_type(N)));
+  const int lane = threadIdx.x & 63, d = lane * N & (HD - 1);
   const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), all = (int64_t)a.rows * a.n_q;
   if (at >= all) return;
   const int row = (int)(at / a.n_q), b = seq_of(meta.row_off, meta.n_seqs, row);
-  const int splits = max(1, ((meta.n_keys[b] + 31) / 32 + meta.chunk - 1) / meta.chunk);
-  float M = NEG_BIG;
-  for (int s = 0; s < splits; ++s) M = fmaxf(M, a.part_ml[2 * (s * all + at)]);
-  float ls = 0.f, acc[N] = {};
-  for (int s = 0; s < splits; ++s) {
-    const int64_t i = s * all + at;
-    const float f = __builtin_amdgcn_exp2f(a.part_ml[2 * i] - M);
-    ls += f * a.part_ml[2 * i + 1];
+  const int shares = max(1, ((meta.n_keys[b] + 31) / 32 + meta.chunk - 1) / meta.chunk);
+  const float* ml = a.part_ml + 2 * (min(lane, shares - 1) * all + at);
+  const float top = lane < shares ? ml[0] : NEG_BIG, M = wave_max(top), w = __builtin_amdgcn_exp2f(top - M);
+  const float inv = reciprocal(wave_sum(lane < shares ? w * ml[1] : 0.f));
+  vec acc = 0.f;
+  for (int s0 = 0; s0 < shares; s0 += AHEAD) {
+    vec v[AHEAD];
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      if (lane * N < HD) acc[j] += f * a.part[i * HD + lane * N + j];
+    for (int i = 0; i < AHEAD; ++i) v[i] = *(const vec*)(a.part + (min(s0 + i, shares - 1) * all + at) * HD + d);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) acc += v[i] * (s0 + i < shares ? __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), min(s0 + i, 63))) : 0.f);
   }
-  const float inv = reciprocal(ls);
 #pragma unroll
   for (int j = 0; j < N; ++j)
-    if (lane * N < HD) ((T*)a.out)[at * HD + lane * N + j] = (T)(acc[j] * inv);
+    if (lane * N < HD) ((T*)a.out)[at * HD + d + j] = (T)(acc[j] * inv);
 }
 
-constexpr int64_t MAX_PARTIALS = 1 << 16;
-constexpr int MAX_SPLITS = 32;
+constexpr int64_t MAX_PARTIALS = 1 << 16;  // (share, row, head) triples: 34 MB of workspace at a head dim of 128
+constexpr int MAX_SHARES = 32, CUS = 256;
+
+int blocks_of(int n_keys) { return (n_keys + 31) / 32; }
+int64_t tiles_of(int rows, int group) { return ((int64_t)rows * group + 31) / 32; }
 
 }  // namespace
 
 size_t kv8_attention_partials(int64_t rows, int n_q) {
   const int64_t all = rows * n_q;
-  return 2 * all > MAX_PARTIALS ? 0 : (size_t)(all * MAX_SPLITS < MAX_PARTIALS ? all * MAX_SPLITS : MAX_PARTIALS);
+  return 2 * all > MAX_PARTIALS ? 0 : (size_t)(all * MAX_SHARES < MAX_PARTIALS ? all * MAX_SHARES : MAX_PARTIALS);
 }
 
-Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, int n_seqs, int n_q, int n_kv, int hd, int dtype) {
-  Kv8AttnPlan p;
-  int longest = 0, rows_max = 0;
+// Keys are shared between workgroups where there are too few of them, in shares that make about one workgroup a compute unit (two on one
+// pull no faster than one), of 8 blocks (two a wavefront) to 64; longer ones leave the chip waiting for its last workgroups.  A share
+// takes a second launch to join them (3 to 4 us), which a workgroup's last 18 blocks take too: below that they stay together.
+// Shares of 8 / 16 / 32 / 64 blocks / not shared, us: 8 rows x 32 heads of 392 keys 9.1 / 7.4 / - / - / 7.4; of 1536 9.2 / 10.3 / 12.8 / - / 12.8;
+// of 4096 13.6 / 12.2 / 15.1 / 21.4 / 29.6; 48 rows x 28 of 4 heads of 4144 23.2 / 18.8 / 16.6 / 21.6 / 28.8; one row of 16384 13.0 / 11.9 / 13.7 / 18.5 /
+// 100; 24 rows of up to 8192 41 / 33.4 / 36.6 / 33.5 / 65; 2 x 37 fp32 rows x 32 heads of 1537 29.0 / 24.6 / 22.7 / 25.4 / 25.4.
+Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, int n_seqs, int n_q, int n_kv) {
+  const int group = n_q / n_kv;
+  int64_t work = 0;  // blocks of all workgroups
+  int blocks = 1;    // ... of the longest
   for (int b = 0; b < n_seqs; ++b) {
-    const int nr = row_off[b + 1] - row_off[b];
-    if (nr > rows_max) rows_max = nr;
-    if (nr && n_keys[b] > longest) longest = n_keys[b];
+    const int64_t tiles = tiles_of(row_off[b + 1] - row_off[b], group);
+    work += tiles * n_kv * blocks_of(n_keys[b]);
+    if (tiles && blocks_of(n_keys[b]) > blocks) blocks = blocks_of(n_keys[b]);
   }
-  const int64_t queries = (int64_t)rows_max * (n_q / n_kv);
-  p.queries = queries <= 32 ? 32 : 128;
-  int64_t wgs = 0;
-  for (int b = 0; b < n_seqs; ++b) wgs += ((int64_t)(row_off[b + 1] - row_off[b]) * (n_q / n_kv) + p.queries - 1) / p.queries * n_kv;
-  const int blocks = (longest + 31) / 32;
+  const int64_t all = (int64_t)row_off[n_seqs] * n_q, most = all ? MAX_PARTIALS / all < MAX_SHARES ? MAX_PARTIALS / all : MAX_SHARES : 1;
+  Kv8AttnPlan p;
+  p.chunk = blocks;
   p.splits = 1;
-  p.chunk = blocks ? blocks : 1;
-  const int64_t all = (int64_t)row_off[n_seqs] * n_q;
-  if (wgs > 0 && wgs < 256) {
-    int64_t s = 512 / wgs, most = MAX_PARTIALS / all;
-    if (s > most) s = most;
-    if (s > MAX_SPLITS) s = MAX_SPLITS;
-    if (s > 1) {
-      int chunk = (int)((blocks + s - 1) / s);
-      if (chunk < 8) chunk = 8;
-      chunk += chunk & 1;
-      if (chunk < blocks) { p.chunk = chunk; p.splits = (blocks + chunk - 1) / chunk; }
+  if (most >= 2) {
+    int64_t chunk = work / CUS + 1;
+    chunk = chunk < 8 ? 8 : chunk > 64 ? 64 : chunk;
+    if (chunk * most < blocks) chunk = (blocks + most - 1) / most;
+    if (chunk + 18 < blocks) {
+      p.chunk = (int)chunk;
+      p.splits = (int)((blocks + chunk - 1) / chunk);
     }
   }
   p.items = 0;
+  for (int b = 0; b < n_seqs; ++b) {
+    const int shares = (blocks_of(n_keys[b]) + p.chunk - 1) / p.chunk;
+    p.item_off[b] = p.items;
+    p.items += tiles_of(row_off[b + 1] - row_off[b], group) * (shares > 1 ? shares : 1);
+  }
+  p.item_off[n_seqs] = p.items;
   return p;
 }
 
@@ -500,8 +433,8 @@ namespace {
 template <typename T, int HD, int FMT>
 void launch_shape(const Kv8View& c, const Kv8AttnArgs& a, const Kv8AttnMeta& m, const Kv8AttnPlan& p, hipStream_t st) {
   const int grid = (int)(p.items * c.n_kv), sp = p.splits > 1;
-  if (p.queries == 32) kv8_attention_few_kernel<T, HD, FMT, 4><<<grid, 256, 0, st>>>(a, c, m, sp);
-  else kv8_attention_many_kernel<T, HD, FMT><<<grid, 256, 0, st>>>(a, c, m, sp);
+  kv8_attention_kernel<T, HD, FMT><<<grid, NWV * 64, 0, st>>>(c.data, (int)(c.head_bytes / kv8_block_bytes(HD)), c.n_kv, (const T*)a.q, a.q_stride, a.n_q, a.rows, m.chunk,
+                                                                  m.n_keys[0], m.n_seqs == 1 ? m.slot[0] : -1, sp, a, m);
   if (sp) kv8_attention_join_kernel<T, HD><<<(int)(((int64_t)a.rows * a.n_q + 3) / 4), 256, 0, st>>>(a, m);
 }
 template <typename T, int HD>
