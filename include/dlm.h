@@ -289,8 +289,9 @@ int dlm_kv8_read(const dlm_kv8_cache* c, void* k, void* v, int64_t row_stride, i
  * drafted tokens sets its ancestors' bits and its own, a causal span the bits up to its own.  A row that sees nothing (or n_keys 0)
  * gives zeros; NaN or infinite keys and values that a row does not see do not touch it, those that it sees make it NaN.  Slots may repeat.
  * q is read as it is (fp32: products to 22 bits of it); out must not overlap q.
- * workspace: DEVICE scratch of dlm_kv8_attention_workspace(rows, n_q, head_dim) bytes (16-byte aligned; NULL where that is 0),
- * used until the call's work is done: calls that may overlap need one each.
+ * workspace: DEVICE scratch at a multiple of 16, for calls that share a sequence's keys between workgroups; nothing needs more than
+ * dlm_kv8_attention_workspace(rows, n_q, head_dim) bytes, and many calls need none (then it may be NULL).  It is in use until the
+ * call's work is done: calls that may overlap need one each.
  * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, bad dtype or format, offsets, slot, n_keys < 0 or, with a mask, < nr),
  * DLM_ESHAPE (cache shape, n_q), DLM_ECAPACITY (n_seqs > 32, n_keys > max_len, mask_words or workspace too small, too many rows for
  * one launch), DLM_EHIP. */

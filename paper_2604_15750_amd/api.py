@@ -401,6 +401,29 @@ def dlm_attention(q, k, v):
 KV8_FORMATS = ("e4m3", "i8")
 
 
+# Calls that need no refusal go through an extension (csrc/kv8_py.c); what it declines (None) comes the way below it, which says what it refuses.
+@functools.lru_cache(maxsize=None)
+def _kv8_calls():
+    """The extension, bound to the library; None where it has not been built."""
+    try:
+        from . import _kv8 as m
+    except ImportError:
+        return None
+    L = lib()
+    m.bind(*(C.cast(f, C.c_void_p).value for f in (L.dlm_kv8_write, L.dlm_kv8_read, L.dlm_kv8_attention, L.dlm_qk_norm_rope)), torch.float32,
+           torch.bfloat16, torch.int32)
+    return m
+
+
+def _taken(rc):
+    """Whether the extension made the call; its error raised."""
+    if rc is None:
+        return False
+    if rc < 0:
+        _check(rc)
+    return True
+
+
 def _int32s(name, v, n):
     """A host list as the bytes of 32-bit integers, at least n of them; what is none is refused."""
     if v is None:
@@ -417,10 +440,14 @@ def _int32s(name, v, n):
     return _int_packer(len(v))(*whole)
 
 
+def _device():
+    return torch.cuda.current_device()
+
+
 def _gpu_of(name, t):
     """The index of the current GPU, which t is on."""
     dev = t.get_device()  # (-1: on none)
-    if dev < 0 or dev != torch.cuda.current_device():
+    if dev < 0 or dev != _device():
         raise ValueError(f"{name}: not on the current GPU")
     return dev
 
@@ -491,6 +518,9 @@ def _kv8_spans(cache, k, v, row_offsets, start, slot):
 
 def dlm_kv8_write(cache, k, v, row_offsets, start, slot=None):
     """k, v: device tensors [rows, n_kv, head_dim] (rows may be strided: columns of a wider matrix); the rest: host int lists."""
+    ext = _kv8_calls()
+    if ext is not None and _taken(ext.span(0, cache._ref, cache.data, k, v, row_offsets, start, slot, _device(), _stream())):
+        return
     args = _kv8_spans(cache, k, v, row_offsets, start, slot)
     if k.shape[0]:  # (a tensor without rows has no address)
         _check(lib().dlm_kv8_write(*args))
@@ -503,6 +533,9 @@ def dlm_kv8_read(cache, row_offsets, start, slot=None, k=None, v=None, dtype=tor
     if k is None:
         rows = int(row_offsets[len(start)])
         k, v = (torch.empty((rows, cache.n_kv, cache.head_dim), dtype=dtype, device=cache.data.device) for _ in "kv")
+    ext = _kv8_calls()
+    if ext is not None and _taken(ext.span(1, cache._ref, cache.data, k, v, row_offsets, start, slot, _device(), _stream())):
+        return k, v
     args = _kv8_spans(cache, k, v, row_offsets, start, slot)
     if k.shape[0]:
         _check(lib().dlm_kv8_read(*args))
@@ -513,6 +546,11 @@ def dlm_kv8_attention(cache, q, row_offsets, n_keys, slot=None, mask=None, out=N
     """q: device tensor [rows, n_q, head_dim] (rows may be strided); mask: device int32 [rows, words], bits as in include/dlm.h; out:
     contiguous, of q's shape and dtype (None: a new one); workspace: a contiguous device tensor of at least
     dlm_kv8_attention_workspace bytes that nothing else uses meanwhile (None: a new one); the rest: host int lists.  Returns out."""
+    ext = _kv8_calls()
+    if ext is not None and out is not None:
+        size = 0 if workspace is None or not workspace.is_contiguous() else workspace.numel() * workspace.element_size()
+        if _taken(ext.attention(cache._ref, cache.data, q, row_offsets, n_keys, slot, mask, out, workspace, size, _device(), _stream())):
+            return out
     n, dev = len(n_keys), _gpu_of("q", q)
     stride = _row_stride("q", q, dev, (None, cache.head_dim), _FLOATS)
     rows, n_q, hd = q.shape
@@ -550,6 +588,9 @@ def dlm_qk_norm_rope(x, positions, n_q, n_kv, head_dim, q_gain=None, k_gain=None
     """x: device tensor [rows, columns] whose first (n_q + n_kv) * head_dim columns are the query and key heads (rows may be
     strided); positions: device int32 [rows]; gains: [head_dim] of x's dtype, or None; out: as x (x itself: in place; None: a new
     tensor of those columns alone).  Returns out."""
+    ext = _kv8_calls()
+    if ext is not None and out is not None and _taken(ext.rope(x, positions, n_q, n_kv, head_dim, q_gain, k_gain, eps, theta, out, _device(), _stream())):
+        return out
     width, dev, dtype = (n_q + n_kv) * head_dim, _gpu_of("x", x), x.dtype
     stride = _row_stride("x", x, dev, (None,), _FLOATS)
     rows, columns = x.shape

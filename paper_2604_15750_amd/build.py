@@ -1,4 +1,5 @@
-"""Compile csrc/*.hip into paper_2604_15750_amd/libdlm.so for gfx950 and csrc/decisions_py.c into _decisions (in-tree, no torch dependency)."""
+"""Compile csrc/*.hip into paper_2604_15750_amd/libdlm.so for gfx950, csrc/decisions_py.c into _decisions and csrc/kv8_py.c into _kv8 (in-tree,
+no torch dependency)."""
 import os
 import shutil
 import subprocess
@@ -11,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libdlm.so")
 # (tagged with the interpreter it was built for: it reads that one's objects, and another does not load it)
 OUT_PY = os.path.join(HERE, "_decisions" + sysconfig.get_config_var("EXT_SUFFIX"))
+OUT_KV8 = os.path.join(HERE, "_kv8" + sysconfig.get_config_var("EXT_SUFFIX"))
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # amdgpu-kernarg-preload-count: a kernel's first arguments (14 dwords at most, up to the first struct) arrive in scalar registers with the
 # launch instead of by a trip to memory, so its first loads go out at once (161 launches of an in-block pass of the 8B model: 2888 -> 2864 us;
@@ -41,7 +43,20 @@ def build(verbose=False):
     if r.returncode != 0:
         raise RuntimeError("link failed:\n" + r.stderr)
     build_extension()
+    build_kv8_extension()
     return OUT
+
+
+def _compile_extension(source, out, calls):
+    """None without gcc or Python's headers: `calls` then go through ctypes."""
+    gcc, include = shutil.which("gcc"), sysconfig.get_paths()["include"]
+    if gcc is None or not os.path.exists(os.path.join(include, "Python.h")):
+        print(f"no gcc or no Python.h: {calls} are called through ctypes", file=sys.stderr)
+        return None
+    r = subprocess.run([gcc, "-O2", "-shared", "-fPIC", "-I", include, "-o", out, os.path.join(CSRC, source)], capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"gcc failed on {source}:\n" + r.stderr)
+    return out
 
 
 def build_extension():
@@ -49,14 +64,14 @@ def build_extension():
     for old in (OUT_PY, os.path.join(os.path.dirname(OUT_PY), "_decisions.so")):  # (the latter: without a tag)
         if os.path.exists(old):
             os.remove(old)
-    gcc, include = shutil.which("gcc"), sysconfig.get_paths()["include"]
-    if gcc is None or not os.path.exists(os.path.join(include, "Python.h")):
-        print("no gcc or no Python.h: block_boundary and select_parallel are called through ctypes", file=sys.stderr)
-        return None
-    r = subprocess.run([gcc, "-O2", "-shared", "-fPIC", "-I", include, "-o", OUT_PY, os.path.join(CSRC, "decisions_py.c")], capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError("gcc failed on decisions_py.c:\n" + r.stderr)
-    return OUT_PY
+    return _compile_extension("decisions_py.c", OUT_PY, "block_boundary and select_parallel")
+
+
+def build_kv8_extension():
+    """The same for the 8-bit cache's operators."""
+    if os.path.exists(OUT_KV8):
+        os.remove(OUT_KV8)
+    return _compile_extension("kv8_py.c", OUT_KV8, "the 8-bit cache's operators")
 
 
 if __name__ == "__main__":

@@ -158,11 +158,11 @@ extern "C" int dlm_kv8_attention(const dlm_kv8_cache* c, const void* q, int64_t 
   }
   const int rows = row_offsets[n_seqs];
   REQUIRE(!overlap(q, span_bytes(rows, q_stride, width, dtype), out, rows * width * elem_bytes(dtype)), DLM_EINVAL, "dlm_kv8_attention: out overlaps q");
-  const size_t need = dlm_kv8_attention_workspace(rows, n_q, c->head_dim);
-  REQUIRE(workspace_bytes >= need && (workspace || !need), DLM_ECAPACITY, "dlm_kv8_attention: workspace of %zu bytes < %zu", workspace ? workspace_bytes : 0, need);
   if (rows == 0) return DLM_OK;
   const Kv8AttnPlan p = kv8_attention_plan(row_offsets, n_keys, n_seqs, n_q, c->n_kv);
   REQUIRE((int64_t)rows * (n_q / c->n_kv) <= INT32_MAX && p.items * c->n_kv < INT32_MAX, DLM_ECAPACITY, "dlm_kv8_attention: too many rows for one launch");
+  const size_t need = p.splits > 1 ? (size_t)p.splits * rows * n_q * (c->head_dim + 2) * 4 : 0;
+  REQUIRE(!need || (workspace && workspace_bytes >= need), DLM_ECAPACITY, "dlm_kv8_attention: workspace of %zu bytes < %zu", workspace ? workspace_bytes : 0, need);
   m.chunk = p.chunk;
   for (int b = 0; b <= n_seqs; ++b) m.item_off[b] = (int32_t)p.item_off[b];
   Kv8AttnArgs a{q, q_stride, out, mask, mask_words, n_q, rows, nullptr, nullptr};

@@ -489,7 +489,7 @@ def test_captured_and_on_another_stream(device, dtype):
 
 
 def test_empty_calls_and_refusals(device):
-    cache = api.Kv8Cache(2, 64, 2, 64, "e4m3")
+    cache, long = api.Kv8Cache(2, 64, 2, 64, "e4m3"), api.Kv8Cache(1, 2000, 2, 64, "e4m3")
     x = torch.randn(6, 2, 64, device=device).to(BF16)
     none = x[:0]
     api.dlm_kv8_write(cache, none, none, [0, 0], [3])
@@ -520,7 +520,7 @@ def test_empty_calls_and_refusals(device):
                  lambda: api.dlm_kv8_attention(cache, x, [0, 6], [65]),
                  lambda: api.dlm_kv8_attention(cache, x, [0, 6], [6], out=x),
                  lambda: api.dlm_kv8_attention(cache, x, [0, 6], [5], mask=torch.ones(6, 1, dtype=torch.int32, device=device)),
-                 lambda: api.dlm_kv8_attention(cache, x, [0, 6], [6], workspace=torch.empty(16, dtype=torch.uint8, device=device)),
+                 lambda: api.dlm_kv8_attention(long, x, [0, 6], [2000], workspace=torch.empty(16, dtype=torch.uint8, device=device)),
                  lambda: api.dlm_qk_norm_rope(x.flatten(1), pos, 1, 1, 64, eps=0.0)):
         with pytest.raises(api.DlmError):
             call()

@@ -76,7 +76,11 @@ def test_attention_refusals():
     assert call(keys=_ints(-1)) == EINVAL and call(keys=_ints(101)) == ECAPACITY
     assert call(mask=P, words=0) == EINVAL and call(mask=P, words=1, keys=_ints(2)) == EINVAL
     assert call(mask=P, words=1, off=_ints(0, 33), keys=_ints(50)) == ECAPACITY and "mask_words" in _err()
-    assert call(size=need - 1) == ECAPACITY and call(ws=None) == ECAPACITY and "workspace" in _err()
+    # keys that are shared between workgroups: a partial output, a maximum and a sum per share, row and head
+    long = dict(c=_cache(max_len=5000), off=_ints(0, 1), keys=_ints(5000))
+    assert call(ws=None, **long) == ECAPACITY and call(size=1000, **long) == ECAPACITY and "workspace" in _err()
+    least = int(_err().split("<")[1])
+    assert 1000 < least <= api.lib().dlm_kv8_attention_workspace(1, 4, 64) and least % (4 * 66 * 4) == 0 and call(size=least - 1, **long) == ECAPACITY
     assert call(off=_ints(0, 0), size=0, ws=None) == 0  # nothing to do
 
 
@@ -97,11 +101,11 @@ def test_norm_rope_refusals():
     assert call(rows=0, gq=None, gk=None) == 0
 
 
-def test_python_refusals_before_the_library():
+def test_python_refusals_before_the_library(monkeypatch):
     """What a C call cannot see: tensors elsewhere, of other types, shapes or orders, lists that are too short or no 32-bit integers."""
-    c = object.__new__(api.Kv8Cache)
-    c.slots, c.max_len, c.n_kv, c.head_dim = 2, 64, 2, 64
-    c.data = torch.zeros(16, dtype=torch.uint8)
+    c = api.Kv8Cache(2, 64, 2, 64, device="cpu")
+    monkeypatch.setattr(api, "_device", lambda: 0)
+    monkeypatch.setattr(api, "_stream", lambda: 0)
     x = torch.zeros(4, 2, 64, dtype=torch.bfloat16)
     for call in (lambda: api.dlm_kv8_write(c, x, x, [0, 4], [0]), lambda: api.dlm_kv8_read(c, [0, 4], [0], k=x, v=x),
                  lambda: api.dlm_kv8_attention(c, x, [0, 4], [4]), lambda: api.dlm_qk_norm_rope(x[:, 0], torch.zeros(4, dtype=torch.int32), 1, 0, 64)):
@@ -117,3 +121,145 @@ def test_python_refusals_before_the_library():
         api.Kv8Cache(1, 64, 2, 64, format="e5m2", device="cpu")
     with pytest.raises(api.DlmError, match="ESHAPE"):
         api.Kv8Cache(1, 64, 2, 65, device="cpu")
+
+
+# ---- the extension and the way through ctypes: the same C call, or the same refusal ----------------------------------------------------
+
+VP, I32, I64, F32 = C.c_void_p, C.c_int, C.c_int64, C.c_float
+SPAN = C.CFUNCTYPE(I32, VP, VP, VP, I64, I32, VP, VP, VP, I32, VP)
+ATTENTION = C.CFUNCTYPE(I32, VP, VP, I64, VP, I32, I32, VP, VP, VP, I32, VP, I32, VP, C.c_size_t, VP)
+ROPE = C.CFUNCTYPE(I32, VP, I64, I32, I32, I32, I32, I32, VP, VP, F32, F32, VP, VP, I64, VP)
+
+
+@pytest.fixture
+def both(monkeypatch):
+    """both(f): what f's call hands to the library through the extension and through ctypes, or the exceptions' types; both.taken: whether
+    the extension made the call itself.  CPU tensors stand for the GPU's (index -1); nothing is launched."""
+    ext = api._kv8_calls()
+    assert ext is not None, "the extension has not been built"
+    L, seen = api.lib(), []
+    ints = lambda p, n: None if not p else tuple((C.c_int32 * n).from_address(p))  # noqa: E731
+
+    class Both:
+        status = 0
+
+        def __call__(self, f):
+            out = []
+            for through in (True, False):
+                seen.clear()
+                self.taken = False
+                monkeypatch.setattr(api, "_kv8_calls", (lambda: Spy) if through else (lambda: None))
+                try:
+                    f()
+                    out.append(list(seen))
+                except Exception as e:  # noqa: BLE001
+                    out.append(type(e))
+                if through:
+                    taken = self.taken
+            self.taken = taken
+            return out
+
+    self = Both()
+
+    def span(which):
+        def call(c, k, v, stride, dt, off, start, slot, n, st):
+            seen.append((which, c, k, v, stride, dt, ints(off, n + 1), ints(start, n), ints(slot, n), n, st))
+            return self.status
+        return SPAN(call)
+
+    def attention(c, q, stride, out, dt, n_q, off, keys, slot, n, mask, words, ws, size, st):
+        seen.append((c, q, stride, out, dt, n_q, ints(off, n + 1), ints(keys, n), ints(slot, n), n, mask, words, bool(ws), size, st))
+        return self.status
+
+    def rope(*a):
+        seen.append(a)
+        return self.status
+
+    calls = [span(0), span(1), ATTENTION(attention), ROPE(rope)]
+
+    class Recorder:
+        dlm_kv8_write, dlm_kv8_read, dlm_kv8_attention, dlm_qk_norm_rope = calls
+        dlm_kv8_attention_workspace, dlm_last_error = staticmethod(lambda *a: 0), L.dlm_last_error
+
+    class Spy:
+        @staticmethod
+        def ask(f, args):
+            rc = f(*args)
+            self.taken = rc is not None
+            assert self.taken == (len(seen) == 1)
+            return rc
+
+        span, attention, rope = (staticmethod(lambda *a, f=f: Spy.ask(f, a)) for f in (ext.span, ext.attention, ext.rope))
+
+    types = (torch.float32, torch.bfloat16, torch.int32)
+    real = [C.cast(f, VP).value for f in (L.dlm_kv8_write, L.dlm_kv8_read, L.dlm_kv8_attention, L.dlm_qk_norm_rope)]
+    for name, value in (("lib", lambda: Recorder), ("_device", lambda: -1), ("_stream", lambda: 0x1230), ("_gpu_of", lambda name, t: -1)):
+        monkeypatch.setattr(api, name, value)
+    ext.bind(*(C.cast(f, VP).value for f in calls), *types)
+    yield self
+    ext.bind(*real, *types)
+
+
+BF = torch.bfloat16
+LISTS = [([0, 3, 5], [7, 2]), ((0, 3, 5), (7, 2)), ([0, 3, 5, 9], [7, 2]), (torch.tensor([0, 3, 5]), [7, 2]), ([0, 3, 5], [7.0, 2]), ([0, 3], [7, 2]),
+         ([0, 3, 7], [7, 2]), ([0, 3, 5], [2**31, 2]), ([0, 3, 5], ["7", 2]), ([0] * 41, [0] * 40)]
+
+
+@pytest.fixture(scope="module")
+def cpu_cache():
+    return api.Kv8Cache(50, 64, 2, 64, device="cpu")
+
+
+@pytest.mark.parametrize("write", [True, False])
+@pytest.mark.parametrize("off,start", LISTS)
+def test_span_calls_either_way(both, cpu_cache, write, off, start):
+    wide = torch.zeros(6, 400, dtype=BF)
+    k, v = torch.zeros(6, 2, 64, dtype=BF), torch.ones(6, 2, 64, dtype=BF)
+    cut = lambda c: wide[:, c:c + 128].unflatten(1, (2, 64))  # noqa: E731
+    call = (lambda k, v, s: api.dlm_kv8_write(cpu_cache, k, v, off, start, s)) if write else (lambda k, v, s: api.dlm_kv8_read(cpu_cache, off, start, s, k=k, v=v))
+    plain = all(type(x) in (list, tuple) and all(type(i) is int and i < 2**31 for i in x) for x in (off, start)) and len(off) > len(start) <= 32
+    for slot in (None, [1, 0] * 20, torch.tensor([1, 0] * 20), [1]):
+        for pair, ok in (((k, v), True), ((cut(0), cut(128)), True), ((k, cut(0)), False), ((k.float(), v), False), ((k.float(), v.float()), True), ((k.half(), v.half()), False),
+                         ((k[:, :1], v[:, :1]), False), ((k[..., :32], v[..., :32]), False), ((k.transpose(1, 2).contiguous().transpose(1, 2), v), False),
+                         ((k[:5], v), False), ((k[:1], v[:1]), True)):
+            a, b = both(lambda: call(*pair, slot))
+            assert a == b
+            assert both.taken == (ok and plain and (slot is None or (type(slot) is list and len(slot) >= len(start))) and off[len(start)] <= len(pair[0]))
+            if ok and plain and slot is None and len(pair[0]) == 6:
+                assert (type(a) is list and len(a) == 1) == (off[len(start)] <= 6)
+    both.status = -2
+    assert both(lambda: api.dlm_kv8_write(cpu_cache, k, v, [0, 3], [0])) == [api.DlmError, api.DlmError] and both.taken
+
+
+@pytest.mark.parametrize("off,keys", LISTS)
+def test_attention_calls_either_way(both, cpu_cache, off, keys):
+    q, out, mask = torch.zeros(6, 4, 64), torch.zeros(6, 4, 64), torch.zeros(6, 2, dtype=torch.int32)
+    wide = torch.zeros(6, 300)[:, 4:260].unflatten(1, (4, 64))
+    plain = all(type(x) in (list, tuple) and all(type(i) is int and i < 2**31 for i in x) for x in (off, keys)) and len(off) > len(keys) <= 32 and off[len(keys)] <= 6
+    ws = torch.zeros(64, dtype=torch.uint8)
+    for kw, ok in ((dict(q=q), True), (dict(q=wide), True), (dict(q=q, mask=mask), True), (dict(q=q, workspace=ws), True), (dict(q=q.to(BF)), False),
+                   (dict(q=q.to(BF), out=out.to(BF)), True), (dict(q=q, out=wide), False), (dict(q=q, out=None), False), (dict(q=q, out=out[:5]), False),
+                   (dict(q=q, mask=mask.long()), False), (dict(q=q, mask=mask[:4]), False), (dict(q=q, mask=mask.t()), False), (dict(q=q[..., :32]), False),
+                   (dict(q=q[:, :, None]), False), (dict(q=q.to(torch.int32), out=out.to(torch.int32)), False)):
+        kw = dict(dict(row_offsets=off, n_keys=keys, out=out), **kw)
+        a, b = both(lambda: api.dlm_kv8_attention(cpu_cache, **kw))
+        if kw["out"] is None and type(a) is list:  # (a new one each time)
+            a, b = ([c[:3] + c[4:] for c in x] for x in (a, b))
+        assert a == b and both.taken == (ok and plain)
+    # a call that may need a workspace and has none is not the extension's
+    both.status = -3
+    seen = both(lambda: api.dlm_kv8_attention(cpu_cache, q, [0, 3], [5], out=out, workspace=ws))
+    assert seen == [api.DlmError, api.DlmError] and both.taken
+
+
+def test_norm_rope_calls_either_way(both):
+    x, pos, g = torch.zeros(6, 400), torch.zeros(6, dtype=torch.int32), torch.ones(64)
+    base = dict(x=x, positions=pos, n_q=2, n_kv=1, head_dim=64, q_gain=g, k_gain=g, eps=1e-5, theta=1e4, out=torch.zeros(6, 192))
+    for change, ok in (({}, True), (dict(out=x), True), (dict(out=torch.zeros(6, 500)[:, :200]), True), (dict(x=x[:, 8:]), True), (dict(q_gain=None, k_gain=None), True),
+                       (dict(out=torch.zeros(5, 192)), False), (dict(out=torch.zeros(6, 191)), False), (dict(out=torch.zeros(6, 192, dtype=BF)), False),
+                       (dict(x=x[:, :191]), False), (dict(x=x.t()), False), (dict(positions=pos.long()), False), (dict(positions=pos[:5]), False),
+                       (dict(positions=torch.zeros(12, dtype=torch.int32)[::2]), False), (dict(q_gain=torch.ones(32)), False), (dict(k_gain=g.to(BF)), False),
+                       (dict(q_gain=torch.ones(128)[::2]), False), (dict(eps=1), False), (dict(theta=500000.0), True), (dict(x=x.half()), False)):
+        a, b = both(lambda: api.dlm_qk_norm_rope(**dict(base, **change)))
+        assert a == b and both.taken == ok, change
+        assert (type(a) is list and len(a) == 1) == (ok or change == dict(eps=1)), change
