@@ -264,7 +264,7 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 
     int split_out, Kv8AttnArgs a, Kv8AttnMeta meta) {
   constexpr int PIECES = HD / 32;
   __shared__ AttnLds<HD> L;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = lane >> 5, c = lane & 31;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, c = lane & 31;
   // (the heads of an item are neighbours: where their number is a multiple of 8 all items of a head are on one XCD, and its L2 has the head's K and V)
   Work w;
   w.head = blockIdx.x % n_kv;
@@ -287,25 +287,28 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 
   w.blk0 = w.split * chunk;
   w.blk1 = min((w.n_keys + 31) >> 5, w.blk0 + chunk);
   w.region = data + ((int64_t)slot * n_kv + w.head) * head_blocks * kv8_block_bytes(HD);
-  // the next block is in flight while this one is worked on
+  // The next block is in flight while this one is worked on.  Its loads are made in any case, past the last block a line each that nothing
+  // uses: a path around them would be one that the compiler's count of them cannot follow, and each use would wait for all of them.
   u32x4 kr[PIECES], vr[PIECES];
-  unsigned kb = 0, vb = 0;  // scale bytes of position c
+  unsigned kb, vb;  // scale bytes of position c
   auto load_k = [&](int blk) __attribute__((always_inline)) {
-    const unsigned char* p = w.region + (int64_t)blk * kv8_block_bytes(HD);
+    const bool there = blk < w.blk1;
+    const unsigned char* p = w.region + (int64_t)(there ? blk : 0) * kv8_block_bytes(HD);
+    const int at = there ? lane : 0;
     kb = p[64 * HD + c];
     vb = p[64 * HD + 32 + c];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) kr[i] = ((const u32x4*)p)[i * 64 + lane];
+    for (int i = 0; i < PIECES; ++i) kr[i] = ((const u32x4*)p)[i * 64 + at];
   };
   auto load_v = [&](int blk) __attribute__((always_inline)) {
-    const u32x4* p = (const u32x4*)(w.region + (int64_t)blk * kv8_block_bytes(HD));
+    const bool there = blk < w.blk1;
+    const u32x4* p = (const u32x4*)(w.region + (int64_t)(there ? blk : 0) * kv8_block_bytes(HD));
+    const int at = there ? lane : 0;
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) vr[i] = p[(PIECES + i) * 64 + lane];
+    for (int i = 0; i < PIECES; ++i) vr[i] = p[(PIECES + i) * 64 + at];
   };
-  if (w.blk0 + wave < w.blk1) {
-    load_k(w.blk0 + wave);
-    load_v(w.blk0 + wave);
-  }
+  load_k(w.blk0 + wave);
+  load_v(w.blk0 + wave);
   w.first = a.mask ? w.n_keys - nr : w.n_keys;
   Tile<T, HD, FMT> t;
   t.start(q, q_stride, a, w, lane);
@@ -315,9 +318,8 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 
     else L.inv[wave][c] = undo_of(vb);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const bool more = blk + NWV < w.blk1;
     t.block(a, w, blk, h, k_now, nan_keys, L.b[wave], L.inv[wave], [&](int i) { return kr[i]; }, [&](int i) { return vr[i]; },
-            [&] { if (more) load_k(blk + NWV); }, [&] { if (more) load_v(blk + NWV); });
+            [&] { load_k(blk + NWV); }, [&] { load_v(blk + NWV); });
     __builtin_amdgcn_wave_barrier();
   }
   // each wavefront brings its own part to the common maximum
@@ -391,12 +393,13 @@ size_t kv8_attention_partials(int64_t rows, int n_q) {
   return 2 * all > MAX_PARTIALS ? 0 : (size_t)(all * MAX_SHARES < MAX_PARTIALS ? all * MAX_SHARES : MAX_PARTIALS);
 }
 
-// Keys are shared between workgroups where there are too few of them, in shares that make about one workgroup a compute unit (two on one
-// pull no faster than one), of 8 blocks (two a wavefront) to 64; longer ones leave the chip waiting for its last workgroups.  A share
-// takes a second launch to join them (3 to 4 us), which a workgroup's last 18 blocks take too: below that they stay together.
-// Shares of 8 / 16 / 32 / 64 blocks / not shared, us: 8 rows x 32 heads of 392 keys 9.1 / 7.4 / - / - / 7.4; of 1536 9.2 / 10.3 / 12.8 / - / 12.8;
-// of 4096 13.6 / 12.2 / 15.1 / 21.4 / 29.6; 48 rows x 28 of 4 heads of 4144 23.2 / 18.8 / 16.6 / 21.6 / 28.8; one row of 16384 13.0 / 11.9 / 13.7 / 18.5 /
-// 100; 24 rows of up to 8192 41 / 33.4 / 36.6 / 33.5 / 65; 2 x 37 fp32 rows x 32 heads of 1537 29.0 / 24.6 / 22.7 / 25.4 / 25.4.
+// Keys are shared between workgroups where there are too few of them: in the shortest shares (8 blocks or more, two a wavefront) that make at
+// most one workgroup a compute unit, or two if those of one would be longer than 40 blocks, or else in shares of 24, which leave the
+// chip's last round short.  A share takes a second launch to join them (3 to 4 us), as long as a workgroup's last 18 blocks: below that
+// they stay together.  us a call, shares of 8 / 16 / 24 / 40 / 64 blocks / not shared, K and V from HBM: 8 rows x 32 heads of 4096 keys (8 and 16:
+// 544 and 288 workgroups) 13.6 / 12.7 / 13.0 / 15.4 / 19.1 / 30; 48 rows x 28 of 4 heads of 4144 22.9 / 18.1 / 16.1 / 17.5 / 21.2 / 29; 4 rows 11.5 at 16, 12.2 at 24,
+// 28 not; 4 x 8 rows x 32 heads of up to 4096 34.1 / 28.3 / 28.2 / 29.8 / 33.6; 24 rows x 28 of 4 heads of up to 8192 46.9 / 40.3 / 38.8 / 35.2 / 44.7; 16 x 8
+// rows x 32 heads of up to 4096 107 / 91.0 / 85.9 / 85.5 / 94.5.
 Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, int n_seqs, int n_q, int n_kv) {
   const int group = n_q / n_kv;
   int64_t work = 0;  // blocks of all workgroups
@@ -411,8 +414,23 @@ Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, in
   p.chunk = blocks;
   p.splits = 1;
   if (most >= 2) {
-    int64_t chunk = work / CUS + 1;
-    chunk = chunk < 8 ? 8 : chunk > 64 ? 64 : chunk;
+    // the least chunk with which the workgroups are no more than `rounds` a compute unit, from `least` to `last`; 0 if there is none
+    auto fit = [&](int rounds, int64_t least, int64_t last) -> int64_t {
+      int64_t chunk = (work + rounds * CUS - 1) / (rounds * CUS);
+      if (chunk < least) chunk = least;
+      for (; chunk <= last; ++chunk) {
+        int64_t wgs = 0;
+        for (int b = 0; b < n_seqs; ++b) {
+          const int64_t shares = (blocks_of(n_keys[b]) + chunk - 1) / chunk;
+          wgs += tiles_of(row_off[b + 1] - row_off[b], group) * n_kv * (shares > 1 ? shares : 1);
+        }
+        if (wgs <= rounds * CUS) return chunk;
+      }
+      return 0;
+    };
+    int64_t chunk = fit(1, 8, 40);
+    if (!chunk) chunk = fit(2, 24, 44);
+    if (!chunk) chunk = 24;
     if (chunk * most < blocks) chunk = (blocks + most - 1) / most;
     if (chunk + 18 < blocks) {
       p.chunk = (int)chunk;
