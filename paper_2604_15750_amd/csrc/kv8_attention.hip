@@ -15,8 +15,8 @@
 //   b  is the addend of the multiply-add that applies the softmax's scale, and the sum's addition becomes a multiply-add.  p' stays
 //      bounded whatever the scales; b in [-60, 60] keeps every p' that weighs in l within 32 bits.
 // The softmax's instructions weigh as much as the products (16 scores a lane against 512 cycles of them for 32 x 32 scores), so each
-// score costs a multiply-add, half a maximum, an exponential, a multiply-add and half a conversion: the products start from -m, and m
-// moves only where a score would leave half's range: the largest p' is brought to 2^8 (fp32: 2^13) and may grow to 2^15 before that.
+// score costs a multiply-add, half a maximum, an exponential, a multiply-add and half a conversion: the products start from -m (bf16), and m
+// moves only where a score would leave half's range: the largest p' is brought to about 2^8 (fp32: 2^13) and may grow to 2^15 before that.
 #include <type_traits>
 
 #include "kv8.h"
@@ -85,7 +85,7 @@ struct Tile {
   static constexpr int PIECES = HD / 32, KF = HD / 16, TERMS = F32 ? 2 : 1;
   f16x8 qf[TERMS][KF];
   f32x16 o[PIECES], from_m;        // from_m: -m / cq in every element, what the products start from
-  float qs, cq, m, l, limit;       // limit: minus infinity until the query has seen a key
+  float qs, cq, rest, m, l, limit; // rest: what cq leaves of the scale (fp32); m: a whole number; limit: minus infinity until the query has seen a key
   int ref;                         // biased exponent that K's scales are relative to
   const uint32_t* words;           // of the query's row in the mask
 
@@ -103,7 +103,7 @@ struct Tile {
       for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[f][i]) & 0x7FFFFFFFu);
     const int e = min(max((int)(__float_as_uint(halves_max(__uint_as_float(top & 0x7F800000u))) >> 23) - 127, -100), 127);
     const float up = __uint_as_float((unsigned)(127 + 14 - e) << 23);
-    qs = __uint_as_float((unsigned)(127 - 14 + e) << 23) * (float)(1.44269504088896340736 / (HD == 128 ? 11.3137084989847603904 : HD == 64 ? 8.0 : 5.65685424949238019521));
+    qs = __uint_as_float((unsigned)(127 - 14 + e) << 23);
 #pragma unroll
     for (int f = 0; f < KF; ++f)
 #pragma unroll
@@ -113,7 +113,7 @@ struct Tile {
         qf[0][f][i] = hi;
         if (F32) qf[TERMS - 1][f][i] = (f16_t)(y - (float)hi);
       }
-    m = l = cq = 0.f;
+    m = l = cq = rest = 0.f;
     limit = -__builtin_inff();
     ref = -1000;
 #pragma unroll
@@ -152,13 +152,18 @@ struct Tile {
       t = row_butterfly(t, [](unsigned p, unsigned q) { return p > q ? p : q; });
       const auto r = __builtin_amdgcn_permlane16_swap(t, t, false, false);
       ref = __builtin_amdgcn_readfirstlane(r[0] > r[1] ? r[0] : r[1]);
-      cq = fmaxf(qs * __uint_as_float((unsigned)ref << 23), 7.8886090522101181e-31f);  // (2^-100: scores that far below 1 are zero beside anything)
+      constexpr double SCALE = 1.44269504088896340736 / (HD == 128 ? 11.3137084989847603904 : HD == 64 ? 8.0 : 5.65685424949238019521);
+      const float unit = fmaxf(qs * __uint_as_float((unsigned)ref << 23), 7.8886090522101181e-31f);  // (2^-100: scores that far below 1 are zero beside anything)
+      cq = unit * (float)SCALE;
+      rest = unit * (float)(SCALE - (double)(float)SCALE);
       start_from_m();
     }
     const float k_scale = __uint_as_float((unsigned)max((int)kb - ref + 127, 0) << 23);
     const f16x2 k_mul = {(f16_t)k_scale, (f16_t)k_scale}, k_add = k_mul * f16x2{(f16_t)-1152.f, (f16_t)-1152.f};
     const f16x2 v_mul = {(f16_t)1.f, (f16_t)1.f}, v_add = {(f16_t)-1152.f, (f16_t)-1152.f};
-    f32x16 s = from_m;
+    f32x16 s;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[i] = F32 ? 0.f : from_m[i];
 #pragma unroll
     for (int f = 0; f < KF; ++f) {
       const u32x4 raw = k(f >> 1);
@@ -172,7 +177,11 @@ struct Tile {
     for (int j = 0; j < 4; ++j) {
       const f32x4 t = *(const f32x4*)&vb[8 * j + 4 * h];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p[4 * j + i] = __builtin_fmaf(s[4 * j + i], cq, t[i]);
+      for (int i = 0; i < 4; ++i) {
+        // fp32: products that start from zero, and no rounding but at the size of the difference (b and m are whole numbers)
+        p[4 * j + i] = __builtin_fmaf(s[4 * j + i], cq, F32 ? t[i] - m : t[i]);
+        if (F32) p[4 * j + i] = __builtin_fmaf(s[4 * j + i], rest, p[4 * j + i]);
+      }
     }
     if (nan_keys) {
       asm volatile("; keys marked NaN");  // (keeps the branch: the compiler would make 48 instructions of every block out of it)
@@ -192,7 +201,7 @@ struct Tile {
     if (__builtin_amdgcn_ballot_w64(mx > limit)) {  // some query's maximum moves
       mx = halves_max(mx);
       const bool up = mx > limit;
-      const float by = up ? mx - P_TOP : 0.f, corr = !up ? 1.f : limit > 0.f ? __builtin_amdgcn_exp2f(-by) : 0.f;
+      const float by = up ? floorf(mx) - P_TOP : 0.f, corr = !up ? 1.f : limit > 0.f ? __builtin_amdgcn_exp2f(-by) : 0.f;
       m += by;
       if (up) limit = P_LIMIT;
       l *= corr;
