@@ -160,7 +160,7 @@ extern "C" int dlm_kv8_attention(const dlm_kv8_cache* c, const void* q, int64_t 
   REQUIRE(!overlap(q, span_bytes(rows, q_stride, width, dtype), out, rows * width * elem_bytes(dtype)), DLM_EINVAL, "dlm_kv8_attention: out overlaps q");
   if (rows == 0) return DLM_OK;
   const Kv8AttnPlan p = kv8_attention_plan(row_offsets, n_keys, n_seqs, n_q, c->n_kv);
-  REQUIRE((int64_t)rows * (n_q / c->n_kv) <= INT32_MAX && p.items * c->n_kv < INT32_MAX, DLM_ECAPACITY, "dlm_kv8_attention: too many rows for one launch");
+  REQUIRE((int64_t)rows * (n_q / c->n_kv) <= INT32_MAX && p.items / (n_seqs == 1 ? p.splits : 1) <= 65535, DLM_ECAPACITY, "dlm_kv8_attention: too many rows for one launch");
   const size_t need = p.splits > 1 ? (size_t)p.splits * rows * n_q * (c->head_dim + 2) * 4 : 0;
   REQUIRE(!need || (workspace && workspace_bytes >= need), DLM_ECAPACITY, "dlm_kv8_attention: workspace of %zu bytes < %zu", workspace ? workspace_bytes : 0, need);
   m.chunk = p.chunk;

@@ -75,6 +75,7 @@ __device__ inline float reciprocal(float l) { return l > 0.f ? 1.f / l : l == 0.
 struct Work {
   int head, row0, nq, group, q0, split, blk0, blk1, n_keys, first;  // first: positions from here on are visible to whom the mask says
   const unsigned char* region;
+  __device__ inline int row_of(int x) const { return group == 1 ? x : (int)((unsigned)x / (unsigned)group); }  // of query x
 };
 
 // 32 queries of a wavefront and their running softmax
@@ -90,7 +91,7 @@ struct Tile {
   const uint32_t* words;           // of the query's row in the mask
 
   __device__ inline void start(const T* q, int64_t q_stride, const Kv8AttnArgs& a, const Work& w, int lane) {
-    const int h = lane >> 5, x = w.q0 + (lane & 31), r = x < w.nq ? x / w.group : 0, hq = x < w.nq ? x - r * w.group : 0;
+    const int h = lane >> 5, x = w.q0 + (lane & 31), r = x < w.nq ? w.row_of(x) : 0, hq = x < w.nq ? x - r * w.group : 0;
     const T* from = q + (int64_t)(w.row0 + r) * q_stride + (w.head * w.group + hq) * HD + 16 * h;
     words = a.mask + (int64_t)(w.row0 + r) * a.mask_words;
     float v[KF][8];
@@ -136,7 +137,7 @@ struct Tile {
   }
 
   __device__ inline void start_from_m() {
-    const float t = -m / cq;
+    const float t = -m * __builtin_amdgcn_rcpf(cq);  // (a step of fp32 off: what the products start from is the same for all keys)
 #pragma unroll
     for (int i = 0; i < 16; ++i) from_m[i] = t;
   }
@@ -147,7 +148,7 @@ struct Tile {
   template <typename K, typename V, typename AK, typename AV>
   __device__ __attribute__((always_inline)) inline void block(const Kv8AttnArgs& a, const Work& w, int blk, int h, unsigned kb, unsigned nan_keys, const float* vb,
                                                               const float* inv, K k, V v, AK after_k, AV after_v) {
-    if (__builtin_amdgcn_ballot_w64((int)kb > ref + 5 && kb != KV8_NAN)) {  // (5: 1152 2^5 and 448 2^5 are below half's largest)
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)kb > ref + 5 && kb != KV8_NAN) != 0, 0)) {  // (5: 1152 2^5 and 448 2^5 are below half's largest)
       unsigned t = kb == KV8_NAN ? 1u : kb;
       t = row_butterfly(t, [](unsigned p, unsigned q) { return p > q ? p : q; });
       const auto r = __builtin_amdgcn_permlane16_swap(t, t, false, false);
@@ -183,13 +184,13 @@ struct Tile {
         if (F32) p[4 * j + i] = __builtin_fmaf(s[4 * j + i], rest, p[4 * j + i]);
       }
     }
-    if (nan_keys) {
+    if (__builtin_expect(nan_keys != 0, 0)) {
       asm volatile("; keys marked NaN");  // (keeps the branch: the compiler would make 48 instructions of every block out of it)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (nan_keys >> (8 * (i >> 2) + 4 * h + (i & 3)) & 1u) p[i] = __uint_as_float(0x7FC00000u);
     }
-    if (32 * blk + 32 > w.first) {  // (uniform)
+    if (__builtin_expect(32 * blk + 32 > w.first, 0)) {  // (uniform)
       const unsigned see = visible(a, w, blk, h);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
@@ -198,7 +199,7 @@ struct Tile {
     float mx = p[0];
 #pragma unroll
     for (int i = 1; i < 16; ++i) mx = fmaxf(mx, p[i]);
-    if (__builtin_amdgcn_ballot_w64(mx > limit)) {  // some query's maximum moves
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > limit) != 0, 0)) {  // some query's maximum moves
       mx = halves_max(mx);
       const bool up = mx > limit;
       const float by = up ? floorf(mx) - P_TOP : 0.f, corr = !up ? 1.f : limit > 0.f ? __builtin_amdgcn_exp2f(-by) : 0.f;
@@ -247,7 +248,7 @@ __device__ inline float undo_of(unsigned vb) { return vb == KV8_NAN ? 0.f : __ui
 // where a query's four dims from d on go: the output, or the workspace if the keys are split
 template <typename T, int HD>
 __device__ inline void put(const Kv8AttnArgs& a, const Work& w, int split_out, int x, int d, f32x4 v, float top, float sum_or_inv) {
-  const int r = x / w.group;
+  const int r = w.row_of(x);
   const int64_t at = (int64_t)(w.row0 + r) * a.n_q + w.head * w.group + (x - r * w.group);
   if (!split_out) {
     store4((T*)a.out + at * HD + d, v * sum_or_inv);
@@ -269,30 +270,31 @@ struct alignas(16) AttnLds {
 
 template <typename T, int HD, int FMT>
 __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 128 && sizeof(T) == 4 ? 1 : 2))) void kv8_attention_kernel(
-    const unsigned char* __restrict__ data, int head_blocks, int n_kv, const T* __restrict__ q, int64_t q_stride, int n_q, int rows, int chunk, int one_keys, int one_slot,
-    int split_out, Kv8AttnArgs a, Kv8AttnMeta meta) {
+    const unsigned char* __restrict__ data, int head_blocks, int n_kv, const T* __restrict__ q, int64_t q_stride, int group, int chunk, int one_rows, int one_keys,
+    int one_slot, int split_out, Kv8AttnArgs a, Kv8AttnMeta meta) {
   constexpr int PIECES = HD / 32;
   __shared__ AttnLds<HD> L;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, c = lane & 31;
-  // (the heads of an item are neighbours: where their number is a multiple of 8 all items of a head are on one XCD, and its L2 has the head's K and V)
+  // (the heads of a tile are neighbours: where their number is a multiple of 8 all tiles of a head are on one XCD, and its L2 has the head's K and V)
   Work w;
-  w.head = blockIdx.x % n_kv;
-  w.group = n_q / n_kv;
-  int item = blockIdx.x / n_kv, nr = rows, slot = one_slot;
+  w.head = blockIdx.x;
+  w.group = group;
   w.row0 = 0;
   w.n_keys = one_keys;
-  if (one_slot < 0) {  // (a single sequence's figures arrive in registers instead of by two trips to memory)
-    const int b = seq_of(meta.item_off, meta.n_seqs, item);
+  w.q0 = blockIdx.y * 32;
+  w.split = blockIdx.z;
+  int nr = one_rows, slot = one_slot;
+  if (one_slot < 0) {  // (a single sequence's figures arrive in registers instead of by two trips to memory, and it needs no division)
+    const int b = seq_of(meta.item_off, meta.n_seqs, blockIdx.y), item = blockIdx.y - meta.item_off[b];
     w.row0 = meta.row_off[b];
     nr = meta.row_off[b + 1] - w.row0;
     w.n_keys = meta.n_keys[b];
     slot = meta.slot[b];
-    item -= meta.item_off[b];
+    const int qtiles = (nr * group + 31) >> 5;
+    w.split = item / qtiles;
+    w.q0 = (item - w.split * qtiles) * 32;
   }
-  w.nq = nr * w.group;
-  const int qtiles = (w.nq + 31) >> 5;
-  w.split = item / qtiles;
-  w.q0 = (item - w.split * qtiles) * 32;
+  w.nq = nr * group;
   w.blk0 = w.split * chunk;
   w.blk1 = min((w.n_keys + 31) >> 5, w.blk0 + chunk);
   w.region = data + ((int64_t)slot * n_kv + w.head) * head_blocks * kv8_block_bytes(HD);
@@ -331,34 +333,30 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 
             [&] { load_k(blk + NWV); }, [&] { load_v(blk + NWV); });
     __builtin_amdgcn_wave_barrier();
   }
-  // each wavefront brings its own part to the common maximum
-  const float ls = halves_sum(t.l), mw = t.top();
-  if (h == 0) { L.m[wave][c] = mw; L.l[wave][c] = ls; }
-  __syncthreads();
-  float M = L.m[0][c];
+  // merge the wavefronts
+  const float ls = halves_sum(t.l);
+  if (w.q0 + c < w.nq) {
+    if (h == 0) { L.m[wave][c] = t.top(); L.l[wave][c] = ls; }
 #pragma unroll
-  for (int v = 1; v < NWV; ++v) M = fmaxf(M, L.m[v][c]);
-  const float f = __builtin_amdgcn_exp2f(mw - M);
+    for (int d = 0; d < PIECES; ++d)
 #pragma unroll
-  for (int d = 0; d < PIECES; ++d)
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      *(f32x4*)&L.o[wave][c][32 * d + 8 * j + 4 * h] = f32x4{t.o[d][4 * j] * f, t.o[d][4 * j + 1] * f, t.o[d][4 * j + 2] * f, t.o[d][4 * j + 3] * f};
-  if (wave == 0) {
-    float all = 0.f;
-#pragma unroll
-    for (int v = 0; v < NWV; ++v) all += __builtin_amdgcn_exp2f(L.m[v][c] - M) * L.l[v][c];
-    if (h == 0) L.inv[0][c] = split_out ? all : reciprocal(all);
-    else L.b[0][c] = M;
+      for (int j = 0; j < 4; ++j) *(f32x4*)&L.o[wave][c][32 * d + 8 * j + 4 * h] = f32x4{t.o[d][4 * j], t.o[d][4 * j + 1], t.o[d][4 * j + 2], t.o[d][4 * j + 3]};
   }
   __syncthreads();
   for (int i = tid; i < 32 * HD / 4; i += NWV * 64) {
     const int x = i / (HD / 4), d = i % (HD / 4) * 4;
     if (w.q0 + x >= w.nq) break;
-    f32x4 acc = *(const f32x4*)&L.o[0][x][d];
+    float M = L.m[0][x], sum = 0.f;
 #pragma unroll
-    for (int v = 1; v < NWV; ++v) acc += *(const f32x4*)&L.o[v][x][d];
-    put<T, HD>(a, w, split_out, w.q0 + x, d, acc, L.b[0][x], L.inv[0][x]);
+    for (int v = 1; v < NWV; ++v) M = fmaxf(M, L.m[v][x]);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < NWV; ++v) {
+      const float f = __builtin_amdgcn_exp2f(L.m[v][x] - M);
+      sum += f * L.l[v][x];
+      acc += *(const f32x4*)&L.o[v][x][d] * f;
+    }
+    put<T, HD>(a, w, split_out, w.q0 + x, d, acc, M, split_out ? sum : reciprocal(sum));
   }
 }
 
@@ -459,9 +457,9 @@ Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, in
 namespace {
 template <typename T, int HD, int FMT>
 void launch_shape(const Kv8View& c, const Kv8AttnArgs& a, const Kv8AttnMeta& m, const Kv8AttnPlan& p, hipStream_t st) {
-  const int grid = (int)(p.items * c.n_kv), sp = p.splits > 1;
-  kv8_attention_kernel<T, HD, FMT><<<grid, NWV * 64, 0, st>>>(c.data, (int)(c.head_bytes / kv8_block_bytes(HD)), c.n_kv, (const T*)a.q, a.q_stride, a.n_q, a.rows, m.chunk,
-                                                                  m.n_keys[0], m.n_seqs == 1 ? m.slot[0] : -1, sp, a, m);
+  const int sp = p.splits > 1, one = m.n_seqs == 1;
+  kv8_attention_kernel<T, HD, FMT><<<dim3(c.n_kv, (int)p.items / (one ? p.splits : 1), one ? p.splits : 1), NWV * 64, 0, st>>>(
+      c.data, (int)(c.head_bytes / kv8_block_bytes(HD)), c.n_kv, (const T*)a.q, a.q_stride, a.n_q / c.n_kv, m.chunk, a.rows, m.n_keys[0], one ? m.slot[0] : -1, sp, a, m);
   if (sp) kv8_attention_join_kernel<T, HD><<<(int)(((int64_t)a.rows * a.n_q + 3) / 4), 256, 0, st>>>(a, m);
 }
 template <typename T, int HD>
