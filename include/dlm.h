@@ -255,12 +255,13 @@ int dlm_attention(const void* q, const void* k, const void* v, void* out, int A,
  *   y = x * rsqrt(mean(x^2) + eps) * gain          (q_gain / k_gain DEVICE [head_dim] of dtype; NULL: y = x)
  *   out_i = y_i cos a - y_j sin a, out_j = y_j cos a + y_i sin a,   j = i + head_dim/2, a = position * theta^(-2 i / head_dim)
  * positions DEVICE [rows], any int32; the angle is computed in 64 bits, sums are fp32, values are rounded once.  out may be x (with
- * the same stride); else the two must not overlap.  Errors: DLM_EINVAL (null pointer, alignment, stride shorter than a row, overlap,
- * eps or theta not positive and finite, bad dtype), DLM_ESHAPE (rows < 0, heads, head_dim), DLM_EHIP. */
+ * the same stride); else the two must not overlap (columns of one matrix do not; with different strides, from the first row to the
+ * last).  Errors: DLM_EINVAL (null pointer, alignment, stride shorter than a row, overlap, eps or theta not positive and finite, bad
+ * dtype), DLM_ESHAPE (rows < 0, heads, head_dim), DLM_ECAPACITY (more than 67108860 rows), DLM_EHIP. */
 int dlm_qk_norm_rope(const void* x, int64_t x_stride, int rows, int n_q, int n_kv, int head_dim, int dtype, const void* q_gain,
                      const void* k_gain, float eps, float theta, const int32_t* positions, void* out, int64_t out_stride, void* stream);
 
-/* A cache of n_slots sequences of up to max_len positions, in caller-owned DEVICE memory of dlm_kv8_bytes(...) bytes (0: an
+/* A cache of n_slots sequences of up to max_len (at most 2^31 - 256) positions, in caller-owned DEVICE memory of dlm_kv8_bytes(...) bytes (0: an
  * unsupported shape) at a multiple of 16, zero-filled before its first use.  Each vector (K or V of one position and kv head) is held
  * as 8-bit codes and a scale 2^E: E is the smallest integer in [-60, 60] with max|x| <= M 2^E, a code is x 2^-E rounded to the
  * format (ties to even, saturated where E = 60 is not enough).  DLM_KV8_E4M3: 8-bit floating point with 3 fraction bits, M = 448;
@@ -274,9 +275,9 @@ size_t dlm_kv8_bytes(int n_slots, int max_len, int n_kv, int head_dim);
 
 /* Row r of sequence b (k and v: [rows, n_kv * head_dim] at row_stride) becomes position start[b] + r of its slot; a slot may be given
  * once.  dlm_kv8_read writes the values the positions stand for (exact in both dtypes) to k and v; slots may repeat, k and v must
- * not overlap.  Positions outside the spans, and rows behind the last sequence, are left as they are.
- * Errors: DLM_EINVAL (null pointer, alignment, stride, bad dtype or format, offsets, slot), DLM_ESHAPE (cache shape),
- * DLM_ECAPACITY (n_seqs > 32, a span beyond max_len), DLM_EHIP. */
+ * not overlap (columns of one matrix do not).  Positions outside the spans, and rows behind the last sequence, are left as they are.
+ * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap with each other or the cache, bad dtype or format, offsets, slot),
+ * DLM_ESHAPE (cache shape), DLM_ECAPACITY (n_seqs > 32, a span beyond max_len, 2^24 blocks of 32 positions of one head or more), DLM_EHIP. */
 int dlm_kv8_write(const dlm_kv8_cache* c, const void* k, const void* v, int64_t row_stride, int dtype, const int32_t* row_offsets,
                   const int32_t* start, const int32_t* slot, int n_seqs, void* stream);
 int dlm_kv8_read(const dlm_kv8_cache* c, void* k, void* v, int64_t row_stride, int dtype, const int32_t* row_offsets, const int32_t* start,
@@ -288,13 +289,14 @@ int dlm_kv8_read(const dlm_kv8_cache* c, void* k, void* v, int64_t row_stride, i
  * before them and position n_keys[b] - nr + j where bit j % 32 of word j / 32 of its mask is set (32 mask_words >= nr): a tree of
  * drafted tokens sets its ancestors' bits and its own, a causal span the bits up to its own.  A row that sees nothing (or n_keys 0)
  * gives zeros; NaN or infinite keys and values that a row does not see do not touch it, those that it sees make it NaN.  Slots may repeat.
- * q is read as it is (fp32: products to 22 bits of it); out must not overlap q.
+ * q is read as it is (fp32: products to 22 bits of it); out must not overlap
+ * what is read, nor the workspace anything else.
  * workspace: DEVICE scratch at a multiple of 16, for calls that share a sequence's keys between workgroups; nothing needs more than
  * dlm_kv8_attention_workspace(rows, n_q, head_dim) bytes, and many calls need none (then it may be NULL).  It is in use until the
  * call's work is done: calls that may overlap need one each.
  * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, bad dtype or format, offsets, slot, n_keys < 0 or, with a mask, < nr),
- * DLM_ESHAPE (cache shape, n_q), DLM_ECAPACITY (n_seqs > 32, n_keys > max_len, mask_words or workspace too small, too many rows for
- * one launch), DLM_EHIP. */
+ * DLM_ESHAPE (cache shape, n_q), DLM_ECAPACITY (n_seqs > 32, n_keys > max_len, mask_words or workspace too small, more than
+ * 65535 tiles of 32 queries of a kv head: rows * n_q / n_kv beyond 2 million), DLM_EHIP. */
 size_t dlm_kv8_attention_workspace(int rows, int n_q, int head_dim);
 int dlm_kv8_attention(const dlm_kv8_cache* c, const void* q, int64_t q_stride, void* out, int dtype, int n_q, const int32_t* row_offsets,
                       const int32_t* n_keys, const int32_t* slot, int n_seqs, const uint32_t* mask, int mask_words, void* workspace,

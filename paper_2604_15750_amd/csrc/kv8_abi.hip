@@ -11,14 +11,31 @@ bool known_head(int hd) { return hd == 32 || hd == 64 || hd == 128; }
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 // rows [rows, width] at `stride` elements: the stride holds a row and keeps 16-byte alignment
 bool good_stride(int64_t stride, int64_t width, int dtype) { return stride >= width && stride <= INT64_C(1) << 40 && stride * elem_bytes(dtype) % 16 == 0; }
-bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
-  return (uintptr_t)a < (uintptr_t)b + (uintptr_t)b_bytes && (uintptr_t)b < (uintptr_t)a + (uintptr_t)a_bytes;
+typedef __int128 wide;  // (rows x strides do not fit 64 bits)
+bool overlap(const void* a, wide a_bytes, const void* b, wide b_bytes) {
+  return a_bytes && b_bytes && (wide)(uintptr_t)a < (wide)(uintptr_t)b + b_bytes && (wide)(uintptr_t)b < (wide)(uintptr_t)a + a_bytes;
 }
-int64_t span_bytes(int64_t rows, int64_t stride, int64_t width, int dtype) { return rows ? ((rows - 1) * stride + width) * elem_bytes(dtype) : 0; }
+// [rows, width] at `stride`: what lies between its first and its last byte
+struct Rows {
+  const void* p;
+  int64_t rows, stride, width;  // bytes
+  Rows(const void* at, int64_t n, int64_t stride_elems, int64_t width_elems, int dtype)
+      : p(at), rows(n), stride(stride_elems * elem_bytes(dtype)), width(width_elems * elem_bytes(dtype)) {}
+  wide span() const { return rows ? (wide)(rows - 1) * stride + width : 0; }
+};
+// whether two such arrays share a byte: columns of one matrix need not; of different strides: whether their spans do
+bool overlap(const Rows& a, const Rows& b) {
+  if (a.stride != b.stride || a.rows != b.rows || a.width != b.width) return overlap(a.p, a.span(), b.p, b.span());
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p, d = x > y ? x - y : y - x;
+  const int64_t r = (int64_t)(d % (uintptr_t)a.stride);
+  const uintptr_t n = d / (uintptr_t)a.stride;
+  return (n < (uintptr_t)a.rows && r < a.width) || (n + 1 < (uintptr_t)a.rows && a.stride - r < a.width);
+}
+constexpr int MAX_GRID = (1 << 24) - 1;  // workgroups of 256 in a dimension of a launch
 
 // bytes of a (slot, kv head), 0 for an unsupported shape
 int64_t head_bytes(int n_slots, int max_len, int n_kv, int hd) {
-  if (n_slots < 1 || max_len < 1 || n_kv < 1 || n_kv > 65535 || !known_head(hd)) return 0;
+  if (n_slots < 1 || max_len < 1 || max_len > INT32_MAX - 255 || n_kv < 1 || n_kv > 65535 || !known_head(hd)) return 0;
   const int64_t per = ((int64_t)max_len + 31) / 32 * kv8_block_bytes(hd);
   return (INT64_C(1) << 46) / per < (int64_t)n_slots * n_kv ? 0 : per;
 }
@@ -34,7 +51,7 @@ int check_cache(const char* name, const dlm_kv8_cache* c, Kv8View* view) {
   return DLM_OK;
 }
 
-// the packing that all calls share; once: a slot may be given once
+// the packing that all calls share; once: a slot may be given once (a write)
 int check_seqs(const char* name, const dlm_kv8_cache* c, const int32_t* row_offsets, const int32_t* slot, int n_seqs, bool once, int32_t* row_off, int32_t* slots) {
   REQUIRE(n_seqs >= 1, DLM_EINVAL, "%s: n_seqs %d < 1", name, n_seqs);
   REQUIRE(n_seqs <= DLM_MAX_SEQS, DLM_ECAPACITY, "%s: n_seqs %d > %d", name, n_seqs, DLM_MAX_SEQS);
@@ -71,9 +88,13 @@ int check_spans(const char* name, const dlm_kv8_cache* c, const void* k, const v
     REQUIRE(start[b] + n <= c->max_len, DLM_ECAPACITY, "%s: span end %lld of sequence %d > max_len %d", name, (long long)(start[b] + n), b, c->max_len);
     m->start[b] = start[b];
     if (n) blocks += (start[b] + n - 1) / 32 - start[b] / 32 + 1;
-    REQUIRE(blocks * c->n_kv < INT32_MAX, DLM_ECAPACITY, "%s: too many rows for one launch", name);
+    REQUIRE(blocks * c->n_kv <= MAX_GRID, DLM_ECAPACITY, "%s: too many rows for one launch", name);
     m->block_off[b + 1] = (int32_t)blocks;
   }
+  const Rows kr(k, row_offsets[n_seqs], row_stride, (int64_t)c->n_kv * c->head_dim, dtype), vr(v, kr.rows, row_stride, (int64_t)c->n_kv * c->head_dim, dtype);
+  const wide cached = (wide)view->head_bytes * c->n_slots * c->n_kv;
+  REQUIRE(!overlap(k, kr.span(), c->data, cached) && !overlap(v, vr.span(), c->data, cached), DLM_EINVAL, "%s: rows overlap the cache", name);
+  REQUIRE(once || !overlap(kr, vr), DLM_EINVAL, "%s: k overlaps v", name);
   return DLM_OK;
 }
 
@@ -91,8 +112,9 @@ extern "C" int dlm_qk_norm_rope(const void* x, int64_t x_stride, int rows, int n
   REQUIRE(aligned16(x) && aligned16(out) && aligned16(q_gain) && aligned16(k_gain) && ((uintptr_t)positions & 3) == 0, DLM_EINVAL, "dlm_qk_norm_rope: unaligned pointer");
   REQUIRE(good_stride(x_stride, width, dtype) && good_stride(out_stride, width, dtype), DLM_EINVAL, "dlm_qk_norm_rope: strides %lld and %lld of rows of %lld",
           (long long)x_stride, (long long)out_stride, (long long)width);
-  REQUIRE((x == out && x_stride == out_stride) || !overlap(x, span_bytes(rows, x_stride, width, dtype), out, span_bytes(rows, out_stride, width, dtype)), DLM_EINVAL,
-          "dlm_qk_norm_rope: out overlaps x");
+  REQUIRE(rows <= 4 * MAX_GRID, DLM_ECAPACITY, "dlm_qk_norm_rope: too many rows for one launch");
+  const Rows from(x, rows, x_stride, width, dtype), to(out, rows, out_stride, width, dtype);
+  REQUIRE((x == out && x_stride == out_stride) || !overlap(from, to), DLM_EINVAL, "dlm_qk_norm_rope: out overlaps x");
   if (rows == 0) return DLM_OK;
   launch_qk_norm_rope(x, x_stride, rows, n_q, n_kv, head_dim, dtype, q_gain, k_gain, eps, theta, positions, out, out_stride, (hipStream_t)stream);
   DLM_HIP(hipGetLastError());
@@ -157,12 +179,18 @@ extern "C" int dlm_kv8_attention(const dlm_kv8_cache* c, const void* q, int64_t 
     m.n_keys[b] = n_keys[b];
   }
   const int rows = row_offsets[n_seqs];
-  REQUIRE(!overlap(q, span_bytes(rows, q_stride, width, dtype), out, rows * width * elem_bytes(dtype)), DLM_EINVAL, "dlm_kv8_attention: out overlaps q");
+  const Rows from(q, rows, q_stride, width, dtype), to(out, rows, width, width, dtype);
+  REQUIRE(!overlap(from, to), DLM_EINVAL, "dlm_kv8_attention: out overlaps q");
+  REQUIRE(!overlap(out, to.span(), c->data, (wide)view.head_bytes * c->n_slots * c->n_kv) && !(mask && overlap(out, to.span(), mask, (wide)rows * mask_words * 4)), DLM_EINVAL,
+          "dlm_kv8_attention: out overlaps the cache or the mask");
   if (rows == 0) return DLM_OK;
   const Kv8AttnPlan p = kv8_attention_plan(row_offsets, n_keys, n_seqs, n_q, c->n_kv);
   REQUIRE((int64_t)rows * (n_q / c->n_kv) <= INT32_MAX && p.items / (n_seqs == 1 ? p.splits : 1) <= 65535, DLM_ECAPACITY, "dlm_kv8_attention: too many rows for one launch");
   const size_t need = p.splits > 1 ? (size_t)p.splits * rows * n_q * (c->head_dim + 2) * 4 : 0;
   REQUIRE(!need || (workspace && workspace_bytes >= need), DLM_ECAPACITY, "dlm_kv8_attention: workspace of %zu bytes < %zu", workspace ? workspace_bytes : 0, need);
+  REQUIRE(!need || !(overlap(workspace, need, q, from.span()) || overlap(workspace, need, out, to.span()) || (mask && overlap(workspace, need, mask, (wide)rows * mask_words * 4)) ||
+                     overlap(workspace, need, c->data, (wide)view.head_bytes * c->n_slots * c->n_kv)),
+          DLM_EINVAL, "dlm_kv8_attention: the workspace overlaps an array of the call");
   m.chunk = p.chunk;
   for (int b = 0; b <= n_seqs; ++b) m.item_off[b] = (int32_t)p.item_off[b];
   Kv8AttnArgs a{q, q_stride, out, mask, mask_words, n_q, rows, nullptr, nullptr};

@@ -488,6 +488,25 @@ def test_captured_and_on_another_stream(device, dtype):
     assert torch.equal(a, eager[0]) and torch.equal(b, eager[1])
 
 
+def test_columns_of_one_matrix(device):
+    """q, k and v read into, and heads rotated into, other columns of the matrix they come from."""
+    g = _gen(21)
+    wide = torch.randn(9, 5 * 128, generator=g).to(BF16).to(device)
+    part = lambda i: wide[:, 128 * i:128 * (i + 1)]  # noqa: E731
+    pos = torch.arange(9, dtype=torch.int32, device=device)
+    want = api.dlm_qk_norm_rope(part(0).contiguous(), pos, 2, 0, 64)
+    before = wide.clone()
+    api.dlm_qk_norm_rope(part(0), pos, 2, 0, 64, out=part(1))
+    assert torch.equal(part(1), want)
+    cache = api.Kv8Cache(1, 9, 2, 64)
+    heads = lambda i: part(i).unflatten(1, (2, 64))  # noqa: E731
+    api.dlm_kv8_write(cache, heads(0), heads(1), [0, 9], [0])
+    api.dlm_kv8_read(cache, [0, 9], [0], k=heads(4), v=heads(3))
+    k, v = api.dlm_kv8_read(cache, [0, 9], [0])
+    assert torch.equal(heads(4), k) and torch.equal(heads(3), v)
+    assert torch.equal(part(0), before[:, :128]) and torch.equal(part(2), before[:, 256:384])
+
+
 def test_empty_calls_and_refusals(device):
     cache, long = api.Kv8Cache(2, 64, 2, 64, "e4m3"), api.Kv8Cache(1, 2000, 2, 64, "e4m3")
     x = torch.randn(6, 2, 64, device=device).to(BF16)

@@ -101,6 +101,60 @@ def test_norm_rope_refusals():
     assert call(rows=0, gq=None, gk=None) == 0
 
 
+def test_launches_that_would_be_too_large():
+    """A launch has fewer than 2^32 threads in a dimension, and its other dimensions at most 65535 workgroups."""
+    L = api.lib()
+    rows = 4 * ((1 << 24) - 1) + 1  # 4 rows a workgroup
+    assert L.dlm_qk_norm_rope(P, 64, rows, 1, 0, 32, 1, None, None, 1e-5, 1e4, P, 2 * P, 64, None) == ECAPACITY and "too many rows" in _err()
+    # blocks of 32 positions x heads
+    n = 1 << 29
+    big = _cache(slots=2, max_len=n, n_kv=1, hd=32)
+    for f in (L.dlm_kv8_write, L.dlm_kv8_read):
+        assert f(big, 2 * P, 3 * P, 32, 1, _ints(0, n), _ints(0), None, 1, None) == ECAPACITY and "too many rows" in _err()
+        assert f(big, 2 * P, 3 * P, 32, 1, _ints(0, n // 2, n), _ints(0, 1), None, 2, None) == ECAPACITY
+        assert f(big, 2 * P, 3 * P, 32, 1, _ints(0, n // 2, n // 2 + 1, 2**31 - 1), _ints(0, 1, 2), _ints(0, 1, 0), 3, None) == (EINVAL if f is L.dlm_kv8_write else ECAPACITY)
+    # tiles of 32 queries of a kv head, of one sequence and of several
+    rows = 32 * 65535 // 4 + 1
+    for off, keys in ((_ints(0, rows), _ints(5)), (_ints(0, 1, rows), _ints(5, 7)), (_ints(0, 2**31 - 1), _ints(5))):
+        assert L.dlm_kv8_attention(_cache(), 2 * P, 512, 9 * P, 1, 8, off, keys, None, len(keys), None, 0, None, 0, None) == ECAPACITY and "too many rows" in _err()
+    # positions that a block's end would take past 31 bits
+    assert L.dlm_kv8_bytes(1, 2**31 - 1, 1, 32) == 0 and L.dlm_kv8_bytes(1, 2**31 - 255, 1, 32) == 0 and L.dlm_kv8_bytes(1, 2**31 - 256, 1, 32) > 0
+
+
+def test_overlaps():
+    """Columns of one matrix share no byte; an output that shares one with what is read is refused.  (What is not refused ends at a row
+    count that is: nothing is launched.)"""
+    L, d = api.lib(), P  # the cache's memory
+    f = L.dlm_kv8_read
+    size = L.dlm_kv8_bytes(4, 100, 2, 64)
+
+    def read(k, v, stride, rows=3, write=False):
+        return (L.dlm_kv8_write if write else f)(_cache(), k, v, stride, 1, _ints(0, rows), _ints(0), None, 1, None)
+
+    for stride, apart in ((128, 0), (128, 16), (128, 256 * 3 - 16), (400, 0), (400, 240), (400, 800 - 240), (400, 1600), (400, 1600 + 240), (400, 1600 - 240)):
+        assert read(2 * P, 2 * P + apart, stride) == EINVAL and "overlaps v" in _err(), (stride, apart)
+        assert read(2 * P + apart, 2 * P, stride) == EINVAL, (stride, apart)
+    for k, v in ((d, 2 * P), (2 * P, d), (d + size - 16, 2 * P), (2 * P, d - 256), (d - 768 + 16, 2 * P)):
+        for write in (False, True):
+            assert read(k, v, 128, write=write) == EINVAL and "the cache" in _err(), (k - d, v - d)
+
+    def attention(q=2 * P, out=3 * P, mask=4 * P, ws=5 * P, stride=256, off=_ints(0, 1), c=_cache(max_len=5000)):
+        return L.dlm_kv8_attention(c, q, stride, out, 1, 4, off, _ints(5000), None, 1, mask, 4, ws, 1 << 30, None)
+
+    for kw in (dict(out=d), dict(out=d - 496), dict(out=4 * P), dict(out=4 * P - 496), dict(out=2 * P + 496), dict(out=2 * P, stride=512), dict(ws=2 * P), dict(ws=3 * P + 496),
+               dict(ws=4 * P), dict(ws=d), dict(q=d, ws=d)):
+        assert attention(**kw) == EINVAL and "overlaps" in _err(), kw
+    # rows and strides whose product passes 64 bits
+    assert attention(out=2 * P + (1 << 45), stride=1 << 40, off=_ints(0, 100)) == EINVAL and "out overlaps q" in _err()
+
+    def rope(x, out, xs, os, rows=3):
+        return L.dlm_qk_norm_rope(x, xs, rows, 2, 0, 64, 1, None, None, 1e-5, 1e4, 6 * P, out, os, None)
+
+    for x, out, xs, os in ((P, P + 16, 128, 128), (P, P + 240, 400, 400), (P, P + 800 - 240, 400, 400), (P, P + 256, 400, 408), (P, P, 400, 128), (P, P + 1600 + 240, 400, 400)):
+        assert rope(x, out, xs, os) == EINVAL and "out overlaps x" in _err(), (out - x, xs, os)
+        assert rope(out, x, os, xs) == EINVAL
+
+
 def test_python_refusals_before_the_library(monkeypatch):
     """What a C call cannot see: tensors elsewhere, of other types, shapes or orders, lists that are too short or no 32-bit integers."""
     c = api.Kv8Cache(2, 64, 2, 64, device="cpu")
