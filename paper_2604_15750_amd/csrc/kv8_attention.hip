@@ -13,7 +13,8 @@
 //   a  goes in where codes become half (the conversion scales; i8 takes it in the multiply-add that takes its offset off), relative to a
 //      wavefront's `ref`, which is raised where a block's keys would leave half's range; keys 2^-24 below it lose bits
 //   b  is the addend of the multiply-add that applies the softmax's scale, and the sum's addition becomes a multiply-add.  p' stays
-//      bounded whatever the scales; b in [-60, 60] keeps every p' that weighs in l within 32 bits.
+//      bounded whatever the scales.  b in [-60, 60] keeps l within 32 bits, and a value whose scale is 2^-B of the largest has its part
+//      in l down to a probability of 2^(B-134) of that one's (fp32 2^(B-139)): 2^-34 (2^-39) for values 2^100 apart.
 // The softmax's instructions weigh as much as the products (16 scores a lane against 512 cycles of them for 32 x 32 scores), so each
 // score costs a multiply-add, half a maximum, an exponential, a multiply-add and half a conversion: the products start from -m (bf16), and m
 // moves only where a score would leave half's range: the largest p' is brought to about 2^8 (fp32: 2^13) and may grow to 2^15 before that.
@@ -242,8 +243,11 @@ struct Tile {
   __device__ inline float top() const { return limit > 0.f ? m : NEG_BIG; }
 };
 
-__device__ inline float exponent_of(unsigned vb) { return (float)vb - 127.f; }
-__device__ inline float undo_of(unsigned vb) { return vb == KV8_NAN ? 0.f : __uint_as_float((254u - vb) << 23); }
+// V's scale byte as its exponent and what undoes it.  A position that was never written (0) counts at the least scale, as a vector of zeros that was
+// (its codes: 0 in e4m3, -128 in i8, 2^-53 there): at 2^-127 the sum's terms would pass 32 bits.
+__device__ inline unsigned v_scale(unsigned vb) { return max(vb, 127u - KV8_E_MAX); }
+__device__ inline float exponent_of(unsigned vb) { return (float)v_scale(vb) - 127.f; }
+__device__ inline float undo_of(unsigned vb) { return vb == KV8_NAN ? 0.f : __uint_as_float((254u - v_scale(vb)) << 23); }
 
 // where a query's four dims from d on go: the output, or the workspace if the keys are split
 template <typename T, int HD>

@@ -318,6 +318,29 @@ def test_scales_far_apart(device, fmt, dtype):
 
 @pytest.mark.parametrize("fmt", ["e4m3", "i8"])
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("big", [False, True])
+def test_attention_sees_positions_never_written(device, fmt, dtype, big):
+    """They are keys and values of zeros, whichever wavefront or share has them and whatever the scales of the others.  (i8: the code is
+    -128 at 2^-60, so up to 2^-53 for zero.)"""
+    g = _gen(31, big)
+    for keys, spans in ((64, [(0, 32)]), (290, [(3, 40), (200, 20)]), (3000, [(1500, 300)]), (40, [])):
+        k, v = torch.zeros(keys, 2, 64), torch.zeros(keys, 2, 64)
+        cache = api.Kv8Cache(1, keys, 2, 64, fmt)
+        for at, n in spans:
+            k[at:at + n] = torch.randn(n, 2, 64, generator=g)
+            v[at:at + n] = torch.randn(n, 2, 64, generator=g) * (2.0 ** 45 if big else 1.0)
+            api.dlm_kv8_write(cache, k[at:at + n].to(dtype).to(device), v[at:at + n].to(dtype).to(device), [0, n], [at])
+        K, V = (o_kv8.stored(_np64(x.to(dtype)), fmt) for x in (k, v))
+        q = torch.randn(5, 4, 64, generator=g).to(dtype)
+        see = np.ones((5, keys), dtype=bool)
+        want = o_kv8.attention(_np64(q), K, V, see)
+        bound = _bound(q, K, V, see, dtype) + HALF_STEP[dtype] * np.abs(want) + (2.0 ** -52 if fmt == "i8" else 0.0)
+        err = np.abs(_np64(api.dlm_kv8_attention(cache, q.to(device), [0, 5], [keys])) - want)
+        assert (err <= bound).all(), (keys, (err / np.maximum(bound, 1e-300)).max())
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "i8"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("keys", [70, 3000])
 def test_nan_and_infinity(device, fmt, dtype, keys):
     """In places that a row does not see they change nothing; what a row sees makes that row (and head) NaN, and no other."""
