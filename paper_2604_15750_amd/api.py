@@ -493,14 +493,19 @@ class Kv8Cache:
     format: "e4m3" or "i8"."""
 
     def __init__(self, slots, max_len, n_kv, head_dim, format="e4m3", device="cuda"):
-        n = lib().dlm_kv8_bytes(slots, max_len, n_kv, head_dim)
+        n = lib().dlm_kv8_bytes(slots, max_len, n_kv, head_dim) if max(slots, max_len, n_kv, head_dim) < 2**31 else 0
         if n == 0:
             raise DlmError(-2, f"a cache of {slots} slots x {max_len} positions x {n_kv} heads of {head_dim}")
         self.slots, self.max_len, self.n_kv, self.head_dim, self.format = slots, max_len, n_kv, head_dim, format
         code = KV8_FORMATS.index(format)
-        self.data = torch.zeros(n, dtype=torch.uint8, device=device)
-        self._desc = dlm_kv8_cache(slots, max_len, n_kv, head_dim, code, self.data.data_ptr())
+        self._data = torch.zeros(n, dtype=torch.uint8, device=device)
+        self._desc = dlm_kv8_cache(slots, max_len, n_kv, head_dim, code, self._data.data_ptr())
         self._ref = C.addressof(self._desc)
+
+    @property
+    def data(self):
+        """The memory (one address for life: to be filled in place, not replaced)."""
+        return self._data
 
 
 def _kv8_spans(cache, k, v, row_offsets, start, slot):
@@ -512,14 +517,14 @@ def _kv8_spans(cache, k, v, row_offsets, start, slot):
     rows = k.shape[0]
     if rows != v.shape[0] or row_offsets[n] > rows:
         raise ValueError(f"{rows} rows of k and {v.shape[0]} of v where {row_offsets[n]} are read")
-    _on_gpu("cache", cache.data, dev)
+    _on_gpu("cache", cache._data, dev)
     return cache._ref, k.data_ptr(), v.data_ptr(), stride, _DTYPE_CODES[k.dtype], off, _int32s("start", start, n), _int32s("slot", slot, n), n, _stream()
 
 
 def dlm_kv8_write(cache, k, v, row_offsets, start, slot=None):
     """k, v: device tensors [rows, n_kv, head_dim] (rows may be strided: columns of a wider matrix); the rest: host int lists."""
     ext = _kv8_calls()
-    if ext is not None and _taken(ext.span(0, cache._ref, cache.data, k, v, row_offsets, start, slot, _device(), _stream())):
+    if ext is not None and _taken(ext.span(0, cache._ref, cache._data, k, v, row_offsets, start, slot, _device(), _stream())):
         return
     args = _kv8_spans(cache, k, v, row_offsets, start, slot)
     if k.shape[0]:  # (a tensor without rows has no address)
@@ -531,10 +536,12 @@ def dlm_kv8_read(cache, row_offsets, start, slot=None, k=None, v=None, dtype=tor
     if (k is None) != (v is None):
         raise ValueError("k and v are given together")
     if k is None:
-        rows = int(row_offsets[len(start)])
-        k, v = (torch.empty((rows, cache.n_kv, cache.head_dim), dtype=dtype, device=cache.data.device) for _ in "kv")
+        if len(row_offsets) <= len(start):
+            raise ValueError(f"row_offsets: {len(row_offsets)} entries where {len(start) + 1} are read")
+        rows = max(0, int(row_offsets[len(start)]))
+        k, v = (torch.empty((rows, cache.n_kv, cache.head_dim), dtype=dtype, device=cache._data.device) for _ in "kv")
     ext = _kv8_calls()
-    if ext is not None and _taken(ext.span(1, cache._ref, cache.data, k, v, row_offsets, start, slot, _device(), _stream())):
+    if ext is not None and _taken(ext.span(1, cache._ref, cache._data, k, v, row_offsets, start, slot, _device(), _stream())):
         return k, v
     args = _kv8_spans(cache, k, v, row_offsets, start, slot)
     if k.shape[0]:
@@ -549,7 +556,7 @@ def dlm_kv8_attention(cache, q, row_offsets, n_keys, slot=None, mask=None, out=N
     ext = _kv8_calls()
     if ext is not None and out is not None:
         size = 0 if workspace is None or not workspace.is_contiguous() else workspace.numel() * workspace.element_size()
-        if _taken(ext.attention(cache._ref, cache.data, q, row_offsets, n_keys, slot, mask, out, workspace, size, _device(), _stream())):
+        if _taken(ext.attention(cache._ref, cache._data, q, row_offsets, n_keys, slot, mask, out, workspace, size, _device(), _stream())):
             return out
     n, dev = len(n_keys), _gpu_of("q", q)
     stride = _row_stride("q", q, dev, (None, cache.head_dim), _FLOATS)
@@ -565,9 +572,9 @@ def dlm_kv8_attention(cache, q, row_offsets, n_keys, slot=None, mask=None, out=N
     words = 0
     if mask is not None:
         words = mask.shape[-1]
-        if _row_stride("mask", mask, dev, (words,), (torch.int32,)) != words or mask.shape[0] < packed:
+        if _row_stride("mask", mask, dev, (words,), (torch.int32,)) != words or mask.shape[0] < packed or words >= 2**31:
             raise ValueError(f"mask: {tuple(mask.shape)} for {packed} rows, or not contiguous")
-    _on_gpu("cache", cache.data, dev)
+    _on_gpu("cache", cache._data, dev)
     if rows == 0:
         return out
     L = lib()
@@ -597,7 +604,7 @@ def dlm_qk_norm_rope(x, positions, n_q, n_kv, head_dim, q_gain=None, k_gain=None
     if out is None:
         out = torch.empty((rows, width), dtype=dtype, device=x.device)
     out_stride = stride if out is x else _row_stride("out", out, dev, (None,), (dtype,))
-    if columns < width or out.shape[1] < width or out.shape[0] != rows:
+    if rows >= 2**31 or min(n_q, n_kv, head_dim) < 0 or columns < width or out.shape[1] < width or out.shape[0] != rows:
         raise ValueError(f"rows of {columns} and {out.shape[1]} columns where {width} are read and written, or not as many rows of out")
     _vector("positions", positions, dev, rows, torch.int32)
     if q_gain is not None:

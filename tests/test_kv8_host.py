@@ -175,6 +175,29 @@ def test_python_refusals_before_the_library(monkeypatch):
         api.Kv8Cache(1, 64, 2, 64, format="e5m2", device="cpu")
     with pytest.raises(api.DlmError, match="ESHAPE"):
         api.Kv8Cache(1, 64, 2, 65, device="cpu")
+    with pytest.raises(AttributeError):  # (the library has its address)
+        c.data = torch.zeros_like(c.data)
+
+
+def test_sizes_beyond_32_bits(monkeypatch):
+    """They would arrive at the library as their low 32 bits."""
+    for bad in ((2**32 + 1, 64, 2, 64), (1, 2**32 + 64, 2, 64), (1, 64, 2**32 + 2, 64), (1, 64, 2, 2**32 + 64)):
+        with pytest.raises(api.DlmError, match="ESHAPE"):
+            api.Kv8Cache(*bad, device="cpu")
+    monkeypatch.setattr(api, "_device", lambda: -1)
+    monkeypatch.setattr(api, "_stream", lambda: 0)
+    monkeypatch.setattr(api, "_gpu_of", lambda name, t: -1)
+    many = torch.zeros(1, 128, dtype=torch.bfloat16).expand(2**32 + 1, 128)
+    with pytest.raises(ValueError):
+        api.dlm_qk_norm_rope(many, torch.zeros(1, dtype=torch.int32).expand(2**32 + 1), 1, 1, 64, out=many)
+    few = torch.zeros(3, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        api.dlm_qk_norm_rope(few, torch.zeros(3, dtype=torch.int32), 2**32 + 1, 1 - 2**32, 64)
+    cache = api.Kv8Cache(2, 64, 2, 64, device="cpu")
+    with pytest.raises(ValueError):  # fewer offsets than sequences
+        api.dlm_kv8_read(cache, [0], [0])
+    with pytest.raises(api.DlmError, match="EINVAL"):  # (the library's: offsets that decrease; a row so that it is asked)
+        api.dlm_kv8_read(cache, [0, -3], [0], k=few.unflatten(1, (2, 64)), v=few.clone().unflatten(1, (2, 64)))
 
 
 # ---- the extension and the way through ctypes: the same C call, or the same refusal ----------------------------------------------------
