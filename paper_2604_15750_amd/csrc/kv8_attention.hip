@@ -85,7 +85,8 @@ struct Tile {
   static constexpr bool F32 = std::is_same<T, float>::value;
   static constexpr float P_TOP = F32 ? 13.f : 8.f;  // log2 of where the largest p' is put: half ends 25 bits below 1
   static constexpr int PIECES = HD / 32, KF = HD / 16, TERMS = F32 ? 2 : 1;
-  f16x8 qf[TERMS][KF];
+  f16x8 qf[KF];
+  f16x8* low;                      // fp32: LDS, the low terms (the same in all wavefronts of a workgroup, and each reads what it wrote)
   f32x16 o[PIECES], from_m;        // from_m: -m / cq in every element, what the products start from
   float qs, cq, rest, m, l, limit; // rest: what cq leaves of the scale (fp32); m: a whole number; limit: minus infinity until the query has seen a key
   int ref;                         // biased exponent that K's scales are relative to
@@ -112,8 +113,16 @@ struct Tile {
       for (int i = 0; i < 8; ++i) {
         const float y = v[f][i] * up;
         const f16_t hi = (f16_t)y;
-        qf[0][f][i] = hi;
-        if (F32) qf[TERMS - 1][f][i] = (f16_t)(y - (float)hi);
+        qf[f][i] = hi;
+        v[f][i] = y - (float)hi;
+      }
+    if (F32)
+#pragma unroll
+      for (int f = 0; f < KF; ++f) {
+        f16x8 r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r[i] = (f16_t)v[f][i];
+        low[f * 64 + lane] = r;
       }
     m = l = cq = rest = 0.f;
     limit = -__builtin_inff();
@@ -171,7 +180,7 @@ struct Tile {
       const u32x4 raw = k(f >> 1);
       const f16x8 kf = halves<FMT>(raw[f % 2 * 2], raw[f % 2 * 2 + 1], k_scale, k_mul, k_add);
 #pragma unroll
-      for (int x = 0; x < TERMS; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, qf[x][f], s, 0, 0, 0);
+      for (int x = 0; x < TERMS; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, x ? low[f * 64 + (threadIdx.x & 63)] : qf[f], s, 0, 0, 0);
     }
     after_k();
     float p[16];  // of the lane's keys 8j + 4h + i
@@ -265,19 +274,20 @@ __device__ inline void put(const Kv8AttnArgs& a, const Work& w, int split_out, i
 
 constexpr int NWV = 4;  // wavefronts of a workgroup, which share its keys
 
-template <int HD>
+template <int HD, bool F32>
 struct alignas(16) AttnLds {
+  f16x8 low[F32 ? HD / 16 * 64 : 1];  // (in registers: one wavefront a SIMD instead of two; 1280 rows x 32 heads over themselves 99 us, 70 here)
   float b[NWV][32], inv[NWV][32];  // of a block's keys: V's exponent, and what undoes its scale
   float m[NWV][32], l[NWV][32];    // the wavefronts' maxima and sums
   float o[NWV][32][HD + 4];        // ... and outputs (a query's 16 bytes apart from a multiple of the banks)
 };
 
 template <typename T, int HD, int FMT>
-__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 128 && sizeof(T) == 4 ? 1 : 2))) void kv8_attention_kernel(
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(2))) void kv8_attention_kernel(
     const unsigned char* __restrict__ data, int head_blocks, int n_kv, const T* __restrict__ q, int64_t q_stride, int group, int chunk, int one_rows, int one_keys,
     int one_slot, int split_out, Kv8AttnArgs a, Kv8AttnMeta meta) {
   constexpr int PIECES = HD / 32;
-  __shared__ AttnLds<HD> L;
+  __shared__ AttnLds<HD, Tile<T, HD, FMT>::F32> L;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, c = lane & 31;
   // (the heads of a tile are neighbours: where their number is a multiple of 8 all tiles of a head are on one XCD, and its L2 has the head's K and V)
   Work w;
@@ -326,6 +336,7 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 
   load_v(w.blk0 + wave);
   w.first = a.mask ? w.n_keys - nr : w.n_keys;
   Tile<T, HD, FMT> t;
+  t.low = L.low;
   t.start(q, q_stride, a, w, lane);
   for (int blk = w.blk0 + wave; blk < w.blk1; blk += NWV) {
     const unsigned nan_keys = (unsigned)__builtin_amdgcn_ballot_w64(max(kb, vb) == KV8_NAN), k_now = kb;
