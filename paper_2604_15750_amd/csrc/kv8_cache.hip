@@ -3,7 +3,10 @@
 // Write, per vector x: E = the smallest integer in [-60, 60] with max|x| <= M 2^E (M = 448 e4m3, 127 i8), code = x 2^-E rounded to the
 // format (to even), saturated.  E follows from the bits of max|x|, so nothing is rounded but the code.  Read: code 2^E, exact in
 // bf16 and fp32.  Both are bound by memory: every value is moved once, one workgroup a block of 32 positions of one head, whose
-// image is put together (taken apart) in LDS, because V's codes lie transposed in it.
+// image is put together (taken apart) in LDS, because V's codes lie transposed in it.  The heads of a block's rows are neighbours in the
+// grid, so what the chip touches at a time is whole rows.  16384 rows (TB/s moved, written / read; a large copy reaches 4.9): 32 heads of
+// 128 bf16 5.4 / 5.2, fp32 5.8 / 4.8; 16 of 64 4.4 / 4.2; 32 of 32 3.5 / 3.3 (a head's 64 bytes of a row are half a line).  1280 rows x 32
+// heads of 128 9.0 / 8.5 us (floor 6.4), 8 rows 4.6 / 2.8 us: a launch and its trips to memory.
 #include <type_traits>
 
 #include "kv8.h"
@@ -59,7 +62,8 @@ __device__ inline unsigned group_max(unsigned v) {  // over N neighbouring lanes
 
 // V lies transposed in a block: four neighbouring positions share a word.  A wavefront has four positions 16 lanes apart; a lane's two words
 // (its position's codes of 8 dims) become dims 2i and 2i + 1 of all four positions, i its row of 16 lanes, and back.  (Byte by byte
-// through LDS: 5120 rows x 32 heads written in 26.4 us, 23.0 now; read in 23.6, 19.8 now.)
+// through LDS: 3904 blocks of 32 x 128 bf16 written in 26.4 us, 22.8 to
+// 25 now; read in 23.6, 19 now.)
 struct Two { unsigned a, b; };
 __device__ inline Two swap16(Two v) { const auto r = __builtin_amdgcn_permlane16_swap(v.a, v.b, false, false); return Two{r[0], r[1]}; }
 __device__ inline Two swap32(Two v) { const auto r = __builtin_amdgcn_permlane32_swap(v.a, v.b, false, false); return Two{r[0], r[1]}; }
@@ -148,22 +152,21 @@ __device__ inline Place place_of(const Kv8Meta& m, int n_kv) {
   return p;
 }
 
-// A thread has 8 dims of a position, 16 lanes the dims of one to four positions 4 apart (lane_rows), whose neighbours are in the rows of 16 lanes
+// (heads of 32 with 256 threads, half of them idle: 16384 rows x 32 heads fp32 read in 49.6 us, 41.8 now, bf16 written in 30.5, 29.3 now)
+// A thread has 8 dims of a position, 16 lanes the dims of one to four positions 4 apart, whose neighbours are in the other rows of 16 lanes
 template <int HD>
 struct Lanes {
-  static constexpr int N = HD / 8, ROWS = 256 / N < 32 ? 256 / N : 32, PASSES = 32 / ROWS;  // positions of a pass
+  static constexpr int N = HD / 8, THREADS = 32 * N < 256 ? 32 * N : 256, ROWS = THREADS / N, PASSES = 32 / ROWS;  // ROWS: positions of a pass
   int p, d;
-  bool idle;  // (wavefronts that have no position)
   __device__ inline Lanes() {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     p = (wave * (16 / N) + (lane & 15) / N) * 4 + (lane >> 4);
     d = lane % N * 8;
-    idle = p >= 32;
   }
 };
 
 template <typename T, int HD, int FMT>
-__global__ __launch_bounds__(256) void kv8_write_kernel(const T* __restrict__ k, const T* __restrict__ v, int64_t stride, Kv8View c, Kv8Meta m) {
+__global__ __launch_bounds__(Lanes<HD>::THREADS) void kv8_write_kernel(const T* __restrict__ k, const T* __restrict__ v, int64_t stride, Kv8View c, Kv8Meta m) {
   typedef Lanes<HD> L;
   __shared__ __align__(16) unsigned char img[kv8_block_bytes(HD)];
   const Place w = place_of(m, c.n_kv);
@@ -178,30 +181,29 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(const T* __restrict__ k,
       x[1][n].load(v + at);
     }
   }
-  if (!t.idle)
 #pragma unroll
-    for (int n = 0; n < L::PASSES; ++n) {
-      const int p = n * L::ROWS + t.p;
+  for (int n = 0; n < L::PASSES; ++n) {
+    const int p = n * L::ROWS + t.p;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const unsigned sb = scale_byte<FMT>(group_max<L::N>(x[s][n].top()));
-        const Two codes = codes8<FMT>(x[s][n], sb);
-        if (s == 0) {
-          *(u32x2*)&img[byte_at(kv8_k_index(p, t.d, HD))] = u32x2{codes.a, codes.b};
-        } else {
-          const Two dims = by_dims(codes);
-          const int d = t.d + 2 * (p & 3);
-          *(unsigned*)&img[byte_at(kv8_v_index(p & ~3, d, HD))] = dims.a;
-          *(unsigned*)&img[byte_at(kv8_v_index(p & ~3, d + 1, HD))] = dims.b;
-        }
-        if (t.d == 0) img[kv8_scale_index(p, s, HD)] = (unsigned char)sb;
+    for (int s = 0; s < 2; ++s) {
+      const unsigned sb = scale_byte<FMT>(group_max<L::N>(x[s][n].top()));
+      const Two codes = codes8<FMT>(x[s][n], sb);
+      if (s == 0) {
+        *(u32x2*)&img[byte_at(kv8_k_index(p, t.d, HD))] = u32x2{codes.a, codes.b};
+      } else {
+        const Two dims = by_dims(codes);
+        const int d = t.d + 2 * (p & 3);
+        *(unsigned*)&img[byte_at(kv8_v_index(p & ~3, d, HD))] = dims.a;
+        *(unsigned*)&img[byte_at(kv8_v_index(p & ~3, d + 1, HD))] = dims.b;
       }
+      if (t.d == 0) img[kv8_scale_index(p, s, HD)] = (unsigned char)sb;
     }
+  }
   __syncthreads();
   unsigned char* out = c.data + ((int64_t)w.slot * c.n_kv + w.head) * c.head_bytes + (int64_t)w.block * kv8_block_bytes(HD);
   if (w.lo == 0 && w.hi == 32) {
 #pragma unroll
-    for (int i = threadIdx.x; i < 4 * HD; i += 256) ((u32x4*)out)[i] = ((const u32x4*)img)[unit_at(i)];
+    for (int i = threadIdx.x; i < 4 * HD; i += L::THREADS) ((u32x4*)out)[i] = ((const u32x4*)img)[unit_at(i)];
     if (threadIdx.x < 4) ((u32x4*)out)[4 * HD + threadIdx.x] = ((const u32x4*)img)[4 * HD + threadIdx.x];
     return;
   }
@@ -215,26 +217,25 @@ __global__ __launch_bounds__(256) void kv8_write_kernel(const T* __restrict__ k,
         if (bits >> j & 1) out[4 * i + j] = (unsigned char)(word >> 8 * j);
   };
 #pragma unroll
-  for (int i = threadIdx.x; i < 8 * HD; i += 256)  // K: a word is one position's
+  for (int i = threadIdx.x; i < 8 * HD; i += L::THREADS)  // K: a word is one position's
     if (here >> (i >> 2 & 31) & 1) ((unsigned*)out)[i] = *(const unsigned*)&img[byte_at(4 * i)];
 #pragma unroll
-  for (int i = 8 * HD + threadIdx.x; i < 16 * HD; i += 256)  // V: four positions'
+  for (int i = 8 * HD + threadIdx.x; i < 16 * HD; i += L::THREADS)  // V: four positions'
     put(i, *(const unsigned*)&img[byte_at(4 * i)], here >> ((i & 3) * 8 + (i >> 2 & 32) / 8) & 15u);
   if (threadIdx.x < 16) put(16 * HD + threadIdx.x, ((const unsigned*)img)[16 * HD + threadIdx.x], here >> (threadIdx.x & 7) * 4 & 15u);
 }
 
 template <typename T, int HD, int FMT>
-__global__ __launch_bounds__(256) void kv8_read_kernel(T* __restrict__ k, T* __restrict__ v, int64_t stride, Kv8View c, Kv8Meta m) {
+__global__ __launch_bounds__(Lanes<HD>::THREADS) void kv8_read_kernel(T* __restrict__ k, T* __restrict__ v, int64_t stride, Kv8View c, Kv8Meta m) {
   typedef Lanes<HD> L;
   __shared__ __align__(16) unsigned char img[kv8_block_bytes(HD)];
   const Place w = place_of(m, c.n_kv);
   const unsigned char* in = c.data + ((int64_t)w.slot * c.n_kv + w.head) * c.head_bytes + (int64_t)w.block * kv8_block_bytes(HD);
 #pragma unroll
-  for (int i = threadIdx.x; i < 4 * HD; i += 256) ((u32x4*)img)[unit_at(i)] = ((const u32x4*)in)[i];
+  for (int i = threadIdx.x; i < 4 * HD; i += L::THREADS) ((u32x4*)img)[unit_at(i)] = ((const u32x4*)in)[i];
   if (threadIdx.x < 4) ((u32x4*)img)[4 * HD + threadIdx.x] = ((const u32x4*)in)[4 * HD + threadIdx.x];
   __syncthreads();
   const L t;
-  if (t.idle) return;
 #pragma unroll
   for (int n = 0; n < L::PASSES; ++n) {
     const int p = n * L::ROWS + t.p, d = t.d + 2 * (p & 3);
@@ -264,12 +265,12 @@ void for_shape(int format, int hd, int dtype, F f) {
 void launch_kv8_write(const Kv8View& c, int format, int hd, const void* k, const void* v, int64_t stride, int dtype, const Kv8Meta& m, hipStream_t st) {
   for_shape(format, hd, dtype, [&](auto t, auto hd_c, auto fmt_c) {
     typedef decltype(t) T;
-    kv8_write_kernel<T, hd_c(), fmt_c()><<<m.block_off[m.n_seqs] * c.n_kv, 256, 0, st>>>((const T*)k, (const T*)v, stride, c, m);
+    kv8_write_kernel<T, hd_c(), fmt_c()><<<m.block_off[m.n_seqs] * c.n_kv, Lanes<hd_c()>::THREADS, 0, st>>>((const T*)k, (const T*)v, stride, c, m);
   });
 }
 void launch_kv8_read(const Kv8View& c, int format, int hd, void* k, void* v, int64_t stride, int dtype, const Kv8Meta& m, hipStream_t st) {
   for_shape(format, hd, dtype, [&](auto t, auto hd_c, auto fmt_c) {
     typedef decltype(t) T;
-    kv8_read_kernel<T, hd_c(), fmt_c()><<<m.block_off[m.n_seqs] * c.n_kv, 256, 0, st>>>((T*)k, (T*)v, stride, c, m);
+    kv8_read_kernel<T, hd_c(), fmt_c()><<<m.block_off[m.n_seqs] * c.n_kv, Lanes<hd_c()>::THREADS, 0, st>>>((T*)k, (T*)v, stride, c, m);
   });
 }

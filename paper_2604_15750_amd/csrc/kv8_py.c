@@ -1,6 +1,6 @@
 // Python calls of the 8-bit cache's operators (dlm_kv8_write, dlm_kv8_read, dlm_kv8_attention, dlm_qk_norm_rope of dlm.h) without ctypes.
 // Their kernels take a few microseconds at the row counts of a decode, so a call is bound by what checking and marshalling its
-// arguments costs the host: 3.3 us on top of the C call in Python, 1.0 here (dlm_qk_norm_rope of 8 rows: 7.2 -> 4.7 us a call).
+// arguments costs the host: 3.3 us on top of the C call in Python, 1.0 here (dlm_qk_norm_rope of 8 rows: 7.2 -> 5.1 us a call).
 // Only calls that need no refusal are taken: tensors on the given GPU, of the types and shapes that the operator reads, with
 // contiguous rows; lists or tuples of ints that fit 32 bits, long enough and at most 32 sequences.  Anything else returns None before
 // anything is launched, and the caller goes the way through ctypes, which takes every other form and says what it refuses.

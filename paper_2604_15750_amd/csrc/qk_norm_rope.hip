@@ -3,7 +3,9 @@
 // y = x rsqrt(mean(x^2) + eps) gain;  (y1, y2) -> (y1 cos a - y2 sin a, y2 cos a + y1 sin a), a = position theta^(-2i/hd), pairs
 // (i, i + hd/2).  Bound by memory (each value read and written once).  A lane holds 16 bytes of a head's first half and the 16 bytes
 // of the second half that they are paired with, so the rotation exchanges nothing and the norm's sum goes over 2 to 16 lanes; a
-// wavefront has one row's angles and up to ITERS x 64 / LANES of its heads.
+// wavefront has one row's angles and up to ITERS x 64 / LANES of its heads: the angles (a sine and a cosine in 64-bit turns, by far the
+// most instructions) are computed while its loads are on their way.  2048 rows x 32 heads of 128 bf16 8.6 us (6.8 at the rate of a large
+// copy), fp32 600 rows x 64 heads 8.9 (8.0); 8 rows 3.8: a launch.
 #include "kv8.h"
 
 namespace {
