@@ -58,6 +58,33 @@ __device__ inline int seq_of(const int32_t* off, int n_seqs, int i) {
   return __popcll(__ballot(lane < DLM_MAX_SEQS && lane + 1 < n_seqs && i >= off[min(lane, DLM_MAX_SEQS - 1) + 1]));
 }
 
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
+// eight values of a row as they lie in memory, the bits of their largest magnitude, and the values
+template <typename T> struct Eight;
+template <> struct Eight<bf16_t> {
+  u32x4 w = {0, 0, 0, 0};
+  __device__ inline void load(const bf16_t* p) { w = *(const u32x4*)p; }
+  __device__ inline unsigned top() const {  // (two at a time)
+    u16x2 t = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t = __builtin_elementwise_max(t, __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu));
+    return (unsigned)(t[0] > t[1] ? t[0] : t[1]) << 16;
+  }
+  __device__ inline float operator[](int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xFFFF0000u : w[i >> 1] << 16); }
+};
+template <> struct Eight<float> {
+  f32x4 a = {0.f, 0.f, 0.f, 0.f}, b = {0.f, 0.f, 0.f, 0.f};
+  __device__ inline void load(const float* p) { a = *(const f32x4*)p; b = *(const f32x4*)(p + 4); }
+  __device__ inline unsigned top() const {
+    unsigned t = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t = max(t, max(__float_as_uint(a[i]) & 0x7FFFFFFFu, __float_as_uint(b[i]) & 0x7FFFFFFFu));
+    return t;
+  }
+  __device__ inline float operator[](int i) const { return i < 4 ? a[i] : b[i - 4]; }
+};
+
 void launch_kv8_write(const Kv8View& c, int format, int hd, const void* k, const void* v, int64_t stride, int dtype, const Kv8Meta& m, hipStream_t st);
 void launch_kv8_read(const Kv8View& c, int format, int hd, void* k, void* v, int64_t stride, int dtype, const Kv8Meta& m, hipStream_t st);
 struct Kv8AttnPlan {

@@ -20,7 +20,7 @@
 // moves only where a score would leave half's range: the largest p' is brought to about 2^8 (fp32: 2^13) and may grow to 2^15 before that.
 // What bounds it: 1280 rows x 32 heads of 128 over themselves 42 us, 0.64 PFLOP/s (fp32 70), 4096 rows 330 us, 0.83 (a large half product
 // reaches 1.12 to 1.22): the chip's power limit and the vector instructions, 145 a block of 32 keys beside 16 products.  Single tokens of 24
-// sequences of up to 8192 keys, 28 of 4 heads: 30.7 us, 5 TB/s of cache.  Few rows: latency, 8 rows x 32 heads of 392 keys 6.6 us.
+// sequences of up to 8192 keys, 28 of 4 heads: 30.7 us, 5 TB/s of cache.  Few rows: latency, 8 rows x 32 heads of 392 keys 6.5 us.
 // Why 32 queries, one wavefront's work: a group's heads of a few rows fill 32, not 128.  Four wavefronts share the keys because a decode
 // has few tiles and many keys.  Tried and slower: K and V through LDS for 4 x 32 queries (1280 rows 55.6 us, 42 at that time; only 1024 rows
 // of 4096 keys gained, 110 to 91), two tiles a wavefront (73), 8 wavefronts a workgroup (392 keys 7.9, 7.4 then), V loaded two blocks ahead
@@ -63,16 +63,6 @@ __device__ inline f16x8 halves(unsigned lo, unsigned hi, float scale, f16x2 mul,
   return f16x8{h[0][0], h[0][1], h[1][0], h[1][1], h[2][0], h[2][1], h[3][0], h[3][1]};
 }
 
-__device__ inline void load8(const bf16_t* p, float (&x)[8]) {
-  const bf16x8 v = *(const bf16x8*)p;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = (float)v[i];
-}
-__device__ inline void load8(const float* p, float (&x)[8]) {
-  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
-}
 __device__ inline void store4(bf16_t* p, f32x4 v) { *(bf16x4*)p = bf16x4{(bf16_t)v[0], (bf16_t)v[1], (bf16_t)v[2], (bf16_t)v[3]}; }
 __device__ inline void store4(float* p, f32x4 v) { *(f32x4*)p = v; }
 
@@ -103,34 +93,26 @@ struct Tile {
     const int h = lane >> 5, x = w.q0 + (lane & 31), r = x < w.nq ? w.row_of(x) : 0, hq = x < w.nq ? x - r * w.group : 0;
     const T* from = q + (int64_t)(w.row0 + r) * q_stride + (w.head * w.group + hq) * HD + 16 * h;
     words = a.mask + (int64_t)(w.row0 + r) * a.mask_words;
-    float v[KF][8];
+    Eight<T> v[KF];
     unsigned top = 0;
 #pragma unroll
-    for (int f = 0; f < KF; ++f) load8(from + 32 * (f >> 1) + 8 * (f & 1), v[f]);
+    for (int f = 0; f < KF; ++f) v[f].load(from + 32 * (f >> 1) + 8 * (f & 1));
 #pragma unroll
-    for (int f = 0; f < KF; ++f)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[f][i]) & 0x7FFFFFFFu);
+    for (int f = 0; f < KF; ++f) top = max(top, v[f].top());
     const int e = min(max((int)(__float_as_uint(halves_max(__uint_as_float(top & 0x7F800000u))) >> 23) - 127, -100), 127);
     const float up = __uint_as_float((unsigned)(127 + 14 - e) << 23);
     qs = __uint_as_float((unsigned)(127 - 14 + e) << 23);
 #pragma unroll
-    for (int f = 0; f < KF; ++f)
+    for (int f = 0; f < KF; ++f) {
+      f16x8 rest_of;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float y = v[f][i] * up;
-        const f16_t hi = (f16_t)y;
-        qf[f][i] = hi;
-        v[f][i] = y - (float)hi;
+        qf[f][i] = (f16_t)y;
+        rest_of[i] = (f16_t)(y - (float)qf[f][i]);
       }
-    if (F32)
-#pragma unroll
-      for (int f = 0; f < KF; ++f) {
-        f16x8 r;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) r[i] = (f16_t)v[f][i];
-        low[f * 64 + lane] = r;
-      }
+      if (F32) low[f * 64 + lane] = rest_of;
+    }
     m = l = cq = rest = 0.f;
     limit = -__builtin_inff();
     ref = -1000;
@@ -324,18 +306,16 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(2))) v
   u32x4 kr[PIECES], vr[PIECES];
   unsigned kb, vb;  // scale bytes of position c
   auto load_k = [&](int blk) __attribute__((always_inline)) {
-    const bool there = blk < w.blk1;
-    const unsigned char* p = w.region + (int64_t)(there ? blk : 0) * kv8_block_bytes(HD);
-    const int at = there ? lane : 0;
+    const int there = (blk - w.blk1) >> 31, at = lane & there;  // (all bits or none: the compiler makes a branch of a condition)
+    const unsigned char* p = w.region + (int64_t)(blk & there) * kv8_block_bytes(HD);
     kb = p[64 * HD + c];
     vb = p[64 * HD + 32 + c];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) kr[i] = ((const u32x4*)p)[i * 64 + at];
   };
   auto load_v = [&](int blk) __attribute__((always_inline)) {
-    const bool there = blk < w.blk1;
-    const u32x4* p = (const u32x4*)(w.region + (int64_t)(there ? blk : 0) * kv8_block_bytes(HD));
-    const int at = there ? lane : 0;
+    const int there = (blk - w.blk1) >> 31, at = lane & there;
+    const u32x4* p = (const u32x4*)(w.region + (int64_t)(blk & there) * kv8_block_bytes(HD));
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) vr[i] = p[(PIECES + i) * 64 + at];
   };
