@@ -411,37 +411,40 @@ size_t kv8_attention_partials(int64_t rows, int n_q) {
 // rows x 32 heads of up to 4096 107 / 91.0 / 85.9 / 85.5 / 94.5.
 Kv8AttnPlan kv8_attention_plan(const int32_t* row_off, const int32_t* n_keys, int n_seqs, int n_q, int n_kv) {
   const int group = n_q / n_kv;
-  int64_t work = 0;  // blocks of all workgroups
-  int blocks = 1;    // ... of the longest
+  int64_t work = 0, whole = 0, tiles[DLM_MAX_SEQS];  // blocks of all workgroups; their number without shares; (32 queries, kv head) pairs
+  int blocks = 1;                                    // of the longest
   for (int b = 0; b < n_seqs; ++b) {
-    const int64_t tiles = tiles_of(row_off[b + 1] - row_off[b], group);
-    work += tiles * n_kv * blocks_of(n_keys[b]);
-    if (tiles && blocks_of(n_keys[b]) > blocks) blocks = blocks_of(n_keys[b]);
+    tiles[b] = tiles_of(row_off[b + 1] - row_off[b], group) * n_kv;
+    whole += tiles[b];
+    work += tiles[b] * blocks_of(n_keys[b]);
+    if (tiles[b] && blocks_of(n_keys[b]) > blocks) blocks = blocks_of(n_keys[b]);
   }
   const int64_t all = (int64_t)row_off[n_seqs] * n_q, most = all ? MAX_PARTIALS / all < MAX_SHARES ? MAX_PARTIALS / all : MAX_SHARES : 1;
   Kv8AttnPlan p;
   p.chunk = blocks;
   p.splits = 1;
-  if (most >= 2) {
+  constexpr int LEAST = 8, JOIN = 18;
+  if (most >= 2 && blocks > LEAST + JOIN) {
     // the least chunk with which the workgroups are no more than `rounds` a compute unit, from `least` to `last`; 0 if there is none
     auto fit = [&](int rounds, int64_t least, int64_t last) -> int64_t {
+      if (whole > rounds * CUS) return 0;
       int64_t chunk = (work + rounds * CUS - 1) / (rounds * CUS);
       if (chunk < least) chunk = least;
       for (; chunk <= last; ++chunk) {
         int64_t wgs = 0;
         for (int b = 0; b < n_seqs; ++b) {
-          const int64_t shares = (blocks_of(n_keys[b]) + chunk - 1) / chunk;
-          wgs += tiles_of(row_off[b + 1] - row_off[b], group) * n_kv * (shares > 1 ? shares : 1);
+          const int shares = (blocks_of(n_keys[b]) + (int)chunk - 1) / (int)chunk;
+          wgs += tiles[b] * (shares > 1 ? shares : 1);
         }
         if (wgs <= rounds * CUS) return chunk;
       }
       return 0;
     };
-    int64_t chunk = fit(1, 8, 40);
+    int64_t chunk = fit(1, LEAST, 40);
     if (!chunk) chunk = fit(2, 24, 44);
     if (!chunk) chunk = 24;
     if (chunk * most < blocks) chunk = (blocks + most - 1) / most;
-    if (chunk + 18 < blocks) {
+    if (chunk + JOIN < blocks) {
       p.chunk = (int)chunk;
       p.splits = (int)((blocks + chunk - 1) / chunk);
     }
