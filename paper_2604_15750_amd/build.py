@@ -1,4 +1,4 @@
-"""Compile csrc/*.hip into paper_2604_15750_amd/libdlm.so for gfx950, csrc/decisions_py.c into _decisions and csrc/kv8_py.c into _kv8 (in-tree,
+"""Compile csrc/*.hip into paper_2604_15750_amd/libdlm.so for gfx950, csrc/decisions_py.c into _decisions and csrc/kv8_py.cpp into _kv8 (in-tree,
 no torch dependency)."""
 import os
 import shutil
@@ -47,15 +47,15 @@ def build(verbose=False):
     return OUT
 
 
-def _compile_extension(source, out, calls):
-    """None without gcc or Python's headers: `calls` then go through ctypes."""
-    gcc, include = shutil.which("gcc"), sysconfig.get_paths()["include"]
-    if gcc is None or not os.path.exists(os.path.join(include, "Python.h")):
-        print(f"no gcc or no Python.h: {calls} are called through ctypes", file=sys.stderr)
+def _compile_extension(source, out, calls, compiler="gcc", flags=()):
+    """None without the compiler or Python's headers: `calls` then go through ctypes."""
+    cc, include = shutil.which(compiler), sysconfig.get_paths()["include"]
+    if cc is None or not os.path.exists(os.path.join(include, "Python.h")):
+        print(f"no {compiler} or no Python.h: {calls} are called through ctypes", file=sys.stderr)
         return None
-    r = subprocess.run([gcc, "-O2", "-shared", "-fPIC", "-I", include, "-o", out, os.path.join(CSRC, source)], capture_output=True, text=True)
+    r = subprocess.run([cc, "-O2", "-shared", "-fPIC", "-I", include, "-o", out, os.path.join(CSRC, source), *flags], capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"gcc failed on {source}:\n" + r.stderr)
+        raise RuntimeError(f"{compiler} failed on {source}:\n" + r.stderr)
     return out
 
 
@@ -68,10 +68,14 @@ def build_extension():
 
 
 def build_kv8_extension():
-    """The same for the 8-bit cache's operators."""
+    """The same for the 8-bit cache's operators, against torch's headers: its tensors are read without a call into Python."""
+    import torch
     if os.path.exists(OUT_KV8):
         os.remove(OUT_KV8)
-    return _compile_extension("kv8_py.c", OUT_KV8, "the 8-bit cache's operators")
+    at = os.path.dirname(torch.__file__)
+    return _compile_extension("kv8_py.cpp", OUT_KV8, "the 8-bit cache's operators", "g++",
+                              ["-std=c++17", "-I", os.path.join(at, "include"), f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                               "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
 
 
 if __name__ == "__main__":

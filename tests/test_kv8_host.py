@@ -268,13 +268,12 @@ def both(monkeypatch):
 
         span, attention, rope = (staticmethod(lambda *a, f=f: Spy.ask(f, a)) for f in (ext.span, ext.attention, ext.rope))
 
-    types = (torch.float32, torch.bfloat16, torch.int32)
     real = [C.cast(f, VP).value for f in (L.dlm_kv8_write, L.dlm_kv8_read, L.dlm_kv8_attention, L.dlm_qk_norm_rope)]
     for name, value in (("lib", lambda: Recorder), ("_device", lambda: -1), ("_stream", lambda: 0x1230), ("_gpu_of", lambda name, t: -1)):
         monkeypatch.setattr(api, name, value)
-    ext.bind(*(C.cast(f, VP).value for f in calls), *types)
+    ext.bind(*(C.cast(f, VP).value for f in calls))
     yield self
-    ext.bind(*real, *types)
+    ext.bind(*real)
 
 
 BF = torch.bfloat16
