@@ -24,7 +24,8 @@
 // Why 32 queries, one wavefront's work: a group's heads of a few rows fill 32, not 128.  Four wavefronts share the keys because a decode
 // has few tiles and many keys.  Tried and slower: K and V through LDS for 4 x 32 queries (1280 rows 55.6 us, 42 at that time; only 1024 rows
 // of 4096 keys gained, 110 to 91), two tiles a wavefront (73), 8 wavefronts a workgroup (392 keys 7.9, 7.4 then), V loaded two blocks ahead
-// (46.6, 44), queries in LDS so that three wavefronts fit a SIMD (392 keys 7.9, 6.7; 4096 rows 351, 343).
+// (46.6, 44), queries in LDS so that three wavefronts fit a SIMD (392 keys 7.9, 6.7; 4096 rows 351, 343), the next block's scores under this
+// block's exponentials (392 keys 6.85, 6.7; 4096 rows 370, 356).
 #include <type_traits>
 
 #include "kv8.h"
