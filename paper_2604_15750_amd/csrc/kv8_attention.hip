@@ -11,7 +11,9 @@
 // The scales: with K_j = 2^a_j code_j and V_j = 2^b_j code_j,
 //   s'_j = (q . K_j) log2(e) / sqrt(hd) + b_j,   p'_j = 2^(s'_j - m),   l = sum_j p'_j 2^-b_j,   o = sum_j p'_j code_j / l
 //   a  goes in where codes become half (the conversion scales; i8 takes it in the multiply-add that takes its offset off), relative to a
-//      wavefront's `ref`, which is raised where a block's keys would leave half's range; keys 2^-24 below it lose bits
+//      wavefront's `ref`, which moves where a block has a key 2^6 above it or 2^-16 below it: half holds every code in between exactly, so
+//      a score does not depend on ref, nor on any other key.  The products of a block whose keys lie further apart are made once
+//      for each range of scales in it, from codes that are loaded again (rare, and out of the way of other blocks)
 //   b  is the addend of the multiply-add that applies the softmax's scale, and the sum's addition becomes a multiply-add.  p' stays
 //      bounded whatever the scales.  b in [-60, 60] keeps l within 32 bits, and a value whose scale is 2^-B of the largest has its part
 //      in l down to a probability of 2^(B-134) of that one's (fp32 2^(B-139)): 2^-34 (2^-39) for values 2^100 apart.
@@ -36,6 +38,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float NEG_BIG = -3.0e38f;
 constexpr float P_LIMIT = 15.f;  // log2 of where the largest p' may go
+constexpr unsigned REF_ABOVE = 5, REF_BELOW = 15;  // of ref: 1152 2^5 and 448 2^5 are below half's largest, 2^-9 2^-15 (e4m3's smallest code) is its smallest
 
 __device__ inline float halves_max(float v) {  // over the two lanes of a query
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -69,6 +72,9 @@ __device__ inline void store4(float* p, f32x4 v) { *(f32x4*)p = v; }
 
 // what an output is multiplied with: a row that sees nothing gives 0, one whose sum is not a positive number NaN
 __device__ inline float reciprocal(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : __uint_as_float(0x7FC00000u); }
+
+// whether a scale byte of K is one: a position that was never written (zero beside any other) or is marked NaN is right with any ref
+__device__ inline bool has_scale(unsigned kb) { return kb - 1u < KV8_NAN - 1u; }
 
 // What a workgroup works on
 struct Work {
@@ -114,11 +120,9 @@ struct Tile {
       }
       if (F32) low[f * 64 + lane] = rest_of;
     }
-    m = l = cq = rest = 0.f;
+    m = l = 0.f;
     limit = -__builtin_inff();
-    ref = -1000;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) from_m[i] = 0.f;
+    set_ref(127);  // (a largest magnitude of 2^-6 to 2^13: what normalised heads hold)
 #pragma unroll
     for (int d = 0; d < PIECES; ++d) o[d] = from_m;
   }
@@ -142,26 +146,31 @@ struct Tile {
     for (int i = 0; i < 16; ++i) from_m[i] = t;
   }
 
-  // One block of 32 positions.  kb: K's scale byte of position lane % 32; nan_keys: bits of positions marked NaN in K or V (the same
-  // in all lanes); vb, inv: LDS, V's exponents and what undoes them; k(i), v(i): the lane's 16 bytes of piece i; after_k, after_v: run
-  // when they are used up.
-  template <typename K, typename V, typename AK, typename AV>
-  __device__ __attribute__((always_inline)) inline void block(const Kv8AttnArgs& a, const Work& w, int blk, int h, unsigned kb, unsigned nan_keys, const float* vb,
-                                                              const float* inv, K k, V v, AK after_k, AV after_v) {
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64((int)kb > ref + 5 && kb != KV8_NAN) != 0, 0)) {  // (5: 1152 2^5 and 448 2^5 are below half's largest)
-      unsigned t = kb == KV8_NAN ? 1u : kb;
-      t = row_butterfly(t, [](unsigned p, unsigned q) { return p > q ? p : q; });
-      const auto r = __builtin_amdgcn_permlane16_swap(t, t, false, false);
-      ref = __builtin_amdgcn_readfirstlane(r[0] > r[1] ? r[0] : r[1]);
-      constexpr double SCALE = 1.44269504088896340736 / (HD == 128 ? 11.3137084989847603904 : HD == 64 ? 8.0 : 5.65685424949238019521);
-      const float unit = fmaxf(qs * __uint_as_float((unsigned)ref << 23), 7.8886090522101181e-31f);  // (2^-100: scores that far below 1 are zero beside anything)
-      cq = unit * (float)SCALE;
-      rest = unit * (float)(SCALE - (double)(float)SCALE);
-      start_from_m();
-    }
+  // K's scales from here on relative to `to`
+  __device__ inline void set_ref(int to) {
+    constexpr double SCALE = 1.44269504088896340736 / (HD == 128 ? 11.3137084989847603904 : HD == 64 ? 8.0 : 5.65685424949238019521);
+    // 2^-64: scores are below 2^-28 then, as good as zero; 2^125: beyond it only where no key that the query sees has a score in range, and finite, so that
+    // a position that was never written scores zero
+    const float unit = __builtin_amdgcn_fmed3f(qs * __uint_as_float((unsigned)to << 23), 0x1p-64f, 0x1p125f);
+    ref = to;
+    cq = unit * (float)SCALE;
+    rest = unit * (float)(SCALE - (double)(float)SCALE);
+    start_from_m();
+  }
+  // ref at the largest scale of the positions whose bits are set (if any); returns those of them that it suits
+  __device__ inline unsigned move_ref(unsigned kb, unsigned of, int lane) {
+    unsigned t = of >> (lane & 31) & 1u ? kb : 0u;
+    t = row_butterfly(t, [](unsigned p, unsigned q) { return p > q ? p : q; });
+    const auto r = __builtin_amdgcn_permlane16_swap(t, t, false, false);
+    const unsigned top = __builtin_amdgcn_readfirstlane(r[0] > r[1] ? r[0] : r[1]);
+    if (top) set_ref((int)top);
+    return of & (unsigned)__builtin_amdgcn_ballot_w64((int)kb + (int)REF_BELOW >= ref);
+  }
+  // s = K Q^T of a block, relative to ref (bf16: from -m on)
+  template <typename K>
+  __device__ __attribute__((always_inline)) inline f32x16 products(unsigned kb, K k, int lane) const {
     const float k_scale = __uint_as_float((unsigned)max((int)kb - ref + 127, 0) << 23);
     const f16x2 k_mul = {(f16_t)k_scale, (f16_t)k_scale}, k_add = k_mul * f16x2{(f16_t)-1152.f, (f16_t)-1152.f};
-    const f16x2 v_mul = {(f16_t)1.f, (f16_t)1.f}, v_add = {(f16_t)-1152.f, (f16_t)-1152.f};
     f32x16 s;
 #pragma unroll
     for (int i = 0; i < 16; ++i) s[i] = F32 ? 0.f : from_m[i];
@@ -170,10 +179,12 @@ struct Tile {
       const u32x4 raw = k(f >> 1);
       const f16x8 kf = halves<FMT>(raw[f % 2 * 2], raw[f % 2 * 2 + 1], k_scale, k_mul, k_add);
 #pragma unroll
-      for (int x = 0; x < TERMS; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, x ? low[f * 64 + (threadIdx.x & 63)] : qf[f], s, 0, 0, 0);
+      for (int x = 0; x < TERMS; ++x) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(kf, x ? low[f * 64 + lane] : qf[f], s, 0, 0, 0);
     }
-    after_k();
-    float p[16];  // of the lane's keys 8j + 4h + i
+    return s;
+  }
+  // log2 p' of the lane's keys 8j + 4h + i
+  __device__ __attribute__((always_inline)) inline void logits(const f32x16& s, const float* vb, int h, float (&p)[16]) const {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const f32x4 t = *(const f32x4*)&vb[8 * j + 4 * h];
@@ -183,6 +194,43 @@ struct Tile {
         p[4 * j + i] = __builtin_fmaf(s[4 * j + i], cq, F32 ? t[i] - m : t[i]);
         if (F32) p[4 * j + i] = __builtin_fmaf(s[4 * j + i], rest, p[4 * j + i]);
       }
+    }
+  }
+
+  // One block of 32 positions.  kb: K's scale byte of position lane % 32; nan_keys: bits of positions marked NaN in K or V (the same
+  // in all lanes); vb, inv: LDS, V's exponents and what undoes them; k(i), v(i): the lane's 16 bytes of piece i; after_k, after_v: run
+  // when they are used up; again_k: brings k back; kept: LDS, 16 words a lane.
+  template <typename K, typename V, typename AK, typename AV, typename RK>
+  __device__ __attribute__((always_inline)) inline void block(const Kv8AttnArgs& a, const Work& w, int blk, int h, unsigned kb, unsigned nan_keys, const float* vb,
+                                                              const float* inv, K k, V v, AK after_k, AV after_v, RK again_k, float* kept) {
+    const int lane = threadIdx.x & 63;
+    const f16x2 v_mul = {(f16_t)1.f, (f16_t)1.f}, v_add = {(f16_t)-1152.f, (f16_t)-1152.f};
+    bool again = false;  // (uniform) whether the block's keys are too far apart for one ref
+    if (__builtin_expect(__builtin_amdgcn_ballot_w64(kb - (unsigned)ref + REF_BELOW > REF_BELOW + REF_ABOVE && has_scale(kb)) != 0, 0)) {
+      const unsigned all = (unsigned)__builtin_amdgcn_ballot_w64(has_scale(kb));
+      again = move_ref(kb, all, lane) != all;
+    }
+    float p[16];
+    {
+      const f32x16 s = products(kb, k, lane);
+      after_k();
+      logits(s, vb, h, p);
+    }
+    if (__builtin_expect(again, 0)) {
+      again_k();
+      const unsigned all = (unsigned)__builtin_amdgcn_ballot_w64(has_scale(kb));
+      unsigned due = all;
+      do {
+        const unsigned now = move_ref(kb, due, lane), mine = (now | ~all) >> 4 * h;
+        logits(products(kb, k, lane), vb, h, p);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (mine >> (8 * (i >> 2) + (i & 3)) & 1u) kept[64 * i + lane] = p[i];
+        due &= ~now;
+      } while (due);
+      after_k();
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = kept[64 * i + lane];
     }
     if (__builtin_expect(nan_keys != 0, 0)) {
       asm volatile("; keys marked NaN");  // (keeps the branch: the compiler would make 48 instructions of every block out of it)
@@ -273,7 +321,7 @@ struct alignas(16) AttnLds {
 };
 
 template <typename T, int HD, int FMT>
-__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(2))) void kv8_attention_kernel(
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 2 : HD == 64 ? 3 : 4))) void kv8_attention_kernel(
     const unsigned char* __restrict__ data, int head_blocks, int n_kv, const T* __restrict__ q, int64_t q_stride, int group, int chunk, int one_rows, int one_keys,
     int one_slot, int split_out, Kv8AttnArgs a, Kv8AttnMeta meta) {
   constexpr int PIECES = HD / 32;
@@ -333,7 +381,7 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(2))) v
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     t.block(a, w, blk, h, k_now, nan_keys, L.b[wave], L.inv[wave], [&](int i) { return kr[i]; }, [&](int i) { return vr[i]; },
-            [&] { load_k(blk + NWV); }, [&] { load_v(blk + NWV); });
+            [&] { load_k(blk + NWV); }, [&] { load_v(blk + NWV); }, [&] { load_k(blk); }, &L.o[wave][0][0]);
     __builtin_amdgcn_wave_barrier();
   }
   // merge the wavefronts
