@@ -250,7 +250,8 @@ struct Tile {
     if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > limit) != 0, 0)) {  // some query's maximum moves
       mx = halves_max(mx);
       const bool up = mx > limit;
-      const float by = up ? floorf(mx) - P_TOP : 0.f, corr = !up ? 1.f : limit > 0.f ? __builtin_amdgcn_exp2f(-by) : 0.f;
+      // (a maximum of 2^24 or more is put to 1: its steps are too coarse for P_TOP, and a step more than that passes half's range)
+      const float by = up ? floorf(mx) - (fabsf(mx) < 0x1p24f ? P_TOP : 0.f) : 0.f, corr = !up ? 1.f : limit > 0.f ? __builtin_amdgcn_exp2f(-by) : 0.f;
       m += by;
       if (up) limit = P_LIMIT;
       l *= corr;

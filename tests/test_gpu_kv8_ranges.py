@@ -68,7 +68,7 @@ CASES = [(fmt, dtype) for fmt in ("e4m3", "i8") for dtype in (BF16, F32)]
 @pytest.mark.parametrize("fmt,dtype", CASES)
 @pytest.mark.parametrize("keys", [70, 3000])
 @pytest.mark.parametrize("big", [2.0 ** 30, 2.0 ** 60, 3.3e38])
-@pytest.mark.parametrize("q_size,k_size", [(1.0, 1.0), (2.0 ** 82, 2.0 ** -100), (2.0 ** -40, 2.0 ** 38)])
+@pytest.mark.parametrize("q_size,k_size", [(1.0, 1.0), (2.0 ** 82, 2.0 ** -100), (2.0 ** 82, 2.0 ** -52), (2.0 ** -40, 2.0 ** 38)])
 def test_finite_keys_that_a_row_does_not_see(device, fmt, dtype, keys, big, q_size, k_size):
     """Behind the keys, masked for all rows, and masked for all but one: no other row's outputs change."""
     g = _gen(keys, 41)
@@ -135,6 +135,21 @@ def test_keys_of_all_sizes(device, fmt, dtype, keys):
     see = rng.random((n, n)) < 0.7
     _check(device, fmt, dtype, q, k, v)
     _check(device, fmt, dtype, q, k, v, see)
+
+
+@pytest.mark.parametrize("fmt,dtype", CASES)
+@pytest.mark.parametrize("keys,at", [(3, 1), (70, 0), (70, 69), (3000, 2), (3000, 1777)])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+def test_scores_of_any_size(device, fmt, dtype, keys, at, sign):
+    """One key's score is twice the others' (half of them, where they are negative), from 2^20 to 2^100: the output is its value."""
+    g = _gen(keys, at)
+    v = torch.randn(keys, 1, 64, generator=g)
+    k = torch.full((keys, 1, 64), 0.5 if sign > 0 else -1.0)
+    k[at] = 1.0 if sign > 0 else -0.5
+    cache, _, V = _cache(device, fmt, dtype, k, v)
+    q = torch.exp2(torch.tensor([*range(17, 33), 45, 60, 77, 96]).float())[:, None, None].expand(-1, 2, 64).contiguous().to(dtype)
+    out = _np64(api.dlm_kv8_attention(cache, q.to(device), [0, len(q)], [keys]))
+    assert (np.abs(out - V[at]) <= (HALF_STEP[dtype] + 64 * U) * np.abs(V[at])).all()
 
 
 @pytest.mark.parametrize("fmt,dtype", CASES)
