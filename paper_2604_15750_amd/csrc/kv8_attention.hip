@@ -38,6 +38,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 constexpr float NEG_BIG = -3.0e38f;
 constexpr float P_LIMIT = 15.f;  // log2 of where the largest p' may go
+constexpr float P_FAR = 32.f;    // ... and from where on scores are made again: fp32's step at m is at most that of the score and 32
 constexpr unsigned REF_ABOVE = 5, REF_BELOW = 15;  // of ref: 1152 2^5 and 448 2^5 are below half's largest, 2^-9 2^-15 (e4m3's smallest code) is its smallest
 
 __device__ inline float halves_max(float v) {  // over the two lanes of a query
@@ -197,9 +198,31 @@ struct Tile {
     }
   }
 
+  // NaN for positions so marked, minus infinity for those that the query does not see
+  __device__ __attribute__((always_inline)) inline void hide(float (&p)[16], const Kv8AttnArgs& a, const Work& w, int blk, int h, unsigned nan_keys) const {
+    if (__builtin_expect(nan_keys != 0, 0)) {
+      asm volatile("; keys marked NaN");  // (keeps the branch: the compiler would make 48 instructions of every block out of it)
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (nan_keys >> (8 * (i >> 2) + 4 * h + (i & 3)) & 1u) p[i] = __uint_as_float(0x7FC00000u);
+    }
+    if (__builtin_expect(32 * blk + 32 > w.first, 0)) {  // (uniform)
+      const unsigned see = visible(a, w, blk, h);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!(see >> (8 * (i >> 2) + (i & 3)) & 1u)) p[i] = -__builtin_inff();
+    }
+  }
+  static __device__ inline float largest(const float (&p)[16]) {
+    float mx = p[0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, p[i]);
+    return mx;
+  }
+
   // One block of 32 positions.  kb: K's scale byte of position lane % 32; nan_keys: bits of positions marked NaN in K or V (the same
   // in all lanes); vb, inv: LDS, V's exponents and what undoes them; k(i), v(i): the lane's 16 bytes of piece i; after_k, after_v: run
-  // when they are used up; again_k: brings k back; kept: LDS, 16 words a lane.
+  // when they are used up; again_k: brings k back; kept: LDS, a place for the outputs.
   template <typename K, typename V, typename AK, typename AV, typename RK>
   __device__ __attribute__((always_inline)) inline void block(const Kv8AttnArgs& a, const Work& w, int blk, int h, unsigned kb, unsigned nan_keys, const float* vb,
                                                               const float* inv, K k, V v, AK after_k, AV after_v, RK again_k, float* kept) {
@@ -216,44 +239,56 @@ struct Tile {
       after_k();
       logits(s, vb, h, p);
     }
-    if (__builtin_expect(again, 0)) {
-      again_k();
-      const unsigned all = (unsigned)__builtin_amdgcn_ballot_w64(has_scale(kb));
-      unsigned due = all;
-      do {
-        const unsigned now = move_ref(kb, due, lane), mine = (now | ~all) >> 4 * h;
-        logits(products(kb, k, lane), vb, h, p);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (mine >> (8 * (i >> 2) + (i & 3)) & 1u) kept[64 * i + lane] = p[i];
-        due &= ~now;
-      } while (due);
-      after_k();
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = kept[64 * i + lane];
-    }
-    if (__builtin_expect(nan_keys != 0, 0)) {
-      asm volatile("; keys marked NaN");  // (keeps the branch: the compiler would make 48 instructions of every block out of it)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (nan_keys >> (8 * (i >> 2) + 4 * h + (i & 3)) & 1u) p[i] = __uint_as_float(0x7FC00000u);
-    }
-    if (__builtin_expect(32 * blk + 32 > w.first, 0)) {  // (uniform)
-      const unsigned see = visible(a, w, blk, h);
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (!(see >> (8 * (i >> 2) + (i & 3)) & 1u)) p[i] = -__builtin_inff();
-    }
-    float mx = p[0];
-#pragma unroll
-    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, p[i]);
-    if (__builtin_expect(__builtin_amdgcn_ballot_w64(mx > limit) != 0, 0)) {  // some query's maximum moves
+    hide(p, a, w, blk, h, nan_keys);
+    float mx = largest(p);
+    if (__builtin_expect(again || __builtin_amdgcn_ballot_w64(mx > limit) != 0, 0)) {  // some query's maximum moves
+      const float was = m;
+      const bool had = limit > 0.f;
       mx = halves_max(mx);
+      // Scores come out relative to m, with the rounding of its size: those of a maximum far above that of the blocks before are made again, from zero
+      if (__builtin_expect(again || __builtin_amdgcn_ballot_w64(had && mx > P_FAR) != 0, 0)) {
+        // (the outputs so far wait in LDS: their registers would be needed, and those that the compiler would spill are used on every block)
+#pragma unroll
+        for (int i = 0; i < 16 * PIECES; ++i) kept[64 * i + lane] = o[i >> 4][i & 15];
+        asm volatile("" ::: "memory");
+        for (bool from_zero = !again;; from_zero = true) {
+          if (from_zero) {
+            const bool far = had && mx > P_FAR;
+            if (__builtin_amdgcn_ballot_w64(far) == 0) break;
+            if (far) {
+              m = 0.f;
+              limit = -__builtin_inff();
+              start_from_m();
+            }
+          }
+          const unsigned all = (unsigned)__builtin_amdgcn_ballot_w64(has_scale(kb));
+          unsigned due = all;
+          do {
+            asm volatile("" ::: "memory");  // (nothing is loaded, or converted, in front of the loop)
+            again_k();
+            const unsigned now = move_ref(kb, due, lane), mine = (now | ~all) >> 4 * h;
+            float x[16];
+            logits(products(kb, k, lane), vb, h, x);
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (mine >> (8 * (i >> 2) + (i & 3)) & 1u) p[i] = x[i];
+            due &= ~now;
+          } while (due);
+          after_k();
+          hide(p, a, w, blk, h, nan_keys);
+          mx = halves_max(largest(p));
+          if (from_zero) break;
+        }
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int i = 0; i < 16 * PIECES; ++i) o[i >> 4][i & 15] = kept[64 * i + lane];
+      }
       const bool up = mx > limit;
       // (a maximum of 2^24 or more is put to 1: its steps are too coarse for P_TOP, and a step more than that passes half's range)
-      const float by = up ? floorf(mx) - (fabsf(mx) < 0x1p24f ? P_TOP : 0.f) : 0.f, corr = !up ? 1.f : limit > 0.f ? __builtin_amdgcn_exp2f(-by) : 0.f;
+      const float by = up ? floorf(mx) - (fabsf(mx) < 0x1p24f ? P_TOP : 0.f) : 0.f;
       m += by;
       if (up) limit = P_LIMIT;
+      const float corr = had ? __builtin_amdgcn_exp2f(was - m) : 0.f;
       l *= corr;
 #pragma unroll
       for (int d = 0; d < PIECES; ++d) o[d] *= corr;
@@ -321,8 +356,9 @@ struct alignas(16) AttnLds {
   float o[NWV][32][HD + 4];        // ... and outputs (a query's 16 bytes apart from a multiple of the banks)
 };
 
+// (wavefronts a SIMD that the registers suffice for; heads of 32 with four, their rare paths spilling: 2048 rows x 4 heads over themselves 14.2 us, 13.4 so)
 template <typename T, int HD, int FMT>
-__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 2 : HD == 64 ? 3 : 4))) void kv8_attention_kernel(
+__global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 128 ? 2 : 3))) void kv8_attention_kernel(
     const unsigned char* __restrict__ data, int head_blocks, int n_kv, const T* __restrict__ q, int64_t q_stride, int group, int chunk, int one_rows, int one_keys,
     int one_slot, int split_out, Kv8AttnArgs a, Kv8AttnMeta meta) {
   constexpr int PIECES = HD / 32;

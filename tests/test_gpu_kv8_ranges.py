@@ -105,6 +105,18 @@ def test_large_keys_without_weight(device, fmt, dtype, keys, exponent, at):
 
 
 @pytest.mark.parametrize("fmt,dtype", CASES)
+@pytest.mark.parametrize("keys,first", [(200, 128), (200, 150), (900, 512), (3000, 1024)])
+@pytest.mark.parametrize("exponent", [6, 10, 14, 17, 22, 30, 60])
+def test_a_maximum_that_comes_from_far_below(device, fmt, dtype, keys, first, exponent):
+    """Every wavefront's first blocks have scores of -2^8 to -2^62 (a running maximum of that size), the keys that have the weight come behind them."""
+    g = _gen(keys, exponent, 7)
+    k, v = torch.randn(keys, 2, 64, generator=g) * 0.4, torch.randn(keys, 2, 64, generator=g)
+    q = 0.2 + torch.rand(9, 4, 64, generator=g)
+    k[:first] = -(0.5 + torch.rand(first, 2, 64, generator=g)) * 2.0 ** exponent
+    _check(device, fmt, dtype, q, k, v)
+
+
+@pytest.mark.parametrize("fmt,dtype", CASES)
 @pytest.mark.parametrize("keys", [70, 3000])
 @pytest.mark.parametrize("exponent", [14, 26, 60])
 def test_large_keys_at_right_angles(device, fmt, dtype, keys, exponent):
