@@ -290,8 +290,9 @@ int dlm_kv8_read(const dlm_kv8_cache* c, void* k, void* v, int64_t row_stride, i
  * drafted tokens sets its ancestors' bits and its own, a causal span the bits up to its own.  A row that sees nothing (or n_keys 0)
  * gives zeros; keys and values that a row does not see do not touch it, whatever they are, NaN or infinite ones that it sees make it NaN.
  * Slots may repeat.  q is read as it is (fp32: products to 22 bits of it); its products with the keys that a row sees, element by element
- * and summed, have to be within fp32's range.  A position never written that a row sees is a key and a value of zeros (DLM_KV8_I8: up
- * to 2^-53).  out must not overlap what is read, nor the workspace anything else.
+ * and summed, have to be within fp32's range.  Where the scales of two values that it sees lie 2^B apart, the smaller one counts for nothing
+ * below a probability of 2^(B-134) of the other's (fp32: 2^(B-139); B is at most 120).  A position never written that a row sees is a key
+ * and a value of zeros (DLM_KV8_I8: up to 2^-53).  out must not overlap what is read, nor the workspace anything else.
  * workspace: DEVICE scratch at a multiple of 16, for calls that share a sequence's keys between workgroups; nothing needs more than
  * dlm_kv8_attention_workspace(rows, n_q, head_dim) bytes, and many calls need none (then it may be NULL).  It is in use until the
  * call's work is done: calls that may overlap need one each.

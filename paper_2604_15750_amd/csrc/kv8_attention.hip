@@ -15,8 +15,9 @@
 //      a score does not depend on ref, nor on any other key.  The products of a block whose keys lie further apart are made once
 //      for each range of scales in it, from codes that are loaded again (rare, and out of the way of other blocks)
 //   b  is the addend of the multiply-add that applies the softmax's scale, and the sum's addition becomes a multiply-add.  p' stays
-//      bounded whatever the scales.  b in [-60, 60] keeps l within 32 bits, and a value whose scale is 2^-B of the largest has its part
-//      in l down to a probability of 2^(B-134) of that one's (fp32 2^(B-139)): 2^-34 (2^-39) for values 2^100 apart.
+//      bounded whatever the scales.  b in [-60, 60] keeps l within 32 bits, and a value whose scale is 2^-B of the largest one's that its
+//      wavefront has met has its part in l down to a probability of 2^(B-134) of that one's (fp32 2^(B-139)): 2^-34 (2^-39) for values
+//      2^100 apart, 2^-14 (2^-19) for the 2^120 that is the most.  Where sums are rescaled and joined nothing more is lost.
 // The softmax's instructions weigh as much as the products (16 scores a lane against 512 cycles of them for 32 x 32 scores), so each
 // score costs a multiply-add, half a maximum, an exponential, a multiply-add and half a conversion: the products start from -m (bf16), and m
 // moves only where a score would leave half's range: the largest p' is brought to about 2^8 (fp32: 2^13) and may grow to 2^15 before that.
@@ -73,6 +74,10 @@ __device__ inline void store4(float* p, f32x4 v) { *(f32x4*)p = v; }
 
 // what an output is multiplied with: a row that sees nothing gives 0, one whose sum is not a positive number NaN
 __device__ inline float reciprocal(float l) { return l > 0.f ? 1.f / l : l == 0.f ? 0.f : __uint_as_float(0x7FC00000u); }
+
+// sum 2^x of a whole number x <= 0.  (A sum with V's scales undone can be far above 1, 2^68 where they are 2^-60, and count where 2^x by itself is below 32
+// bits' range; an output that small beside another does not.)
+__device__ inline float rescaled(float sum, float x) { return __builtin_amdgcn_ldexpf(sum, (int)fmaxf(x, -1000.f)); }
 
 // whether a scale byte of K is one: a position that was never written (zero beside any other) or is marked NaN is right with any ref
 __device__ inline bool has_scale(unsigned kb) { return kb - 1u < KV8_NAN - 1u; }
@@ -288,8 +293,8 @@ struct Tile {
       const float by = up ? floorf(mx) - (fabsf(mx) < 0x1p24f ? P_TOP : 0.f) : 0.f;
       m += by;
       if (up) limit = P_LIMIT;
-      const float corr = had ? __builtin_amdgcn_exp2f(was - m) : 0.f;
-      l *= corr;
+      const float down = had ? was - m : NEG_BIG, corr = __builtin_amdgcn_exp2f(down);
+      l = rescaled(l, down);
 #pragma unroll
       for (int d = 0; d < PIECES; ++d) o[d] *= corr;
 #pragma unroll
@@ -440,9 +445,9 @@ __global__ __launch_bounds__(NWV * 64) __attribute__((amdgpu_waves_per_eu(HD == 
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int v = 0; v < NWV; ++v) {
-      const float f = __builtin_amdgcn_exp2f(L.m[v][x] - M);
-      sum += f * L.l[v][x];
-      acc += *(const f32x4*)&L.o[v][x][d] * f;
+      const float down = L.m[v][x] - M;
+      sum += rescaled(L.l[v][x], down);
+      acc += *(const f32x4*)&L.o[v][x][d] * __builtin_amdgcn_exp2f(down);
     }
     put<T, HD>(a, w, split_out, w.q0 + x, d, acc, M, split_out ? sum : reciprocal(sum));
   }
@@ -460,8 +465,8 @@ __global__ __launch_bounds__(256) void kv8_attention_join_kernel(Kv8AttnArgs a, 
   const int row = (int)(at / a.n_q), b = seq_of(meta.row_off, meta.n_seqs, row);
   const int shares = max(1, ((meta.n_keys[b] + 31) / 32 + meta.chunk - 1) / meta.chunk);
   const float* ml = a.part_ml + 2 * (min(lane, shares - 1) * all + at);
-  const float top = lane < shares ? ml[0] : NEG_BIG, M = wave_max(top), w = __builtin_amdgcn_exp2f(top - M);
-  const float inv = reciprocal(wave_sum(lane < shares ? w * ml[1] : 0.f));
+  const float top = lane < shares ? ml[0] : NEG_BIG;
+  const float down = top - wave_max(top), w = __builtin_amdgcn_exp2f(down), inv = reciprocal(wave_sum(lane < shares ? rescaled(ml[1], down) : 0.f));
   vec acc = 0.f;
   for (int s0 = 0; s0 < shares; s0 += AHEAD) {
     vec v[AHEAD];

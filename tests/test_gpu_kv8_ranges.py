@@ -117,6 +117,30 @@ def test_a_maximum_that_comes_from_far_below(device, fmt, dtype, keys, first, ex
 
 
 @pytest.mark.parametrize("fmt,dtype", CASES)
+@pytest.mark.parametrize("keys", [128, 300, 3000])
+@pytest.mark.parametrize("apart", [100, 110, 120])
+@pytest.mark.parametrize("where", ["first", "second block", "last"])
+def test_small_values_that_have_the_weight_together(device, fmt, dtype, keys, apart, where):
+    """One value, 2^apart times the others, beside keys of 2^-11 of its probability each: together they have up to one and a half times its
+    weight, in its wavefront, in others and in other shares."""
+    g = _gen(keys, apart)
+    code = {"e4m3": 256.0, "i8": 64.0}[fmt]  # (the largest magnitude, to a scale of its own)
+    at = {"first": 0, "second block": 40, "last": keys - 1}[where]
+    k, v = torch.zeros(keys, 1, 64), (1 + torch.rand(keys, 1, 64, generator=g)) * code * 0.4
+    v[..., 0] = code
+    v = v * 2.0 ** -60
+    v[at] *= 2.0 ** apart
+    k[:, :, 0], k[at] = -11 * math.log(2) * 8, 0.0
+    q = torch.zeros(3, 2, 64)
+    q[..., 0] = 1.0
+    cache, K, V = _cache(device, fmt, dtype, k, v)
+    out = _np64(api.dlm_kv8_attention(cache, q.to(dtype).to(device), [0, 3], [keys]))
+    vis = np.ones((3, keys), dtype=bool)
+    want = o_kv8.attention(_np64(q), K, V, vis)
+    assert (np.abs(out - want) <= _bound(q, K, V, vis, dtype) + HALF_STEP[dtype] * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("fmt,dtype", CASES)
 @pytest.mark.parametrize("keys", [70, 3000])
 @pytest.mark.parametrize("exponent", [14, 26, 60])
 def test_large_keys_at_right_angles(device, fmt, dtype, keys, exponent):
