@@ -405,10 +405,12 @@ KV8_FORMATS = ("e4m3", "i8")
 # Calls that need no refusal go through an extension (csrc/kv8_py.cpp); what it declines (None) comes the way below it, which says what it refuses.
 @functools.lru_cache(maxsize=None)
 def _kv8_calls():
-    """The extension, bound to the library; None where it has not been built."""
+    """The extension, bound to the library; None where it has not been built, or for another torch, whose tensors it would misread."""
     try:
         from . import _kv8 as m
     except ImportError:
+        return None
+    if getattr(m, "torch_version", None) != str(torch.__version__):
         return None
     L = lib()
     m.bind(*(C.cast(f, C.c_void_p).value for f in (L.dlm_kv8_write, L.dlm_kv8_read, L.dlm_kv8_attention, L.dlm_qk_norm_rope)))

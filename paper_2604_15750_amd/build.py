@@ -1,5 +1,5 @@
-"""Compile csrc/*.hip into paper_2604_15750_amd/libdlm.so for gfx950, csrc/decisions_py.c into _decisions and csrc/kv8_py.cpp into _kv8 (in-tree,
-no torch dependency)."""
+"""Compile csrc/*.hip into paper_2604_15750_amd/libdlm.so for gfx950 and csrc/decisions_py.c into _decisions (in-tree, no torch dependency), and
+csrc/kv8_py.cpp into _kv8 where torch and its headers are there."""
 import os
 import shutil
 import subprocess
@@ -47,15 +47,18 @@ def build(verbose=False):
     return OUT
 
 
-def _compile_extension(source, out, calls, compiler="gcc", flags=()):
-    """None without the compiler or Python's headers: `calls` then go through ctypes."""
+def _compile_extension(source, out, calls, compiler="gcc", flags=(), needed=True):
+    """None without the compiler or Python's headers (or, if not `needed`, where it refuses the source): `calls` then go through ctypes."""
     cc, include = shutil.which(compiler), sysconfig.get_paths()["include"]
     if cc is None or not os.path.exists(os.path.join(include, "Python.h")):
         print(f"no {compiler} or no Python.h: {calls} are called through ctypes", file=sys.stderr)
         return None
     r = subprocess.run([cc, "-O2", "-shared", "-fPIC", "-I", include, "-o", out, os.path.join(CSRC, source), *flags], capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"{compiler} failed on {source}:\n" + r.stderr)
+        if needed:
+            raise RuntimeError(f"{compiler} failed on {source}:\n" + r.stderr)
+        print(f"{compiler} failed on {source} ({calls} are called through ctypes):\n" + r.stderr, file=sys.stderr)
+        return None
     return out
 
 
@@ -68,14 +71,20 @@ def build_extension():
 
 
 def build_kv8_extension():
-    """The same for the 8-bit cache's operators, against torch's headers: its tensors are read without a call into Python."""
-    import torch
+    """The same for the 8-bit cache's operators, against torch's headers: its tensors are read without a call into Python.  It is of use with that
+    torch alone, and names it."""
+    calls = "the 8-bit cache's operators"
     if os.path.exists(OUT_KV8):
         os.remove(OUT_KV8)
+    try:
+        import torch
+    except ImportError:
+        print(f"no torch: {calls} are called through ctypes", file=sys.stderr)
+        return None
     at = os.path.dirname(torch.__file__)
-    return _compile_extension("kv8_py.cpp", OUT_KV8, "the 8-bit cache's operators", "g++",
-                              ["-std=c++17", "-I", os.path.join(at, "include"), f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-                               "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"])
+    flags = [f'-DTORCH_BUILT_WITH="{torch.__version__}"', "-std=c++17", "-I", os.path.join(at, "include"),
+             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    return _compile_extension("kv8_py.cpp", OUT_KV8, calls, "g++", flags, needed=False)
 
 
 if __name__ == "__main__":

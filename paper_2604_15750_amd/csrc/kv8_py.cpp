@@ -5,6 +5,7 @@
 // Only calls that need no refusal are taken: tensors on the given GPU, of the types and shapes that the operator reads, with
 // contiguous rows; lists or tuples of ints that fit 32 bits, long enough and at most 32 sequences.  Anything else returns None before
 // anything is launched, and the caller goes the way through ctypes, which takes every other form and says what it refuses.
+// Tensors are read in place, as the headers of one torch lay them out: `torch_version` says which, and with another one nothing here is to be called.
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
@@ -205,4 +206,8 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_kv8", nullptr, -1, methods, nullp
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__kv8(void) { return PyModule_Create(&module); }
+PyMODINIT_FUNC PyInit__kv8(void) {
+  PyObject* m = PyModule_Create(&module);
+  if (m && PyModule_AddStringConstant(m, "torch_version", TORCH_BUILT_WITH) < 0) Py_CLEAR(m);
+  return m;
+}
