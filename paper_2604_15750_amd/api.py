@@ -187,13 +187,12 @@ def _params(pack, cls, v):
 
 # what torch.cuda.current_stream() asks, without its Stream object (0.3 us against 2.7); a private name, so the public way stays beside it
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-_get_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # (0.1 us less: whoever has a tensor on a GPU has initialised torch's side of it)
 
 
 def _stream():
     if _raw_stream is None:
         return torch.cuda.current_stream().cuda_stream
-    return _raw_stream(_get_device())
+    return _raw_stream(torch.cuda.current_device())
 
 
 _DTYPE_CODES = {torch.float32: DLM_F32, torch.bfloat16: DLM_BF16}
@@ -443,7 +442,7 @@ def _int32s(name, v, n):
 
 
 def _device():
-    return _get_device()
+    return torch.cuda.current_device()
 
 
 def _gpu_of(name, t):

@@ -32,3 +32,21 @@ def test_an_extension_of_another_torch_is_not_used(monkeypatch):
     assert load() is not None, "the extension has not been built"
     monkeypatch.setattr(torch, "__version__", "0.0.1")
     assert load() is None
+
+
+def test_calls_ask_torch_for_the_device(monkeypatch):
+    """torch initialises its side of the GPU there, and refuses a process forked from one that had: no call goes past it, whether it has a tensor or not."""
+    monkeypatch.setattr(api, "_raw_stream", lambda dev: ("stream of", dev))
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 5)
+    assert api._stream() == ("stream of", 5) and api._device() == 5
+
+    def refused():
+        raise RuntimeError("Cannot re-initialize CUDA in forked subprocess")
+
+    monkeypatch.setattr(torch.cuda, "current_device", refused)
+    x, pos = torch.zeros(4, 2, 64), torch.zeros(4, dtype=torch.int32)
+    cache = api.Kv8Cache(2, 64, 2, 64, device="cpu")
+    for call in (api.probe_mfma, lambda: api.dlm_kv8_write(cache, x, x, [0, 4], [0]), lambda: api.dlm_kv8_read(cache, [0, 4], [0], k=x, v=x),
+                 lambda: api.dlm_kv8_attention(cache, x, [0, 4], [4], out=x), lambda: api.dlm_qk_norm_rope(x[:, 0], pos, 1, 0, 64, out=x[:, 1])):
+        with pytest.raises(RuntimeError, match="forked"):
+            call()
