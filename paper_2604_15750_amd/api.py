@@ -605,6 +605,8 @@ def dlm_qk_norm_rope(x, positions, n_q, n_kv, head_dim, q_gain=None, k_gain=None
     if out is None:
         out = torch.empty((rows, width), dtype=dtype, device=x.device)
     out_stride = stride if out is x else _row_stride("out", out, dev, (None,), (dtype,))
+    if rows == 1:  # (a row has no stride: one that holds either, in multiples of 16 bytes)
+        stride = out_stride = max(columns, out.shape[1]) + 7 & ~7
     if rows >= 2**31 or min(n_q, n_kv, head_dim) < 0 or columns < width or out.shape[1] < width or out.shape[0] != rows:
         raise ValueError(f"rows of {columns} and {out.shape[1]} columns where {width} are read and written, or not as many rows of out")
     _vector("positions", positions, dev, rows, torch.int32)

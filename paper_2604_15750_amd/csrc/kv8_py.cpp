@@ -159,6 +159,7 @@ PyObject* rope(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   DECLINE_UNLESS(to_tensor(a[0], dev, &x) && to_tensor(a[1], dev, &pos) && is_float(x) && x.dims == 2 && x.shape[0] <= INT32_MAX);
   if (a[9] == a[0]) out = x;
   else DECLINE_UNLESS(to_tensor(a[9], dev, &out));
+  if (x.shape[0] == 1 && out.dims == 2) x.stride = out.stride = ((x.shape[1] > out.shape[1] ? x.shape[1] : out.shape[1]) + 7) & ~INT64_C(7);  // (a row has no stride)
   const int64_t width = ((int64_t)n_q + n_kv) * hd;
   DECLINE_UNLESS(out.dtype == x.dtype && out.dims == 2 && out.shape[0] == x.shape[0] && x.shape[1] >= width && out.shape[1] >= width);
   DECLINE_UNLESS(pos.dtype == 2 && pos.dims == 1 && pos.shape[0] == x.shape[0] && pos.stride == 1);

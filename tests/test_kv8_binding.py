@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2604_15750_amd import api, build
+from test_kv8_host import both  # noqa: F401
 
 
 @pytest.fixture
@@ -50,3 +51,29 @@ def test_calls_ask_torch_for_the_device(monkeypatch):
                  lambda: api.dlm_kv8_attention(cache, x, [0, 4], [4], out=x), lambda: api.dlm_qk_norm_rope(x[:, 0], pos, 1, 0, 64, out=x[:, 1])):
         with pytest.raises(RuntimeError, match="forked"):
             call()
+
+
+@pytest.mark.parametrize("rows", [1, 2])
+def test_views_of_one_row_are_taken_as_those_of_several(both, rows):
+    """A row has no stride: in place into fewer columns, or from a number of columns that is no multiple of 16 bytes, is the same call for any number of rows."""
+    wide = torch.zeros(rows, 408)
+    pos = torch.zeros(rows, dtype=torch.int32)
+    for x, out in ((wide[:, :400], wide[:, :192]), (wide[:, :193], wide[:, :400]), (wide[:, :401], torch.zeros(rows, 200)[:, :195]), (wide, wide)):
+        a, b = both(lambda: api.dlm_qk_norm_rope(x, pos, 2, 1, 64, out=out))
+        assert a == b and both.taken
+        x_stride, out_stride = a[0][1], a[0][13]
+        assert x_stride % 4 == 0 and out_stride % 4 == 0 and x_stride >= 192 and out_stride >= 192
+        assert x_stride == out_stride or x.data_ptr() != out.data_ptr()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_one_row_in_place(device, dtype):
+    wide = torch.randn(2, 408, device=device).to(dtype)
+    pos = torch.tensor([7, 7], dtype=torch.int32, device=device)
+    gain = torch.full((64,), 1.5, device=device).to(dtype)
+    want = api.dlm_qk_norm_rope(wide[:, :193], pos, 2, 1, 64, gain, gain)
+    for rows in (2, 1):
+        x = wide.clone()
+        api.dlm_qk_norm_rope(x[:rows, :401], pos[:rows], 2, 1, 64, gain, gain, out=x[:rows, :193])
+        assert torch.equal(x[:rows, :192], want[:rows]) and torch.equal(x[:rows, 192:], wide[:rows, 192:]) and torch.equal(x[rows:], wide[rows:])
