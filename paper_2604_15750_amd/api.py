@@ -494,7 +494,7 @@ class Kv8Cache:
     format: "e4m3" or "i8"."""
 
     def __init__(self, slots, max_len, n_kv, head_dim, format="e4m3", device="cuda"):
-        n = lib().dlm_kv8_bytes(slots, max_len, n_kv, head_dim) if max(slots, max_len, n_kv, head_dim) < 2**31 else 0
+        n = lib().dlm_kv8_bytes(slots, max_len, n_kv, head_dim) if all(0 < x < 2**31 for x in (slots, max_len, n_kv, head_dim)) else 0
         if n == 0:
             raise DlmError(-2, f"a cache of {slots} slots x {max_len} positions x {n_kv} heads of {head_dim}")
         self.slots, self.max_len, self.n_kv, self.head_dim, self.format = slots, max_len, n_kv, head_dim, format

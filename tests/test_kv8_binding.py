@@ -77,3 +77,10 @@ def test_one_row_in_place(device, dtype):
         x = wide.clone()
         api.dlm_qk_norm_rope(x[:rows, :401], pos[:rows], 2, 1, 64, gain, gain, out=x[:rows, :193])
         assert torch.equal(x[:rows, :192], want[:rows]) and torch.equal(x[:rows, 192:], wide[:rows, 192:]) and torch.equal(x[rows:], wide[rows:])
+
+
+def test_sizes_below_32_bits():
+    """They would arrive at the library as their low 32 bits."""
+    for bad in ((1 - 2**32, 64, 2, 64), (1, 64 - 2**32, 2, 64), (1, 64, 2 - 2**32, 64), (1, 64, 2, 64 - 2**32), (-1, 64, 2, 64)):
+        with pytest.raises(api.DlmError, match="ESHAPE"):
+            api.Kv8Cache(*bad, device="cpu")
