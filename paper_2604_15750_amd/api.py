@@ -556,7 +556,8 @@ def dlm_kv8_attention(cache, q, row_offsets, n_keys, slot=None, mask=None, out=N
     dlm_kv8_attention_workspace bytes that nothing else uses meanwhile (None: a new one); the rest: host int lists.  Returns out."""
     ext = _kv8_calls()
     if ext is not None and out is not None:
-        size = 0 if workspace is None or not workspace.is_contiguous() else workspace.numel() * workspace.element_size()
+        # (-1: not for the extension)
+        size = 0 if workspace is None else workspace.numel() * workspace.element_size() if workspace.is_contiguous() else -1
         if _taken(ext.attention(cache._ref, cache._data, q, row_offsets, n_keys, slot, mask, out, workspace, size, _device(), _stream())):
             return out
     n, dev = len(n_keys), _gpu_of("q", q)

@@ -84,3 +84,11 @@ def test_sizes_below_32_bits():
     for bad in ((1 - 2**32, 64, 2, 64), (1, 64 - 2**32, 2, 64), (1, 64, 2 - 2**32, 64), (1, 64, 2, 64 - 2**32), (-1, 64, 2, 64)):
         with pytest.raises(api.DlmError, match="ESHAPE"):
             api.Kv8Cache(*bad, device="cpu")
+
+
+def test_a_workspace_that_is_not_contiguous_is_refused_either_way(both):
+    cache = api.Kv8Cache(2, 64, 2, 64, device="cpu")
+    q, out = torch.zeros(6, 4, 64), torch.zeros(6, 4, 64)
+    for ws, ok in ((torch.zeros(64, dtype=torch.uint8), True), (torch.zeros(128, dtype=torch.uint8)[::2], False), (torch.zeros(16, 4).t(), False)):
+        a, b = both(lambda: api.dlm_kv8_attention(cache, q, [0, 6], [9], out=out, workspace=ws))
+        assert a == b and both.taken == ok and (a is ValueError) != ok
