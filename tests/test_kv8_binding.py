@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from paper_2604_15750_amd import api, build
-from test_kv8_host import both  # noqa: F401
+from test_kv8_host import both, cpu_cache  # noqa: F401
 
 
 @pytest.fixture
@@ -86,9 +86,8 @@ def test_sizes_below_32_bits():
             api.Kv8Cache(*bad, device="cpu")
 
 
-def test_a_workspace_that_is_not_contiguous_is_refused_either_way(both):
-    cache = api.Kv8Cache(2, 64, 2, 64, device="cpu")
+def test_a_workspace_that_is_not_contiguous_is_refused_either_way(both, cpu_cache):
     q, out = torch.zeros(6, 4, 64), torch.zeros(6, 4, 64)
     for ws, ok in ((torch.zeros(64, dtype=torch.uint8), True), (torch.zeros(128, dtype=torch.uint8)[::2], False), (torch.zeros(16, 4).t(), False)):
-        a, b = both(lambda: api.dlm_kv8_attention(cache, q, [0, 6], [9], out=out, workspace=ws))
+        a, b = both(lambda: api.dlm_kv8_attention(cpu_cache, q, [0, 6], [9], out=out, workspace=ws))
         assert a == b and both.taken == ok and (a is ValueError) != ok
