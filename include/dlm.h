@@ -254,10 +254,11 @@ int dlm_attention(const void* q, const void* k, const void* v, void* out, int A,
  * count may be 0; what lies behind them is neither read nor written).  Per head:
  *   y = x * rsqrt(mean(x^2) + eps) * gain          (q_gain / k_gain DEVICE [head_dim] of dtype; NULL: y = x)
  *   out_i = y_i cos a - y_j sin a, out_j = y_j cos a + y_i sin a,   j = i + head_dim/2, a = position * theta^(-2 i / head_dim)
- * positions DEVICE [rows], any int32; the angle is computed in 64 bits, sums are fp32, values are rounded once.  out may be x (with
- * the same stride); else the two must not overlap (columns of one matrix do not; with different strides, from the first row to the
- * last).  Errors: DLM_EINVAL (null pointer, alignment, stride shorter than a row, overlap, eps or theta not positive and finite, bad
- * dtype), DLM_ESHAPE (rows < 0, heads, head_dim), DLM_ECAPACITY (more than 67108860 rows), DLM_EHIP. */
+ * positions DEVICE [rows], any int32; the angle is computed in 64 bits, sums are fp32 (the squares of a head that is normalised have to
+ * sum within its range), values are rounded once.  out may be x (with the same stride); else the two must not overlap (columns of one
+ * matrix do not; with different strides, from the first row to the last).  Errors: DLM_EINVAL (null pointer, alignment, stride shorter
+ * than a row, overlap, eps or theta not positive and finite, bad dtype), DLM_ESHAPE (rows < 0, heads, head_dim), DLM_ECAPACITY (more than
+ * 67108860 rows), DLM_EHIP. */
 int dlm_qk_norm_rope(const void* x, int64_t x_stride, int rows, int n_q, int n_kv, int head_dim, int dtype, const void* q_gain,
                      const void* k_gain, float eps, float theta, const int32_t* positions, void* out, int64_t out_stride, void* stream);
 
@@ -289,10 +290,11 @@ int dlm_kv8_read(const dlm_kv8_cache* c, void* k, void* v, int64_t row_stride, i
  * before them and position n_keys[b] - nr + j where bit j % 32 of word j / 32 of its mask is set (32 mask_words >= nr): a tree of
  * drafted tokens sets its ancestors' bits and its own, a causal span the bits up to its own.  A row that sees nothing (or n_keys 0)
  * gives zeros; keys and values that a row does not see do not touch it, whatever they are, NaN or infinite ones that it sees make it NaN.
- * Slots may repeat.  q is read as it is (fp32: products to 22 bits of it); its products with the keys that a row sees, element by element
- * and summed, have to be within fp32's range.  Where the scales of two values that it sees lie 2^B apart, the smaller one counts for nothing
- * below a probability of 2^(B-134) of the other's (fp32: 2^(B-139); B is at most 120).  A position never written that a row sees is a key
- * and a value of zeros (DLM_KV8_I8: up to 2^-53).  out must not overlap what is read, nor the workspace anything else.
+ * Slots may repeat.  q is read as it is (fp32: products to 22 bits of it), probabilities multiply values with 11 bits (fp32: 22), their
+ * sum is fp32.  The products of q with the keys that a row sees, element by element and summed, have to be within fp32's range.  Where the
+ * scales of two values that it sees lie 2^B apart (at most 2^120), the smaller one counts for nothing below a probability of 2^(B-134) of
+ * the other's (fp32: 2^(B-139)).  A position never written that a row sees is a key and a value of zeros (DLM_KV8_I8: up to 2^-53).  out
+ * must not overlap what is read, nor the workspace anything else.
  * workspace: DEVICE scratch at a multiple of 16, for calls that share a sequence's keys between workgroups; nothing needs more than
  * dlm_kv8_attention_workspace(rows, n_q, head_dim) bytes, and many calls need none (then it may be NULL).  It is in use until the
  * call's work is done: calls that may overlap need one each.

@@ -1,6 +1,6 @@
 // Python calls of the 8-bit cache's operators (dlm_kv8_write, dlm_kv8_read, dlm_kv8_attention, dlm_qk_norm_rope of dlm.h) without ctypes.
 // Their kernels take a few microseconds at the row counts of a decode, so a call is bound by what checking and marshalling its
-// arguments costs the host: dlm_qk_norm_rope of 8 rows 7.2 us a call through ctypes, 3.8 here, of which the launch has 3 (5.0 with the
+// arguments costs the host: dlm_qk_norm_rope of 8 rows 7.2 us a call through ctypes, 4.0 here, of which the launch has 3 (1.2 more with the
 // tensors' properties asked for through Python instead of torch's headers).
 // Only calls that need no refusal are taken: tensors on the given GPU, of the types and shapes that the operator reads, with
 // contiguous rows; lists or tuples of ints that fit 32 bits, long enough and at most 32 sequences.  Anything else returns None before
