@@ -294,7 +294,8 @@ struct Tile {
       }
       const bool up = mx > limit;
       // (a maximum of 2^24 or more is put to 1: its steps are too coarse for P_TOP, and a step more than that passes half's range)
-      const float by = up ? floorf(mx) - (fabsf(mx) < 0x1p24f ? P_TOP : 0.f) : 0.f;
+      float by = up ? floorf(mx) - (fabsf(mx) < 0x1p24f ? P_TOP : 0.f) : 0.f;
+      if (had) by = fmaxf(by, was - m);  // (m never falls: made again, a score of many digits can turn out below the old maximum)
       m += by;
       if (up) limit = P_LIMIT;
       const float down = had ? was - m : NEG_BIG, corr = __builtin_amdgcn_exp2f(down);

@@ -189,6 +189,24 @@ def test_scores_of_any_size(device, fmt, dtype, keys, at, sign):
 
 
 @pytest.mark.parametrize("fmt,dtype", CASES)
+@pytest.mark.parametrize("keys", [300, 3000])
+@pytest.mark.parametrize("value", [-60, 0, 60])
+def test_large_scores_next_to_each_other(device, fmt, dtype, keys, value):
+    """Scores of 2^20 to 2^60 that differ by no more than their own digits tell: any of the keys may have the weight, and all have one value."""
+    g = _gen(keys, value + 100)
+    k = torch.randn(keys, 1, 64, generator=g)
+    k[..., 0] = 4.0
+    v = torch.full((keys, 1, 64), {"e4m3": 256.0, "i8": 64.0}[fmt] * 2.0 ** value)
+    q = torch.randn(20, 2, 64, generator=g)
+    size = torch.exp2(torch.arange(20, 60, 2).float())[:, None]
+    q[..., 0] = size
+    q[..., 1:] *= 2.0 ** -20 * size[..., None]
+    cache, _, V = _cache(device, fmt, dtype, k, v)
+    out = _np64(api.dlm_kv8_attention(cache, q.to(dtype).to(device), [0, 20], [keys]))
+    assert (np.abs(out - V[0, 0, 0]) <= (HALF_STEP[dtype] + (2 * keys + 64) * U) * V[0, 0, 0]).all()
+
+
+@pytest.mark.parametrize("fmt,dtype", CASES)
 def test_positions_never_written_behind_a_key_that_another_row_sees(device, fmt, dtype):
     """Queries beside whose size that key's scale has no place in 32 bits."""
     g = _gen(17)
