@@ -21,9 +21,9 @@
 // The softmax's instructions weigh as much as the products (16 scores a lane against 512 cycles of them for 32 x 32 scores), so each
 // score costs a multiply-add, half a maximum, an exponential, a multiply-add and half a conversion: the products start from -m (bf16), and m
 // moves only where a score would leave half's range: the largest p' is brought to about 2^8 (fp32: 2^13) and may grow to 2^15 before that.
-// What bounds it: 1280 rows x 32 heads of 128 over themselves 42 to 45 us, 0.62 PFLOP/s (fp32 68 to 70), 4096 rows 320 to 330 us, 0.85 (a large half
+// What bounds it: 1280 rows x 32 heads of 128 over themselves 40 to 45 us, 0.6 to 0.67 PFLOP/s (fp32 68 to 70), 4096 rows 320 to 330 us, 0.85 (a large half
 // product reaches 1.12 to 1.22): vector instructions and products in turn.  155 instructions a block of 32 keys on the straight path beside 16 products,
-// 187 at 4096 rows and 248 at 1280 with what is done once a wavefront: at 4096 the products have 41 % of the cycles and they 60 %, at 1280 29 and 56, and the
+// 187 at 4096 rows and 249 at 1280 with what is done once a wavefront: at 4096 the products have 41 % of the cycles and they 60 %, at 1280 29 and 56, and the
 // rest is the chip's last round.  Single tokens of 24 sequences of up to 8192 keys, 28 of 4 heads: 30.6 us, 5 TB/s of cache.  Few rows: latency,
 // 8 rows x 32 heads of 392 keys 6.6 us.
 // The rare paths (scales too far apart, a maximum from far below) cost the others 0 to 3 %: 1280 rows 44.1 us without them, 45.6 with; 24 single tokens 35.0,
