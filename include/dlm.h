@@ -306,6 +306,49 @@ int dlm_kv8_attention(const dlm_kv8_cache* c, const void* q, int64_t q_stride, v
                       const int32_t* n_keys, const int32_t* slot, int n_seqs, const uint32_t* mask, int mask_words, void* workspace,
                       size_t workspace_bytes, void* stream);
 
+/* ---- linear layers in 8-bit integers -----------------------------------------------------------------
+ * For callers that run layers of their own around this library: activations quantised by row, weights by output channel, and products
+ * of the two on the 8-bit matrix cores, at half of bf16's weight bytes and twice its matrix rate.
+ * A row is held as codes, integers q in [-127, 127], and an fp32 scale s, and stands for s q.  Rows are row-major with a stride in elements
+ * (codes: bytes), so that they can be columns of a wider matrix; DEVICE pointers are 16-byte aligned (scales: 4) and strides multiples of 16
+ * bytes (DLM_EINVAL otherwise).  Rows of codes that are read own their bytes up to the next multiple of 16: what those hold does not matter, but
+ * they have to be readable.  dtypes DLM_F32 or DLM_BF16.  None of the calls allocates or synchronises: all can be captured into a graph. */
+
+/* A row t is quantised as q = 127 t / max|t| rounded to the nearest integer (ties to even, of the exact quotient), s = max|t| / 127; a row of
+ * zeros has q = 0 and s = 0.  A row with a NaN or an infinity has q = 0 and s = NaN, so that what is computed from it is NaN.
+ * dlm_q8_rows: t = x [rows, width].
+ * dlm_add_norm_q8: h = residual + x, rounded once to h_dtype and written to h [rows, width]; y = h rsqrt(mean(h^2) + eps) gain is what is
+ * quantised: t = h gain, rounded to fp32 (bf16: exact) gives the codes, and s = max|t| rsqrt(mean(h^2) + eps) / 127.  residual and h are of h_dtype, DLM_F32
+ * or x's; both NULL: h = x.  gain DEVICE [width] of dtype.  The squares are summed in fp32: a row whose sum is past its range counts as one with an infinity.  h may be
+ * residual or x (with the same stride and type); nothing else that is written may overlap anything.
+ * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, eps not positive and finite, bad dtype), DLM_ESHAPE (rows < 0, width not in
+ * 1 .. 1048576), DLM_ECAPACITY (more than 4194303 rows), DLM_EHIP. */
+int dlm_q8_rows(const void* x, int64_t x_stride, int rows, int width, int dtype, int8_t* codes, int64_t codes_stride, float* scale, void* stream);
+int dlm_add_norm_q8(const void* x, int64_t x_stride, int rows, int width, int dtype, const void* residual, int64_t residual_stride, void* h,
+                    int64_t h_stride, int h_dtype, const void* gain, float eps, int8_t* codes, int64_t codes_stride, float* scale, void* stream);
+
+/* A weight of n output channels by k inputs in caller-owned DEVICE memory of dlm_q8_weight_bytes(...) bytes (0: an unsupported shape: n not in
+ * 1 .. 16777216, k not in 1 .. 131071, gated and n odd, more than 32 GiB) at a multiple of 16, in the order in which the matrix cores take it; dlm_q8_weight_pack
+ * writes it from row-major codes [n, k] (any int8, -128 too) and their scales [n].  gated = 1: the channels are n / 2 gate channels and then n / 2
+ * up channels (as w_gate_up), 0: the outputs themselves.  Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, gated), DLM_ESHAPE, DLM_EHIP. */
+typedef struct {
+  int32_t n, k, gated;
+  void* data; /* DEVICE */
+} dlm_q8_weight;
+size_t dlm_q8_weight_bytes(int n, int k, int gated);
+int dlm_q8_weight_pack(const dlm_q8_weight* w, const int8_t* codes, int64_t codes_stride, const float* scale, void* stream);
+
+/* out [rows, n] = x_scale[m] scale[j] sum_k x[m][k] codes[j][k]: the sum exact, converted to fp32 and multiplied by the row's and then the channel's
+ * scale.  gated: out [rows, n / 2] = g / (1 + exp(-g)) u of the gate's and the up channel's values.  Rounded once to out_dtype; columns behind
+ * the outputs are left as they are.  x [rows, k] codes (any int8) and x_scale [rows]; nothing may overlap out.
+ * workspace: DEVICE scratch at a multiple of 16 of dlm_q8_gemm_workspace(r, n, k, gated) bytes for some r >= rows (0: none is needed, it may be NULL),
+ * zero-filled before its first use; a call leaves zeros where the next one needs them.  It is in use until the call's work is done: calls that may overlap need one each.
+ * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, bad dtype, gated), DLM_ESHAPE (weight, rows < 0), DLM_ECAPACITY (workspace too small,
+ * more than 1048576 rows), DLM_EHIP. */
+size_t dlm_q8_gemm_workspace(int rows, int n, int k, int gated);
+int dlm_q8_gemm(const dlm_q8_weight* w, const int8_t* x, int64_t x_stride, const float* x_scale, int rows, void* out, int64_t out_stride, int out_dtype,
+                void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- what the GPU achieves on the resources the rooflines are drawn against -------------------
  * For callers that report measurements (bench.py): kernels that do nothing but the one thing, timed
  * with events on `stream`, which is synchronised before the call returns.

@@ -28,4 +28,5 @@ Parity status of each function against something other than itself
                                          authors' behaviour
   kv8 (8-bit cache and its operators)    pinned (the formats' codes against torch's e4m3, quantisation by brute force, midpoints,
                                          attention and masks by closed forms)
+  q8 (8-bit integer linear layers)       pinned (codes by exact fractions, the norm by scaling, products by triple loops)
 """

@@ -38,6 +38,10 @@ class dlm_weights(C.Structure):
                 ("norm2", C.POINTER(C.c_void_p)), ("final_norm", C.c_void_p), ("lm_head", C.c_void_p)]
 
 
+class dlm_q8_weight(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n", "k", "gated")] + [("data", C.c_void_p)]
+
+
 class dlm_kv8_cache(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_slots", "max_len", "n_kv", "head_dim", "format")] + [("data", C.c_void_p)]
 
@@ -64,7 +68,8 @@ EXPORTS = ["dlm_last_error", "dlm_model_create", "dlm_model_destroy", "dlm_state
            "dlm_gemm_nt", "dlm_attention", "dlm_profile_enable", "dlm_profile_read", "dlm_probe_hbm_read", "dlm_probe_mfma",
            "dlm_state_fuse_stats", "dlm_vocab_stats_static", "dlm_plan_attention",
            "dlm_plan_vocab_stats", "dlm_plan_gemm", "dlm_qk_norm_rope", "dlm_kv8_bytes", "dlm_kv8_write", "dlm_kv8_read",
-           "dlm_kv8_attention_workspace", "dlm_kv8_attention"]
+           "dlm_kv8_attention_workspace", "dlm_kv8_attention", "dlm_q8_rows", "dlm_add_norm_q8", "dlm_q8_weight_bytes",
+           "dlm_q8_weight_pack", "dlm_q8_gemm_workspace", "dlm_q8_gemm"]
 
 
 def lib():
@@ -112,6 +117,15 @@ def lib():
         L.dlm_kv8_attention_workspace.restype = C.c_size_t
         L.dlm_kv8_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_int, C.c_int] + [C.c_void_p] * 3 + \
                                        [C.c_int, C.c_void_p, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.dlm_q8_rows.argtypes = [C.c_void_p, C.c_int64] + [C.c_int] * 3 + [C.c_void_p, C.c_int64] + [C.c_void_p] * 2
+        L.dlm_add_norm_q8.argtypes = [C.c_void_p, C.c_int64] + [C.c_int] * 3 + [C.c_void_p, C.c_int64] * 2 + [C.c_int, C.c_void_p, C.c_float, C.c_void_p, C.c_int64] + \
+                                     [C.c_void_p] * 2
+        L.dlm_q8_weight_bytes.argtypes = [C.c_int] * 3
+        L.dlm_q8_weight_bytes.restype = C.c_size_t
+        L.dlm_q8_weight_pack.argtypes = [C.c_void_p] * 2 + [C.c_int64] + [C.c_void_p] * 2
+        L.dlm_q8_gemm_workspace.argtypes = [C.c_int] * 4
+        L.dlm_q8_gemm_workspace.restype = C.c_size_t
+        L.dlm_q8_gemm.argtypes = [C.c_void_p] * 2 + [C.c_int64, C.c_void_p, C.c_int, C.c_void_p, C.c_int64, C.c_int, C.c_void_p, C.c_size_t, C.c_void_p]
         _lib = L
     return _lib
 
@@ -619,6 +633,150 @@ def dlm_qk_norm_rope(x, positions, n_q, n_kv, head_dim, q_gain=None, k_gain=None
         return out
     _check(lib().dlm_qk_norm_rope(x.data_ptr(), stride, rows, n_q, n_kv, head_dim, _DTYPE_CODES[x.dtype], _ptr(q_gain), _ptr(k_gain), eps, theta,
                                   positions.data_ptr(), out.data_ptr(), out_stride, _stream()))
+    return out
+
+
+# ---- linear layers in 8-bit integers (include/dlm.h) ---------------------------------------------------------------------------------
+
+def _matrix(name, t, dev, rows, width, dtypes):
+    """The stride between the rows of [rows, width] (None: any); a single row, which has none, gets one that holds it in multiples of 16 bytes."""
+    stride = _row_stride(name, t, dev, (width,), dtypes)
+    if rows is not None and t.shape[0] != rows:
+        raise ValueError(f"{name}: {t.shape[0]} rows where {rows} are read")
+    if t.shape[0] == 1:
+        step = 16 // t.element_size()
+        stride = -(-t.shape[1] // step) * step
+    return stride
+
+
+def _new_rows(rows, width, dtype, device):
+    """New rows at a stride of a multiple of 16 bytes."""
+    step = 16 // dtype.itemsize
+    return torch.empty((rows, -(-width // step) * step), dtype=dtype, device=device)[:, :width]
+
+
+def _codes(name, t, dev, rows, width):
+    """As _matrix, of codes that are read: their rows' bytes up to a multiple of 16 have to be the tensor's memory."""
+    stride = _matrix(name, t, dev, rows, width, (torch.int8,))
+    width = t.shape[1]
+    if width % 16 and t.shape[0]:
+        if t.untyped_storage().nbytes() < t.storage_offset() + (t.shape[0] - 1) * stride + -(-width // 16) * 16:
+            raise ValueError(f"{name}: the last row's bytes up to a multiple of 16 are not the tensor's memory")
+    return stride
+
+
+def _code_outputs(x, dev, codes, scale):
+    rows, width = x.shape
+    if codes is None:
+        codes = _new_rows(rows, width, torch.int8, x.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    stride = _matrix("codes", codes, dev, rows, width, (torch.int8,))
+    _vector("scale", scale, dev, rows, torch.float32)
+    return codes, stride, scale
+
+
+def dlm_q8_rows(x, codes=None, scale=None):
+    """Rows in 8-bit integers: x: device tensor [rows, width] (rows may be strided); codes: int8 [rows, width], scale: fp32 [rows] (None: new ones).
+    Returns (codes, scale)."""
+    dev = _gpu_of("x", x)
+    stride = _matrix("x", x, dev, None, None, _FLOATS)
+    codes, code_stride, scale = _code_outputs(x, dev, codes, scale)
+    rows, width = x.shape
+    if rows and max(rows, width) < 2**31:
+        _check(lib().dlm_q8_rows(x.data_ptr(), stride, rows, width, _DTYPE_CODES[x.dtype], codes.data_ptr(), code_stride, scale.data_ptr(), _stream()))
+    elif rows:
+        raise ValueError(f"x: {rows} rows of {width}")
+    return codes, scale
+
+
+def dlm_add_norm_q8(x, gain, residual=None, h=None, eps=1e-5, codes=None, scale=None):
+    """The residual's addition, RMSNorm and the rows in 8-bit integers: x: device tensor [rows, width]; gain: [width] of x's dtype; residual: [rows,
+    width] of x's dtype or fp32, or None (no addition); h: residual + x, of the residual's dtype (None: a new tensor; the residual or x itself: in place);
+    codes, scale: as dlm_q8_rows.  Returns (codes, scale, h); h is x where there is no residual."""
+    dev = _gpu_of("x", x)
+    stride = _matrix("x", x, dev, None, None, _FLOATS)
+    rows, width = x.shape
+    _vector("gain", gain, dev, width, x.dtype)
+    r_stride = h_stride = h_code = 0
+    if residual is not None:
+        r_stride = _matrix("residual", residual, dev, rows, width, (torch.float32, x.dtype))
+        if h is None:
+            h = _new_rows(rows, width, residual.dtype, x.device)
+        h_stride = _matrix("h", h, dev, rows, width, (residual.dtype,))
+        h_code = _DTYPE_CODES[residual.dtype]
+    elif h is not None:
+        raise ValueError("h is given without a residual")
+    codes, code_stride, scale = _code_outputs(x, dev, codes, scale)
+    if rows and max(rows, width) < 2**31:
+        _check(lib().dlm_add_norm_q8(x.data_ptr(), stride, rows, width, _DTYPE_CODES[x.dtype], _ptr(residual), r_stride, _ptr(h), h_stride, h_code, gain.data_ptr(), eps,
+                                     codes.data_ptr(), code_stride, scale.data_ptr(), _stream()))
+    elif rows:
+        raise ValueError(f"x: {rows} rows of {width}")
+    return codes, scale, x if residual is None else h
+
+
+class Q8Weight:
+    """A weight in 8-bit integers (dlm_q8_weight) with its memory, packed from codes (int8 [n, k]) and scales (fp32 [n]), one per output channel.  gated: the
+    first n / 2 channels are the gate's, the others the up channels, and a product with it has n / 2 outputs."""
+
+    def __init__(self, codes, scale, gated=False):
+        dev = _gpu_of("codes", codes)
+        stride = _codes("codes", codes, dev, None, None)
+        self.n, self.k = codes.shape
+        self.gated = bool(gated)
+        size = lib().dlm_q8_weight_bytes(self.n, self.k, int(self.gated)) if max(self.n, self.k) < 2**31 else 0
+        if size == 0:
+            raise DlmError(-2, f"a weight of {self.n} x {self.k}" + (", gated" if gated else ""))
+        _vector("scale", scale, dev, self.n, torch.float32)
+        self._data = torch.empty(size, dtype=torch.uint8, device=codes.device)
+        self._desc = dlm_q8_weight(self.n, self.k, int(self.gated), self._data.data_ptr())
+        self._ref = C.addressof(self._desc)
+        _check(lib().dlm_q8_weight_pack(self._ref, codes.data_ptr(), stride, scale.data_ptr(), _stream()))
+
+    @classmethod
+    def quantise(cls, weight, gated=False):
+        """Of a weight [n, k] in fp32 or bf16, each channel quantised as dlm_q8_rows does."""
+        return cls(*dlm_q8_rows(weight), gated=gated)
+
+    @property
+    def outputs(self):
+        return self.n // 2 if self.gated else self.n
+
+    @property
+    def data(self):
+        """The memory (one address for life)."""
+        return self._data
+
+    def workspace(self, rows):
+        """A new workspace for products of up to `rows` rows, or None where they need none."""
+        size = lib().dlm_q8_gemm_workspace(rows, self.n, self.k, int(self.gated)) if 0 < rows < 2**31 else 0
+        return torch.zeros(size, dtype=torch.uint8, device=self._data.device) if size else None
+
+
+def dlm_q8_gemm(weight, x, x_scale, out=None, dtype=torch.bfloat16, workspace=None):
+    """The product of rows of codes (int8 [rows, k], scales fp32 [rows]) with a Q8Weight: into out [rows, weight.outputs] (fp32 or bf16; rows may be strided), or
+    into a new tensor of `dtype`; workspace: one of weight.workspace(as many rows or more) that nothing else uses meanwhile (None: a new one).  Returns out."""
+    dev = _gpu_of("x", x)
+    stride = _codes("x", x, dev, None, weight.k)
+    rows = x.shape[0]
+    _vector("x_scale", x_scale, dev, rows, torch.float32)
+    if out is None:
+        out = _new_rows(rows, weight.outputs, dtype, x.device)
+    out_stride = _matrix("out", out, dev, rows, weight.outputs, _FLOATS)
+    _on_gpu("weight", weight._data, dev)
+    if rows >= 2**31:
+        raise ValueError(f"x: {rows} rows")
+    if rows == 0:
+        return out
+    if workspace is None:
+        workspace = weight.workspace(rows)
+    else:
+        _on_gpu("workspace", workspace, dev)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace is not contiguous")
+    size = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().dlm_q8_gemm(weight._ref, x.data_ptr(), stride, x_scale.data_ptr(), rows, out.data_ptr(), out_stride, _DTYPE_CODES[out.dtype], _ptr(workspace), size, _stream()))
     return out
 
 

@@ -1,37 +1,12 @@
 // C ABI of the 8-bit KV cache and what feeds and reads it: argument validation and packing.  No kernel code here.
 #include <cstring>
 
+#include "abi_args.h"
 #include "kv8.h"
 
 namespace {
 
-bool known_dtype(int dtype) { return dtype == DLM_F32 || dtype == DLM_BF16; }
-int64_t elem_bytes(int dtype) { return dtype == DLM_BF16 ? 2 : 4; }
 bool known_head(int hd) { return hd == 32 || hd == 64 || hd == 128; }
-bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
-// rows [rows, width] at `stride` elements: the stride holds a row and keeps 16-byte alignment
-bool good_stride(int64_t stride, int64_t width, int dtype) { return stride >= width && stride <= INT64_C(1) << 40 && stride * elem_bytes(dtype) % 16 == 0; }
-typedef __int128 wide;  // (rows x strides do not fit 64 bits)
-bool overlap(const void* a, wide a_bytes, const void* b, wide b_bytes) {
-  return a_bytes && b_bytes && (wide)(uintptr_t)a < (wide)(uintptr_t)b + b_bytes && (wide)(uintptr_t)b < (wide)(uintptr_t)a + a_bytes;
-}
-// [rows, width] at `stride`: what lies between its first and its last byte
-struct Rows {
-  const void* p;
-  int64_t rows, stride, width;  // bytes
-  Rows(const void* at, int64_t n, int64_t stride_elems, int64_t width_elems, int dtype)
-      : p(at), rows(n), stride(stride_elems * elem_bytes(dtype)), width(width_elems * elem_bytes(dtype)) {}
-  wide span() const { return rows ? (wide)(rows - 1) * stride + width : 0; }
-};
-// whether two such arrays share a byte: columns of one matrix need not; of different strides: whether their spans do
-bool overlap(const Rows& a, const Rows& b) {
-  if (a.stride != b.stride || a.rows != b.rows || a.width != b.width) return overlap(a.p, a.span(), b.p, b.span());
-  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p, d = x > y ? x - y : y - x;
-  const int64_t r = (int64_t)(d % (uintptr_t)a.stride);
-  const uintptr_t n = d / (uintptr_t)a.stride;
-  return (n < (uintptr_t)a.rows && r < a.width) || (n + 1 < (uintptr_t)a.rows && a.stride - r < a.width);
-}
-constexpr int MAX_GRID = (1 << 24) - 1;  // workgroups of 256 in a dimension of a launch
 
 // bytes of a (slot, kv head), 0 for an unsupported shape
 int64_t head_bytes(int n_slots, int max_len, int n_kv, int hd) {

@@ -1,0 +1,71 @@
+// Linear layers in 8-bit integers: formats, the layout of a packed weight, and what the kernels and the ABI share.
+//
+// A row of activations, or an output channel of a weight, is held as integers q in [-127, 127] and one fp32 scale s: x = s q.  A
+// product of two such matrices is an exact integer sum, y[m][n] = s_m w_n sum_k q[m][k] c[n][k]; |sum| <= K 2^14 stays below 2^31
+// for K up to Q8_MAX_K.
+//
+// Packed weight: units of 32 channels ("packed rows" R = 0 .. 31) by 64 k, 2 KiB each, [unit][k-tile][sub][chunk][16 rows][16 bytes]: packed row
+// R = 16 sub + row, k = 64 k-tile + 16 chunk + byte.  A sub is one operand of a 16x16x64 product, lane by lane (row = lane % 16, chunk =
+// lane / 16), and both subs together are the two operands of 32x32x32 products.  Behind the codes lie the scales, [unit][R] fp32.
+// Channels and k's past the end are zeros, so that whatever stands behind the last k of a row of activations is multiplied by zero.
+//
+// Which channel packed row R = 8a + 4b + c (a, c = 0..3, b = 0, 1) is: the products leave a lane 4 (16x16) or 16 (32x32: b = lane / 32) packed
+// rows of a token, and these are to be neighbours in the output:
+//   plain  channel 32 unit + 16b + 4a + c
+//   gated  a < 2: gate, a >= 2: up, of output 16 unit + 8b + 4 (a % 2) + c, so that a lane holds both parts of each of its outputs
+#pragma once
+#include "common.h"
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
+
+constexpr int Q8_MAX_K = 131071;
+constexpr int Q8_MAX_N = 1 << 24;
+constexpr int Q8_MAX_WIDTH = 1 << 20;  // of rows that are quantised
+
+struct Q8View {
+  const unsigned char* codes;
+  const float* scale;
+  int n, k, units, kt;  // channels, inputs; units of 32 packed rows, k-tiles of 64
+  bool gated;
+  int outputs() const { return gated ? n / 2 : n; }
+};
+__host__ __device__ inline int q8_units(int n, int gated) { return gated ? (n / 2 + 15) / 16 : (n + 31) / 32; }
+// the channel of packed row R of a unit (n and more: none)
+__host__ __device__ inline int q8_channel(int unit, int R, int n, int gated) {
+  const int a = R >> 3, b = (R >> 2) & 1, c = R & 3;
+  if (!gated) return 32 * unit + 16 * b + 4 * a + c;
+  const int o = 16 * unit + 8 * b + 4 * (a & 1) + c;
+  return o >= n / 2 ? n : a < 2 ? o : n / 2 + o;
+}
+
+struct Q8RowsArgs {
+  const void* x;
+  int64_t x_stride;
+  int rows, width, dtype;
+  const void* residual;  // null: none
+  int64_t r_stride;
+  void* h;
+  int64_t h_stride;
+  int h_dtype;
+  const void* gain;  // null: rows are quantised as they are
+  float eps;
+  int8_t* codes;
+  int64_t codes_stride;
+  float* scale;
+};
+void launch_q8_rows(const Q8RowsArgs& a, hipStream_t st);
+void launch_q8_pack(const int8_t* codes, int64_t stride, const float* scale, const Q8View& w, void* data, hipStream_t st);
+
+struct Q8GemmArgs {
+  const int8_t* x;
+  int64_t x_stride;
+  const float* x_scale;
+  int M;
+  void* out;
+  int64_t out_stride;
+  int out_dtype;
+  void* workspace;
+};
+size_t q8_gemm_workspace(int rows, int n, int k, int gated);  // most bytes that a launch of up to that many rows needs
+void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, hipStream_t st);

@@ -1,0 +1,40 @@
+// What the kernels of the 8-bit integer product share: loads of their operands, and the epilogue.
+#pragma once
+#include "q8.h"
+
+namespace {
+
+template <typename TO> struct Out4;
+template <> struct Out4<bf16_t> { typedef bf16x4 vec; };
+template <> struct Out4<float> { typedef f32x4 vec; };
+
+// y = q-sum x scale of the token x scales of the channels, in this order (each rounded once: 2^-24 of the value, besides the conversion's)
+__device__ inline f32x4 scaled(i32x4 sum, float token, f32x4 channel) {
+  f32x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = (float)sum[i] * token * channel[i];
+  return y;
+}
+// silu(g) u: the exponential and the reciprocal within a few units of fp32's last place
+__device__ inline f32x4 gated_unit(f32x4 g, f32x4 u) {
+  f32x4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = g[i] * __builtin_amdgcn_rcpf(1.f + __expf(-g[i])) * u[i];
+  return y;
+}
+// outputs n .. n + 3 of a row of `outputs`: what is past its end is left as it is
+template <typename TO>
+__device__ inline void store4(TO* row, int n, int outputs, f32x4 y) {
+  if (n + 4 <= outputs) {
+    typename Out4<TO>::vec v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = (TO)y[i];
+    *(typename Out4<TO>::vec*)(row + n) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < outputs) row[n + i] = (TO)y[i];
+  }
+}
+
+}  // namespace

@@ -1,0 +1,204 @@
+// Rows in 8-bit integers, alone or behind the residual's addition and a root-mean-square norm: one pass over the row.
+//
+//   t = x                                    s = max|t| / 127                             (dlm_q8_rows)
+//   h = residual + x, t = h gain             s = max|t| rsqrt(mean(h^2) + eps) / 127      (dlm_add_norm_q8)
+//   q = 127 t / max|t| rounded to the nearest integer, ties to even
+//
+// The norm multiplies every t of a row by the same number, which cancels in q: codes depend on no sum and on no square root, and t is a product of two
+// numbers as they are stored, rounded to fp32 once (exact for bf16).  So q can be what the formula says to the last bit: an fp32 quotient
+// (off by at most 127 x 2^-23) decides all but those next to a border k + 1/2, and for these the sign of 127 t - (k + 1/2) max|t| does, which 64
+// bits hold (31 and 32 bits of product before one rounding).  A border is hit exactly whenever t = +-max|t| / 2.
+// Bound by memory: each value is read once and kept in registers until the row's maximum and sum are known.
+#include "q8.h"
+
+namespace {
+
+template <typename T> struct V8;  // eight values of a row
+template <> struct V8<bf16_t> {
+  bf16x8 v;
+  __device__ inline void load(const bf16_t* p) { v = *(const bf16x8*)p; }
+  __device__ inline float get(int i) const { return (float)v[i]; }
+  __device__ inline void set(int i, float x) { v[i] = (bf16_t)x; }
+  __device__ inline void store(bf16_t* p) const { *(bf16x8*)p = v; }
+};
+template <> struct V8<float> {
+  f32x4 v[2];
+  __device__ inline void load(const float* p) { v[0] = *(const f32x4*)p; v[1] = *(const f32x4*)(p + 4); }
+  __device__ inline float get(int i) const { return v[i >> 2][i & 3]; }
+  __device__ inline void set(int i, float x) { v[i >> 2][i & 3] = x; }
+  __device__ inline void store(float* p) const { *(f32x4*)p = v[0]; *(f32x4*)(p + 4) = v[1]; }
+};
+// values d .. d + 7 of a row of `width` (those past its end are zeros, and are not stored)
+template <typename T>
+__device__ inline V8<T> load8(const T* row, int d, int width) {
+  V8<T> r;
+  if (d + 8 <= width) {
+    r.load(row + d);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.set(i, d + i < width ? (float)row[d + i] : 0.f);
+  }
+  return r;
+}
+template <typename T>
+__device__ inline void store8(const V8<T>& v, T* row, int d, int width) {
+  if (d + 8 <= width) {
+    v.store(row + d);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (d + i < width) row[d + i] = (T)v.get(i);
+  }
+}
+
+// The code of t where the row's largest magnitude is top: inv = 127 / top in fp32
+__device__ inline int code(float t, float top, float inv) {
+  const float q = t * inv, k = rintf(q), r = q - k;
+  int c = (int)k;
+  if (fabsf(r) > 0.4999f) {
+    const double border = (double)k + (r > 0.f ? 0.5 : -0.5), e = fma(-border, (double)top, 127.0 * (double)t);
+    const int below = (int)floor(border);
+    c = e > 0.0 ? below + 1 : e < 0.0 ? below : below + (below & 1);
+  }
+  return c;
+}
+
+// T threads a row; a thread keeps ITERS times eight values, T x 8 of the row apart.  LOOP: rows of any length, read (or, of a sum, read back from h)
+// a second time.
+template <typename TX, typename TH, bool NORM, bool RES, int T, int ITERS, bool LOOP>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void q8_rows_kernel(const TX* x, int64_t x_stride, const TH* residual, int64_t r_stride, TH* h_out, int64_t h_stride,
+                                                                    const TX* __restrict__ gain, float eps, int8_t* __restrict__ codes, int64_t codes_stride,
+                                                                    float* __restrict__ scale, int rows, int width) {
+  constexpr int TPB = T < 256 ? 256 : T, STEP = T * 8;
+  const int row = blockIdx.x * (TPB / T) + threadIdx.x / T, d0 = threadIdx.x % T * 8;
+  if (T == 64 && row >= rows) return;  // (a wavefront has one row, and meets no other)
+  const TX* px = x + row * x_stride;
+  const TH* pr = RES ? residual + row * r_stride : nullptr;
+  TH* ph = RES ? h_out + row * h_stride : nullptr;
+  int8_t* pc = codes + row * codes_stride;
+
+  float t[ITERS][8];
+  unsigned top = 0;
+  float ss = 0.f;
+  auto take = [&](int d, float (&v)[8], bool first) __attribute__((always_inline)) {  // the t's of d .. d + 7
+    if (RES && !first) {
+      const V8<TH> h = load8(ph, d, width);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = h.get(i);
+    } else {
+      const V8<TX> a = load8(px, d, width);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = a.get(i);
+      if (RES) {
+        V8<TH> h = load8(pr, d, width);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          h.set(i, h.get(i) + v[i]);
+          v[i] = h.get(i);
+        }
+        store8(h, ph, d, width);
+      }
+    }
+    if (NORM) {
+      const V8<TX> g = load8(gain, d, width);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (first) ss += v[i] * v[i];
+        v[i] *= g.get(i);
+      }
+    }
+    if (first)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);  // (a NaN is above infinity here)
+  };
+  if (LOOP) {
+    for (int d = d0; d < width; d += STEP) take(d, t[0], true);
+  } else {
+#pragma unroll
+    for (int j = 0; j < ITERS; ++j)
+      if (d0 + j * STEP < width) take(d0 + j * STEP, t[j], true);
+  }
+  struct BitsUMax { __device__ unsigned operator()(unsigned a, unsigned b) const { return max(a, b); } };
+  top = butterfly(top, BitsUMax());
+  if (NORM) ss = wave_sum(ss);
+  if (T > 64) {
+    __shared__ unsigned s_top[T / 64];
+    __shared__ float s_ss[T / 64];
+    const int wave = threadIdx.x >> 6;
+    if ((threadIdx.x & 63) == 0) {
+      s_top[wave] = top;
+      s_ss[wave] = ss;
+    }
+    __syncthreads();
+    top = 0;
+    ss = 0.f;
+#pragma unroll
+    for (int i = 0; i < T / 64; ++i) {
+      top = max(top, s_top[i]);
+      if (NORM) ss += s_ss[i];
+    }
+  }
+  const float a = __uint_as_float(top);
+  const bool bad = top >= 0x7F800000u || (NORM && !(ss < __builtin_inff()));
+  if (threadIdx.x % T == 0) {
+    const float s = NORM && a > 0.f ? a * rsqrtf(ss / (float)width + eps) / 127.f : a / 127.f;
+    scale[row] = bad ? __builtin_nanf("") : s;
+  }
+  // a row of zeros: every quotient 0 x 0; a tiny maximum: its quotient would be past fp32's range, so the row is scaled by a power of two first
+  const float up = a < 0x1p-60f ? 0x1p64f : 1.f, big = a * up, inv = bad || big == 0.f ? 0.f : 127.f / big;
+  auto put = [&](int d, const float (&v)[8]) __attribute__((always_inline)) {
+    union { signed char c[8]; uint64_t w; } o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.c[i] = (signed char)(bad ? 0 : code(v[i] * up, big, inv));
+    if (d + 8 <= width) {
+      *(uint64_t*)(pc + d) = o.w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (d + i < width) pc[d + i] = o.c[i];
+    }
+  };
+  if (LOOP) {
+    for (int d = d0; d < width; d += STEP) {
+      take(d, t[0], false);
+      put(d, t[0]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < ITERS; ++j)
+      if (d0 + j * STEP < width) put(d0 + j * STEP, t[j]);
+  }
+}
+
+template <typename TX, typename TH, bool NORM, bool RES>
+void launch(const Q8RowsArgs& a, hipStream_t st) {
+  auto go = [&](auto kernel, int threads) {
+    const int per = threads < 256 ? 256 / threads : 1;
+    kernel<<<(a.rows + per - 1) / per, threads * per, 0, st>>>((const TX*)a.x, a.x_stride, (const TH*)a.residual, a.r_stride, (TH*)a.h, a.h_stride,
+                                                               (const TX*)a.gain, a.eps, a.codes, a.codes_stride, a.scale, a.rows, a.width);
+  };
+#define GO(T, ITERS, LOOP) go(q8_rows_kernel<TX, TH, NORM, RES, T, ITERS, LOOP>, T)
+  if (a.width <= 512) GO(64, 1, false);
+  else if (a.width <= 2048) GO(256, 1, false);
+  else if (a.width <= 4096) GO(256, 2, false);
+  else if (a.width <= 8192) GO(256, 4, false);
+  else if (a.width <= 16384) GO(1024, 2, false);
+  else if (a.width <= 32768) GO(1024, 4, false);
+  else GO(1024, 1, true);
+#undef GO
+}
+
+}  // namespace
+
+void launch_q8_rows(const Q8RowsArgs& a, hipStream_t st) {
+  if (a.dtype == DLM_BF16) {
+    if (!a.gain) launch<bf16_t, bf16_t, false, false>(a, st);
+    else if (!a.residual) launch<bf16_t, bf16_t, true, false>(a, st);
+    else if (a.h_dtype == DLM_BF16) launch<bf16_t, bf16_t, true, true>(a, st);
+    else launch<bf16_t, float, true, true>(a, st);
+  } else {
+    if (!a.gain) launch<float, float, false, false>(a, st);
+    else if (!a.residual) launch<float, float, true, false>(a, st);
+    else launch<float, float, true, true>(a, st);
+  }
+}
