@@ -7,7 +7,7 @@
 // Packed weight: units of 32 channels ("packed rows" R = 0 .. 31) by 64 k, 2 KiB each, [unit][k-tile][sub][chunk][16 rows][16 bytes]: packed row
 // R = 16 sub + row, k = 64 k-tile + 16 chunk + byte.  A sub is one operand of a 16x16x64 product, lane by lane (row = lane % 16, chunk =
 // lane / 16), and both subs together are the two operands of 32x32x32 products.  Behind the codes lie the scales, [unit][R] fp32.
-// Channels and k's past the end are zeros, so that whatever stands behind the last k of a row of activations is multiplied by zero.
+// k-tiles come in pairs; channels and k's past the end are zeros, so that whatever stands behind the last k of a row of activations is multiplied by zero.
 //
 // Which channel packed row R = 8a + 4b + c (a, c = 0..3, b = 0, 1) is: the products leave a lane 4 (16x16) or 16 (32x32: b = lane / 32) packed
 // rows of a token, and these are to be neighbours in the output:
@@ -26,11 +26,12 @@ constexpr int Q8_MAX_WIDTH = 1 << 20;  // of rows that are quantised
 struct Q8View {
   const unsigned char* codes;
   const float* scale;
-  int n, k, units, kt;  // channels, inputs; units of 32 packed rows, k-tiles of 64
+  int n, k, units, kt;  // channels, inputs; units of 32 packed rows, k-tiles of 64 (an even number)
   bool gated;
   int outputs() const { return gated ? n / 2 : n; }
 };
 __host__ __device__ inline int q8_units(int n, int gated) { return gated ? (n / 2 + 15) / 16 : (n + 31) / 32; }
+__host__ __device__ constexpr int q8_ktiles(int k) { return (k + 127) / 128 * 2; }
 // the channel of packed row R of a unit (n and more: none)
 __host__ __device__ inline int q8_channel(int unit, int R, int n, int gated) {
   const int a = R >> 3, b = (R >> 2) & 1, c = R & 3;

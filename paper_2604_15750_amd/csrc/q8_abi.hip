@@ -7,7 +7,7 @@ namespace {
 // bytes of a packed weight (its codes, then its scales), 0 for an unsupported shape
 int64_t weight_code_bytes(int n, int k, int gated) {
   if (n < 1 || n > Q8_MAX_N || k < 1 || k > Q8_MAX_K || (gated && n % 2)) return 0;
-  const int64_t bytes = (int64_t)q8_units(n, gated) * ((k + 63) / 64) * 2048;
+  const int64_t bytes = (int64_t)q8_units(n, gated) * q8_ktiles(k) * 2048;
   return bytes <= INT64_C(1) << 35 ? bytes : 0;  // (16 of them a thread of the packing's launch)
 }
 int64_t weight_bytes(int n, int k, int gated) {
@@ -20,7 +20,7 @@ int check_weight(const char* name, const dlm_q8_weight* w, Q8View* view) {
   REQUIRE(w->gated == 0 || w->gated == 1, DLM_EINVAL, "%s: gated %d", name, w->gated);
   const int64_t codes = weight_code_bytes(w->n, w->k, w->gated);
   REQUIRE(codes, DLM_ESHAPE, "%s: a weight of %d x %d", name, w->n, w->k);
-  *view = Q8View{(const unsigned char*)w->data, (const float*)((const char*)w->data + codes), w->n, w->k, q8_units(w->n, w->gated), (w->k + 63) / 64, w->gated == 1};
+  *view = Q8View{(const unsigned char*)w->data, (const float*)((const char*)w->data + codes), w->n, w->k, q8_units(w->n, w->gated), q8_ktiles(w->k), w->gated == 1};
   return DLM_OK;
 }
 // rows of 8-bit codes [rows, k], whose bytes up to a multiple of 16 belong to them

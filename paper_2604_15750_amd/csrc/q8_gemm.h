@@ -37,4 +37,23 @@ __device__ inline void store4(TO* row, int n, int outputs, f32x4 y) {
   }
 }
 
+// outputs n .. n + 7
+template <typename TO>
+__device__ inline void store8(TO* row, int n, int outputs, f32x4 lo, f32x4 hi) {
+  if constexpr (sizeof(TO) == 2) {
+    if (n + 8 <= outputs) {
+      bf16x8 v;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = (bf16_t)lo[i];
+        v[4 + i] = (bf16_t)hi[i];
+      }
+      *(bf16x8*)(row + n) = v;
+      return;
+    }
+  }
+  store4(row, n, outputs, lo);
+  store4(row, n + 4, outputs, hi);
+}
+
 }  // namespace

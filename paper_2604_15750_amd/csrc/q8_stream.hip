@@ -17,14 +17,14 @@ __global__ __launch_bounds__(256) void q8_stream_kernel(const i32x4* __restrict_
   extern __shared__ __align__(16) i32x4 red[];  // [NWV][CS * MT][64]
   constexpr int F = CS * MT;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, ml = lane & 15;
-  const int KT = (K + 63) >> 6, KC = (K + 15) >> 4, sub0 = blockIdx.x * CS, m0 = blockIdx.y * (16 * MT);
+  const int KT = (K + 63) >> 6, KTP = q8_ktiles(K), KC = (K + 15) >> 4, sub0 = blockIdx.x * CS, m0 = blockIdx.y * (16 * MT);
   const int per = (KT + NWV - 1) / NWV, t0 = wave * per, t1 = min(KT, t0 + per), steps = t1 - t0;  // this wavefront's k-tiles (possibly none)
 
   const i32x4* wp[CS];
 #pragma unroll
   for (int c = 0; c < CS; ++c) {
     const int s = min(sub0 + c, subs - 1);
-    wp[c] = wt + ((int64_t)(s >> 1) * KT * 2 + (s & 1)) * 64 + lane;
+    wp[c] = wt + ((int64_t)(s >> 1) * KTP * 2 + (s & 1)) * 64 + lane;
   }
   const int8_t* xp[MT];
 #pragma unroll

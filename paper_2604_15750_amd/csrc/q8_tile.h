@@ -1,0 +1,230 @@
+// Product in 8-bit integers for many rows: tiles of the output, both operands through LDS.
+//
+// A workgroup of RW x CW wavefronts owns 32 RW WM rows of X (tokens) x 32 CW WN packed rows of W and walks K in stages of KB k-tiles of 64:
+//   * W's units lie in memory as the products take them, so a stage of them is copied to LDS as it is; X's rows are 64 KB bytes of each of the tile's
+//     rows, in 16-byte chunks whose place in the row is turned by the row's number, so that 16 lanes that read the same chunk of 16 rows
+//     meet 16 different banks' groups.  Both by direct-to-LDS loads, S stages of them in flight or in use;
+//   * a wavefront multiplies WM x WN fragments (v_mfma_i32_32x32x32_i8) of a step of 32 k while it reads the next step's from LDS;
+//   * one barrier a stage, in front of its last step: by then every wavefront has the stage's last fragments in registers, and the copies of
+//     stage s + S go out over the steps that follow.
+#pragma once
+#include <type_traits>
+
+#include "q8_gemm.h"
+
+// {WM, WN, RW, CW, KB, ns4, ns2, ns1}: nanoseconds per k-tile of 64 on a chip full of such workgroups, one each a compute unit, where four or more, two, or one
+// row block share a W that comes from HBM (random codes; slopes between K = 2048 and 8192 of 256 workgroups)
+#define Q8_TILES(X)                                                                          \
+  X(4, 2, 2, 4, 1, 859, 1048, 972) X(3, 3, 2, 4, 1, 861, 996, 1066) X(3, 2, 2, 4, 1, 631, 693, 795) \
+  X(2, 3, 2, 4, 1, 669, 871, 917) X(2, 2, 2, 4, 2, 445, 476, 633) X(5, 1, 1, 8, 1, 563, 652, 710)   \
+  X(5, 1, 1, 4, 1, 371, 371, 430) X(3, 1, 2, 4, 1, 393, 393, 561) X(1, 2, 4, 2, 2, 257, 257, 320)   \
+  X(1, 2, 2, 4, 2, 266, 381, 635) X(1, 2, 2, 2, 2, 178, 178, 287) X(3, 1, 1, 8, 1, 377, 496, 614)   \
+  X(3, 1, 1, 4, 1, 250, 250, 316) X(1, 1, 2, 2, 2, 145, 147, 148)
+// rows: 256 (x 256 packed rows), 192 (x 384, 256, 128), 128 (x 384, 256, 128), 160 (x 256, 128), 64 (x 256, 128, 64), 96 (x 256, 128)
+
+struct Q8TilePlan {
+  int tile;  // index into Q8_TILES
+  int nblocks, mblocks;
+  float us;  // estimated
+};
+Q8TilePlan q8_tile_plan(int M, int units, int K);
+template <bool GATED, typename TO>
+void launch_q8_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);  // q8_tile_<form>_<type>.hip
+
+#ifdef Q8_TILE_INSTANTIATE
+namespace {
+
+// 1 KiB, 16 bytes a lane, from a buffer to LDS (dst: the wavefront's)
+template <bool NT>
+__device__ inline void copy_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* dst, int lane_at, int at) {
+  __attribute__((address_space(3))) void* to = (__attribute__((address_space(3))) void*)dst;
+  if constexpr (NT) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, lane_at, at, 0, 2);
+  else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, lane_at, at, 0, 0);
+}
+
+template <int WM, int WN, int RW, int CW, int KB>
+struct Q8Tile {
+  static constexpr int NW = RW * CW, TPB = NW * 64, BM = 32 * RW * WM, UN = CW * WN;  // rows of X, units of W
+  static constexpr int W_LOADS = UN * KB * 2, X_LOADS = BM * KB / 16;                 // of 1 KiB, a stage
+  static constexpr int LPS = (W_LOADS + X_LOADS + NW - 1) / NW;                       // ... of a wavefront (surplus ones repeat the last)
+  static constexpr int W_BYTES = W_LOADS * 1024, STAGE = W_BYTES + X_LOADS * 1024;
+  static constexpr int S_FIT = 160 * 1024 / STAGE, S_CNT = 63 / LPS + 1, S_ = S_FIT < S_CNT ? S_FIT : S_CNT, S = S_ > 6 ? 6 : S_;
+  static constexpr int LDS_BYTES = S * STAGE;
+  static_assert(W_LOADS % NW == 0 && (KB == 1 || X_LOADS % NW == 0) && S >= 2 && (KB == 1 || KB == 2), "tile shape");
+};
+
+template <int WM, int WN, int RW, int CW, int KB, bool GATED, typename TO>
+__global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kernel(const unsigned char* __restrict__ wt, const int8_t* __restrict__ x, int x_stride, int M, int K, int units,
+                                                                      int nblocks, int mblocks, const float* __restrict__ wscale, const float* __restrict__ x_scale,
+                                                                      TO* __restrict__ out, int64_t out_stride, int outputs) {
+  typedef Q8Tile<WM, WN, RW, CW, KB> SH;
+  constexpr int NW = SH::NW, BM = SH::BM, UN = SH::UN, LPS = SH::LPS, STAGE = SH::STAGE, S = SH::S, W_LOADS = SH::W_LOADS, LOADS = W_LOADS + SH::X_LOADS;
+  constexpr int STEPS = 2 * KB;  // of 32 k, a stage
+  extern __shared__ __align__(16) unsigned char lds[];
+
+  // Workgroup id -> tile: ids congruent mod 8 share an XCD, which gets one contiguous eighth of the tiles; in groups of 8 row blocks, row blocks fastest, so that
+  // the tiles an XCD works on at a time share both operands in its L2
+  const int tiles = nblocks * mblocks, lin = (blockIdx.x & 7) * ((tiles + 7) >> 3) + (blockIdx.x >> 3);
+  if (lin >= tiles) return;  // (the whole workgroup)
+  const int group = lin / (8 * nblocks), rows_in = min(8, mblocks - 8 * group), at = lin - group * 8 * nblocks;
+  const int cb = at / rows_in, rb = 8 * group + at - cb * rows_in;
+
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / CW, wn = wave % CW;
+  const int KTP = (K + 127) >> 7 << 1, nst = ((K + 63) / 64 + KB - 1) / KB;  // k-tiles of a unit in memory; stages
+  const int u0 = cb * UN, m0 = rb * BM, mrows = min(BM, M - m0), nunits = min(UN, units - u0);
+
+  // Direct-to-LDS loads, 1 KiB each: wavefront w moves the ones congruent w mod NW, W's first.  Rows and units past the end are the last one again, chunks
+  // past a row's last are that one again (W is zero there): every address is one of the operands'.
+  const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void*)(wt + (int64_t)u0 * KTP * 2048), 0, nunits * KTP * 2048, 0x00020000);
+  const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + (int64_t)m0 * x_stride), 0, (mrows - 1) * x_stride + (K + 15) / 16 * 16, 0x00020000);
+  constexpr int CPR = 4 * KB, RPL = 64 / CPR;  // chunks of a row, rows of a load
+  int off[LPS];
+#pragma unroll
+  for (int i = 0; i < LPS; ++i) {
+    const int f = min(i * NW + wave, LOADS - 1);
+    if (i * NW < W_LOADS) {
+      off[i] = min(f / (2 * KB), nunits - 1) * (KTP * 2048) + f % (2 * KB) * 1024 + lane * 16;
+    } else {
+      off[i] = min((f - W_LOADS) * RPL + lane / CPR, mrows - 1) * x_stride;
+    }
+  }
+  const int my_row = (wave * RPL + lane / CPR) & 15;  // (of 16: the same in all of a lane's loads, or NW is odd)
+  static_assert(NW * RPL % 16 == 0 && W_LOADS % NW == 0, "a lane's rows are congruent mod 16");
+  const int my_chunk = ((lane % CPR) ^ (KB == 2 ? my_row >> 1 : my_row >> 2)) * 16;
+  const int k_last = (K + 15) / 16 * 16 - 16;
+  auto issue = [&](int s, int buf, int lo, int hi) __attribute__((always_inline)) {
+    const int t = min(s, nst - 1);
+    const int chunk = min(my_chunk, k_last - t * (64 * KB));
+#pragma unroll
+    for (int i = lo; i < hi; ++i) {
+      unsigned char* dst = lds + buf * STAGE + min(i * NW + wave, LOADS - 1) * 1024;
+      if (i * NW < W_LOADS) copy_to_lds<false>(wr, dst, off[i], t * (KB * 2048));
+      else copy_to_lds<false>(xr, dst, off[i] + chunk, t * (64 * KB));
+    }
+  };
+
+  i32x16 acc[WN][WM];
+#pragma unroll
+  for (int j = 0; j < WN; ++j)
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) acc[j][i][v] = 0;
+  i32x4 xf[2][WM], wf[2][WN];
+  const int half = lane >> 5, r32 = lane & 31;
+  const int w_at = (r32 >> 4) * 1024 + half * 256 + (r32 & 15) * 16, turn = KB == 2 ? (r32 >> 1) & 7 : (r32 >> 2) & 3;
+  auto read_frags = [&](int set, int buf, int q) __attribute__((always_inline)) {
+    const unsigned char* st = lds + buf * STAGE;
+#pragma unroll
+    for (int j = 0; j < WN; ++j) wf[set][j] = *(const i32x4*)(st + ((wn * WN + j) * KB + (q >> 1)) * 2048 + (q & 1) * 512 + w_at);
+#pragma unroll
+    for (int i = 0; i < WM; ++i) xf[set][i] = *(const i32x4*)(st + SH::W_BYTES + ((wm * WM + i) * 32 + r32) * (64 * KB) + (((2 * q + half) ^ turn) << 4));
+  };
+  auto multiply = [&](int set) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < WN; ++j)
+#pragma unroll
+      for (int i = 0; i < WM; ++i) acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[set][j], xf[set][i], acc[j][i], 0, 0, 0);
+  };
+
+  // stages 0 .. S - 2 and the first part of S - 1 go out at once; the rest of it during stage 0, as for every later stage
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s) issue(s, s, 0, LPS);
+  issue(S - 1, S - 1, 0, LPS / STEPS);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * LPS + LPS / STEPS) : "memory");  // stage 0 has landed (this wavefront's share)
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  read_frags(0, 0, 0);
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  auto step = [&](auto Qc, int s, int buf, int nbuf) __attribute__((always_inline)) {
+    constexpr int Q = decltype(Qc)::value, SET = Q & 1;
+    constexpr bool LAST = Q == STEPS - 1;
+    constexpr int LO = LAST ? 0 : LPS * (Q + 1) / STEPS, HI = LAST ? LPS / STEPS : LPS * (Q + 2) / STEPS;
+    if (LAST) {
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * LPS) : "memory");  // stage s + 1 has landed
+      __builtin_amdgcn_s_barrier();  // ... for every wavefront, and every wavefront has read the last of stage s
+      asm volatile("" ::: "memory");
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    if (LAST) issue(s + S, buf, LO, HI);
+    else issue(s + S - 1, buf == 0 ? S - 1 : buf - 1, LO, HI);
+    read_frags(SET ^ 1, LAST ? nbuf : buf, LAST ? 0 : Q + 1);
+    multiply(SET);
+    constexpr int NM = WN * WM, RF = WM + WN, LI = HI - LO;
+    constexpr int OPS = 2 * (LI + RF) <= NM ? 1 : LI + RF <= NM ? 2 : 4;
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+#pragma unroll
+    for (int i = 0; i < RF; i += OPS) {
+      __builtin_amdgcn_sched_group_barrier(0x100, OPS, 0);  // LDS reads
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);    // one product
+    }
+#pragma unroll
+    for (int i = 0; i < LI; i += OPS) {
+      __builtin_amdgcn_sched_group_barrier(0x010, OPS, 0);  // copies to LDS
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, NM, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the reads have had the products' time to complete
+  };
+  int buf = 0;
+  for (int s = 0; s < nst; ++s) {
+    const int nbuf = buf + 1 == S ? 0 : buf + 1;
+    step(std::integral_constant<int, 0>{}, s, buf, nbuf);
+    step(std::integral_constant<int, 1>{}, s, buf, nbuf);
+    if constexpr (KB == 2) {
+      step(std::integral_constant<int, 2>{}, s, buf, nbuf);
+      step(std::integral_constant<int, 3>{}, s, buf, nbuf);
+    }
+    buf = nbuf;
+  }
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last stages land before the workgroup's LDS is another's
+
+  // ---- epilogue, straight from the accumulators: a lane has 16 packed rows of a token, neighbours in the output
+#pragma unroll
+  for (int i = 0; i < WM; ++i) {
+    const int m = m0 + (wm * WM + i) * 32 + r32;
+    const float xs = x_scale[min(m, M - 1)];
+    TO* row = out + (int64_t)m * out_stride;
+#pragma unroll
+    for (int j = 0; j < WN; ++j) {
+      const int u = u0 + wn * WN + j;
+      if (u >= units) continue;
+      f32x4 y[4];
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+        y[a] = scaled(i32x4{acc[j][i][4 * a], acc[j][i][4 * a + 1], acc[j][i][4 * a + 2], acc[j][i][4 * a + 3]}, xs, *(const f32x4*)(wscale + u * 32 + 8 * a + 4 * half));
+      if (m >= M) continue;
+      if (GATED) {
+        store8(row, 16 * u + 8 * half, outputs, gated_unit(y[0], y[2]), gated_unit(y[1], y[3]));
+      } else {
+        store8(row, 32 * u + 16 * half, outputs, y[0], y[1]);
+        store8(row, 32 * u + 16 * half + 8, outputs, y[2], y[3]);
+      }
+    }
+  }
+}
+
+template <int WM, int WN, int RW, int CW, int KB, bool GATED, typename TO>
+void launch_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
+  typedef Q8Tile<WM, WN, RW, CW, KB> SH;
+  static bool configured = false;  // raise the dynamic LDS limit of this instantiation once
+  if (!configured) {
+    (void)hipFuncSetAttribute((const void*)q8_tile_kernel<WM, WN, RW, CW, KB, GATED, TO>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS_BYTES);
+    configured = true;
+  }
+  q8_tile_kernel<WM, WN, RW, CW, KB, GATED, TO><<<(p.nblocks * p.mblocks + 7) / 8 * 8, SH::TPB, SH::LDS_BYTES, st>>>(
+      w.codes, a.x, (int)a.x_stride, a.M, w.k, w.units, p.nblocks, p.mblocks, w.scale, a.x_scale, (TO*)a.out, a.out_stride, w.outputs());
+}
+
+}  // namespace
+
+template <bool GATED, typename TO>
+void launch_q8_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
+  int i = 0;
+#define GO(WM, WN, RW, CW, KB, NS4, NS2, NS1) \
+  if (p.tile == i++) return launch_tile<WM, WN, RW, CW, KB, GATED, TO>(w, a, p, st);
+  Q8_TILES(GO)
+#undef GO
+}
+#endif  // Q8_TILE_INSTANTIATE

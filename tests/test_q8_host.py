@@ -22,9 +22,9 @@ def _weight(n=64, k=256, gated=0, data=T):
 def test_weight_bytes():
     f = api.lib().dlm_q8_weight_bytes
     assert C.sizeof(api.dlm_q8_weight) == 24
-    # units of 32 channels x 64 k, and 32 scales each
-    assert f(1, 1, 0) == 2048 + 128 and f(33, 65, 0) == 2 * (2 * 2048 + 128) and f(64, 64, 1) == 2 * (2048 + 128) and f(66, 64, 1) == 3 * (2048 + 128)
-    assert f(1 << 17, 131071, 0) == 4096 * (2048 * 2048 + 128)  # (beyond 32 bits)
+    # units of 32 channels x 128 k, and 32 scales each
+    assert f(1, 1, 0) == 4096 + 128 and f(33, 129, 0) == 2 * (2 * 4096 + 128) and f(64, 64, 1) == 2 * (4096 + 128) and f(66, 128, 1) == 3 * (4096 + 128)
+    assert f(1 << 17, 131071, 0) == 4096 * (1024 * 4096 + 128)  # (beyond 32 bits)
     for bad in ((0, 1, 0), (1, 0, 0), (3, 8, 1), (-2, 8, 1), (1, 131072, 0), ((1 << 24) + 1, 8, 0), (1 << 24, 131071, 0)):
         assert f(*bad) == 0, bad
 
