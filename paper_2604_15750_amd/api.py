@@ -665,6 +665,21 @@ def _codes(name, t, dev, rows, width):
     return stride
 
 
+# Calls with all their outputs given go through an extension (csrc/q8_py.cpp), as those of the 8-bit cache do.
+@functools.lru_cache(maxsize=None)
+def _q8_calls():
+    """The extension, bound to the library; None where it has not been built, or for another torch, whose tensors it would misread."""
+    try:
+        from . import _q8 as m
+    except ImportError:
+        return None
+    if getattr(m, "torch_version", None) != str(torch.__version__):
+        return None
+    L = lib()
+    m.bind(*(C.cast(f, C.c_void_p).value for f in (L.dlm_q8_rows, L.dlm_add_norm_q8, L.dlm_q8_gemm)))
+    return m
+
+
 def _code_outputs(x, dev, codes, scale):
     rows, width = x.shape
     if codes is None:
@@ -679,6 +694,9 @@ def _code_outputs(x, dev, codes, scale):
 def dlm_q8_rows(x, codes=None, scale=None):
     """Rows in 8-bit integers: x: device tensor [rows, width] (rows may be strided); codes: int8 [rows, width], scale: fp32 [rows] (None: new ones).
     Returns (codes, scale)."""
+    ext = _q8_calls()
+    if ext is not None and _taken(ext.rows(x, codes, scale, _device(), _stream())):
+        return codes, scale
     dev = _gpu_of("x", x)
     stride = _matrix("x", x, dev, None, None, _FLOATS)
     codes, code_stride, scale = _code_outputs(x, dev, codes, scale)
@@ -694,6 +712,9 @@ def dlm_add_norm_q8(x, gain, residual=None, h=None, eps=1e-5, codes=None, scale=
     """The residual's addition, RMSNorm and the rows in 8-bit integers: x: device tensor [rows, width]; gain: [width] of x's dtype; residual: [rows,
     width] of x's dtype or fp32, or None (no addition); h: residual + x, of the residual's dtype (None: a new tensor; the residual or x itself: in place);
     codes, scale: as dlm_q8_rows.  Returns (codes, scale, h); h is x where there is no residual."""
+    ext = _q8_calls()
+    if ext is not None and _taken(ext.norm(x, gain, residual, h, eps, codes, scale, _device(), _stream())):
+        return codes, scale, x if residual is None else h
     dev = _gpu_of("x", x)
     stride = _matrix("x", x, dev, None, None, _FLOATS)
     rows, width = x.shape
@@ -757,6 +778,9 @@ class Q8Weight:
 def dlm_q8_gemm(weight, x, x_scale, out=None, dtype=torch.bfloat16, workspace=None):
     """The product of rows of codes (int8 [rows, k], scales fp32 [rows]) with a Q8Weight: into out [rows, weight.outputs] (fp32 or bf16; rows may be strided), or
     into a new tensor of `dtype`; workspace: one of weight.workspace(as many rows or more) that nothing else uses meanwhile (None: a new one).  Returns out."""
+    ext = _q8_calls()
+    if ext is not None and _taken(ext.gemm(weight._ref, weight._data, x, x_scale, out, workspace, _device(), _stream())):
+        return out
     dev = _gpu_of("x", x)
     stride = _codes("x", x, dev, None, weight.k)
     rows = x.shape[0]

@@ -1,5 +1,5 @@
 """Compile csrc/*.hip into paper_2604_15750_amd/libdlm.so for gfx950 and csrc/decisions_py.c into _decisions (in-tree, no torch dependency), and
-csrc/kv8_py.cpp into _kv8 where torch and its headers are there."""
+csrc/kv8_py.cpp and csrc/q8_py.cpp into _kv8 and _q8 where torch and its headers are there."""
 import os
 import shutil
 import subprocess
@@ -13,6 +13,7 @@ OUT = os.path.join(HERE, "libdlm.so")
 # (tagged with the interpreter it was built for: it reads that one's objects, and another does not load it)
 OUT_PY = os.path.join(HERE, "_decisions" + sysconfig.get_config_var("EXT_SUFFIX"))
 OUT_KV8 = os.path.join(HERE, "_kv8" + sysconfig.get_config_var("EXT_SUFFIX"))
+OUT_Q8 = os.path.join(HERE, "_q8" + sysconfig.get_config_var("EXT_SUFFIX"))
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # amdgpu-kernarg-preload-count: a kernel's first arguments (14 dwords at most, up to the first struct) arrive in scalar registers with the
 # launch instead of by a trip to memory, so its first loads go out at once (161 launches of an in-block pass of the 8B model: 2888 -> 2864 us;
@@ -44,6 +45,7 @@ def build(verbose=False):
         raise RuntimeError("link failed:\n" + r.stderr)
     build_extension()
     build_kv8_extension()
+    build_q8_extension()
     return OUT
 
 
@@ -73,9 +75,17 @@ def build_extension():
 def build_kv8_extension():
     """The same for the 8-bit cache's operators, against torch's headers: its tensors are read without a call into Python.  It is of use with that
     torch alone, and names it."""
-    calls = "the 8-bit cache's operators"
-    if os.path.exists(OUT_KV8):
-        os.remove(OUT_KV8)
+    return _compile_with_torch("kv8_py.cpp", OUT_KV8, "the 8-bit cache's operators")
+
+
+def build_q8_extension():
+    """... and for the 8-bit integer layers'."""
+    return _compile_with_torch("q8_py.cpp", OUT_Q8, "the 8-bit integer layers' operators")
+
+
+def _compile_with_torch(source, out, calls):
+    if os.path.exists(out):
+        os.remove(out)
     try:
         import torch
     except ImportError:
@@ -84,7 +94,7 @@ def build_kv8_extension():
     at = os.path.dirname(torch.__file__)
     flags = [f'-DTORCH_BUILT_WITH="{torch.__version__}"', "-std=c++17", "-I", os.path.join(at, "include"),
              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-L", os.path.join(at, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
-    return _compile_extension("kv8_py.cpp", OUT_KV8, calls, "g++", flags, needed=False)
+    return _compile_extension(source, out, calls, "g++", flags, needed=False)
 
 
 if __name__ == "__main__":

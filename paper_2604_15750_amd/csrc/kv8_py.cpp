@@ -6,93 +6,14 @@
 // contiguous rows; lists or tuples of ints that fit 32 bits, long enough and at most 32 sequences.  Anything else returns None before
 // anything is launched, and the caller goes the way through ctypes, which takes every other form and says what it refuses.
 // Tensors are read in place, as the headers of one torch lay them out: `torch_version` says which, and with another one nothing here is to be called.
-#include <torch/csrc/autograd/python_variable.h>
-
-#include <cstdint>
-
-#include "../../include/dlm.h"
+#include "py_args.h"
 
 namespace {
-
-constexpr int MAX_SEQS = 32;
 
 int (*g_span[2])(const dlm_kv8_cache*, void*, void*, int64_t, int, const int32_t*, const int32_t*, const int32_t*, int, void*);
 int (*g_attention)(const dlm_kv8_cache*, const void*, int64_t, void*, int, int, const int32_t*, const int32_t*, const int32_t*, int, const uint32_t*, int,
                           void*, size_t, void*);
 int (*g_rope)(const void*, int64_t, int, int, int, int, int, const void*, const void*, float, float, const int32_t*, void*, int64_t, void*);
-// Each returns 0 for an argument that is not plain (with no error set).
-int to_i64(PyObject* o, int64_t* out) {
-  int overflow;
-  if (!PyLong_Check(o)) return 0;
-  *out = PyLong_AsLongLongAndOverflow(o, &overflow);
-  return !overflow;
-}
-int to_int(PyObject* o, int* out) {
-  int64_t v;
-  if (!to_i64(o, &v) || v < INT32_MIN || v > INT32_MAX) return 0;
-  *out = (int)v;
-  return 1;
-}
-int to_float(PyObject* o, float* out) {
-  if (!PyFloat_CheckExact(o)) return 0;
-  const double v = PyFloat_AS_DOUBLE(o);
-  *out = (float)v;
-  return (*out - *out == 0.f) || v - v != 0.;  // (a finite value that overflows is the other way's error)
-}
-// the first n entries of an array that has as many (n < 0: all of them); their number, or -1
-int to_ints(PyObject* o, int n, int32_t* out) {
-  PyObject** item;
-  Py_ssize_t len;
-  if (PyList_CheckExact(o)) {
-    item = ((PyListObject*)o)->ob_item;
-    len = PyList_GET_SIZE(o);
-  } else if (PyTuple_CheckExact(o)) {
-    item = ((PyTupleObject*)o)->ob_item;
-    len = PyTuple_GET_SIZE(o);
-  } else {
-    return -1;
-  }
-  if (n < 0) n = len <= MAX_SEQS ? (int)len : -1;
-  if (n < 0 || len < n) return -1;
-  for (int i = 0; i < n; ++i)
-    if (!to_int(item[i], out + i)) return -1;
-  return n;
-}
-
-const at::Tensor* plain(PyObject* o, int dev) {  // of torch's own type, in memory of GPU `dev`
-  if (!THPVariable_CheckExact(o)) return nullptr;
-  const at::Tensor& x = THPVariable_Unpack(o);
-  return x.defined() && x.get_device() == dev && x.layout() == at::kStrided ? &x : nullptr;
-}
-struct Tensor {
-  void* p;
-  int dtype, dims;  // dtype: a DLM_ code, or 2 for int32
-  int64_t shape[3], stride;
-};
-// a tensor of 1 to 3 dimensions whose rows (everything behind the first) are contiguous
-bool to_tensor(PyObject* o, int dev, Tensor* t) {
-  const at::Tensor* x = plain(o, dev);
-  if (!x) return false;
-  const auto type = x->scalar_type();
-  t->dtype = type == at::kBFloat16 ? DLM_BF16 : type == at::kFloat ? DLM_F32 : type == at::kInt ? 2 : -1;
-  const auto shape = x->sizes(), stride = x->strides();
-  t->dims = (int)shape.size();
-  if (t->dtype < 0 || t->dims < 1 || t->dims > 3 || shape[0] < 1) return false;  // (a tensor without rows has no address)
-  int64_t width = 1;
-  for (int i = t->dims - 1; i >= 0; --i) {
-    t->shape[i] = shape[i];
-    if (i == 0) break;
-    if (stride[i] != width && shape[i] != 1) return false;
-    width *= shape[i];
-  }
-  t->stride = shape[0] > 1 ? stride[0] : width;
-  t->p = x->data_ptr();
-  return true;
-}
-bool is_float(const Tensor& t) { return t.dtype == DLM_F32 || t.dtype == DLM_BF16; }
-#define DECLINE_UNLESS(cond) \
-  if (!(cond)) Py_RETURN_NONE
-
 // span(0 write, 1 read, cache, cache memory, k, v, row_offsets, start, slot, device, stream) -> status or None
 PyObject* span(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   int32_t off[MAX_SEQS + 1], start[MAX_SEQS], slot[MAX_SEQS];
@@ -186,16 +107,6 @@ PyObject* bind(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   *(void**)&g_attention = f[2];
   *(void**)&g_rope = f[3];
   Py_RETURN_NONE;
-}
-
-// what torch throws (a tensor without memory, say) is the other way's to report
-template <PyObject* (*F)(PyObject*, PyObject* const*, Py_ssize_t)>
-PyObject* quiet(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
-  try {
-    return F(self, a, n_args);
-  } catch (...) {
-    Py_RETURN_NONE;
-  }
 }
 
 PyMethodDef methods[] = {{"span", (PyCFunction)(void (*)(void))quiet<span>, METH_FASTCALL, "dlm_kv8_write and dlm_kv8_read"},

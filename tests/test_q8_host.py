@@ -119,7 +119,7 @@ def test_python_refusals(monkeypatch):
     """Shapes, types and memory that the library could not see."""
     monkeypatch.setattr(api, "_device", lambda: -1)  # (tensors here are on the CPU, whose index is -1)
     monkeypatch.setattr(api, "_gpu_of", lambda name, t: -1)
-    monkeypatch.setattr(api, "_stream", lambda: None)
+    monkeypatch.setattr(api, "_stream", lambda: 0)
     x, gain = torch.zeros(4, 64), torch.ones(64)
     for bad in (dict(codes=torch.zeros(4, 64)), dict(codes=torch.zeros(3, 64, dtype=torch.int8)), dict(codes=torch.zeros(4, 80, dtype=torch.int8)),
                 dict(scale=torch.zeros(4, dtype=torch.float64)), dict(scale=torch.zeros(5)), dict(scale=torch.zeros(8)[::2])):
@@ -164,7 +164,7 @@ def test_python_refusals(monkeypatch):
 def test_calls_without_rows_return(monkeypatch):
     monkeypatch.setattr(api, "_device", lambda: -1)
     monkeypatch.setattr(api, "_gpu_of", lambda name, t: -1)
-    monkeypatch.setattr(api, "_stream", lambda: None)
+    monkeypatch.setattr(api, "_stream", lambda: 0)
     codes, scale = api.dlm_q8_rows(torch.zeros(0, 64))
     assert codes.shape == (0, 64) and scale.shape == (0,)
     assert api.dlm_add_norm_q8(torch.zeros(0, 64), torch.ones(64), torch.zeros(0, 64))[2].shape == (0, 64)
