@@ -123,13 +123,14 @@ extern "C" int dlm_q8_gemm(const dlm_q8_weight* w, const int8_t* x, int64_t x_st
   const Rows xr = Rows::of_bytes(x, rows, x_stride, ((int64_t)view.k + 15) / 16 * 16), to(out, rows, out_stride, outputs, out_dtype);
   const wide bytes = weight_bytes(view.n, view.k, view.gated);
   REQUIRE(!overlap(xr, to) && !overlap(out, to.span(), x_scale, (wide)rows * 4) && !overlap(out, to.span(), w->data, bytes), DLM_EINVAL, "%s: out overlaps an array of the call", name);
-  const size_t need = rows ? q8_gemm_workspace(rows, view.n, view.k, view.gated) : 0;
+  const Q8GemmArgs args{x, x_stride, x_scale, rows, out, out_stride, out_dtype, workspace};
+  const size_t need = rows ? q8_gemm_need(view, args) : 0;
   REQUIRE(!need || (workspace && workspace_bytes >= need), DLM_ECAPACITY, "%s: workspace of %zu bytes < %zu", name, workspace ? workspace_bytes : 0, need);
   REQUIRE(!need || !(overlap(workspace, need, x, xr.span()) || overlap(workspace, need, out, to.span()) || overlap(workspace, need, x_scale, (wide)rows * 4) ||
                      overlap(workspace, need, w->data, bytes)),
           DLM_EINVAL, "%s: the workspace overlaps an array of the call", name);
   if (rows == 0) return DLM_OK;
-  launch_q8_gemm(view, Q8GemmArgs{x, x_stride, x_scale, rows, out, out_stride, out_dtype, workspace}, (hipStream_t)stream);
+  launch_q8_gemm(view, args, (hipStream_t)stream);
   DLM_HIP(hipGetLastError());
   return DLM_OK;
 }

@@ -1,5 +1,7 @@
 // What the kernels of the 8-bit integer product share: loads of their operands, and the epilogue.
 #pragma once
+#include <type_traits>
+
 #include "q8.h"
 
 namespace {
@@ -54,6 +56,16 @@ __device__ inline void store8(TO* row, int n, int outputs, f32x4 lo, f32x4 hi) {
   }
   store4(row, n, outputs, lo);
   store4(row, n + 4, outputs, hi);
+}
+
+// What a product writes: bit 0: fp32, not bf16; bit 1: gated.  f(gated, out) with both in its arguments' types (the branch is uniform, behind the product's loop)
+inline int out_form(const Q8View& w, const Q8GemmArgs& a) { return (a.out_dtype == DLM_F32) | (int)w.gated << 1; }
+template <typename F>
+__device__ inline void with_form(int form, void* out, F f) {
+  if (form == 0) f(std::false_type{}, (bf16_t*)out);
+  else if (form == 1) f(std::false_type{}, (float*)out);
+  else if (form == 2) f(std::true_type{}, (bf16_t*)out);
+  else f(std::true_type{}, (float*)out);
 }
 
 }  // namespace

@@ -1,6 +1,8 @@
 // Products in 8-bit integers: the packing of a weight, and the choice of the kernel.
+#include <cmath>
+
 #include "q8_gemm.h"
-#include "q8_tile.h"
+#include "q8_plan.h"
 
 namespace {
 
@@ -37,36 +39,101 @@ void launch_q8_pack(const int8_t* codes, int64_t stride, const float* scale, con
   q8_pack_scale_kernel<<<(w.units * 32 + 255) / 256, 256, 0, st>>>(scale, w.n, w.gated, w.units, (float*)w.scale);
 }
 
-size_t q8_gemm_workspace(int, int, int, int) { return 0; }
-
-// The tile with the least estimated time.  A round is what 256 compute units take together; a chip that is partly full runs its workgroups up to 40 %
-// faster, and every round pays for its pipeline's start and its epilogue.
+// The tile and K split with the least estimated time.  A round is what 256 compute units take together.  A k-tile takes what a workgroup alone on the chip
+// takes (ns), or what the chip's power leaves the matrix cores (2.7 PFLOP/s), what the L2s (23.7 TB/s) or, for W, HBM (6.0 TB/s, shared by up to 8
+// row blocks) give to all of the round's workgroups, whichever is most, joined by a 4-norm; a round pays for its copies' start and its
+// epilogue; a K split adds the hand-off, the partial tiles' traffic, and those that the last workgroup reads.  Constants fitted to the launches named
+// at Q8_TILES: 9 % off in the mean square.
 Q8TilePlan q8_tile_plan(int M, int units, int K) {
-  const struct { int wm, wn, rw, cw, kb; float ns4, ns2, ns1; } tiles[] = {
-#define ROW(WM, WN, RW, CW, KB, NS4, NS2, NS1) {WM, WN, RW, CW, KB, NS4, NS2, NS1},
-      Q8_TILES(ROW)
-#undef ROW
+  struct Shape {
+    int frags, bm, un, kb, first_loads;  // first_loads: copies of a wavefront before the loop
+    float ns_4, chip_4, hbm;             // 4th powers of ns, and of what power and the L2s allow on a full chip; ns that HBM allows where one row block reads W
   };
-  constexpr int CUS = 256;
+  constexpr float CUS = 256.f;
+#define ROW(WM, WN, RW, CW, KB, NT, NS) q8_shape(WM, WN, RW, CW, KB, NS),
+  static const auto q8_shape = [](int wm, int wn, int rw, int cw, int kb, float ns) {
+    const int bm = 32 * rw * wm, un = cw * wn, loads = un * kb * 2 + bm * kb / 16, lps = (loads + rw * cw - 1) / (rw * cw), fit = 160 / loads, count = 63 / lps + 1;
+    const int stages = fit < count ? (fit < 6 ? fit : 6) : (count < 6 ? count : 6);
+    auto p4 = [](float x) { return x * x * x * x; };
+    return Shape{wm * wn, bm, un, kb, lps * stages, p4(ns), p4(bm * un * 32 * 128 * CUS / 2.73e6f) + p4((bm + un * 32) * 64 * CUS / 23.7e3f), un * 2048 * CUS / 6.0e3f};
+  };
+  static const Shape shapes[] = {Q8_TILES(ROW)};
+#undef ROW
   const int KT = (K + 63) / 64;
-  Q8TilePlan best{0, 1, 1, 1e30f};
+  Q8TilePlan best{};
+  best.us = 1e30f;
   int i = -1;
-  for (auto& t : tiles) {
+  for (const Shape& t : shapes) {
     ++i;
-    const int bm = 32 * t.rw * t.wm, un = t.cw * t.wn, mb = (M + bm - 1) / bm, nb = (units + un - 1) / un, kt = (KT + t.kb - 1) / t.kb * t.kb;
-    const int64_t wgs = (int64_t)mb * nb, full = (wgs - 1) / CUS, last = wgs - CUS * full;
-    const float ns = mb == 1 ? t.ns1 : mb < 4 ? t.ns2 : t.ns4, fixed = 3.f + bm * un * 32 * 1e-4f;
-    const float us = kt * ns * 1e-3f * (full + 0.6f + 0.4f * last / CUS) + (full + 1) * fixed;
-    if (us < best.us) best = Q8TilePlan{i, nb, mb, us};
+    const int mb = (M + t.bm - 1) / t.bm, nb = (units + t.un - 1) / t.un, stages = (KT + t.kb - 1) / t.kb;
+    const float out = t.bm * t.un * 32.f, edge = t.bm + t.un * 32.f, hbm = t.hbm / (mb < 8 ? mb : 8), full_4 = t.chip_4 + hbm * hbm * hbm * hbm;
+    auto ns = [&](float share) { return sqrtf(sqrtf(t.ns_4 + full_4 * (share * share) * (share * share))); };
+    const int64_t wgs = (int64_t)mb * nb;
+    for (int sp = 1; sp <= (t.frags <= Q8_SPLIT_FRAGS ? Q8_MAX_SPLITS : 1); ++sp) {
+      if (sp > 1 && (wgs * sp > Q8_SPLIT_WGS || stages < 4 * sp)) break;
+      const int per = (stages + sp - 1) / sp;
+      if ((stages + per - 1) / per != sp) continue;  // (a split without stages)
+      const int64_t all = wgs * sp, full = (all - 1) / 256;
+      const float last = (all - 256 * full) / CUS;
+      float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 0.6f + 0.057f * t.first_loads + (full + last) * 1.5e-4f * out + (full + 1) * 9.3e-3f * edge;
+      if (sp > 1) us += 2.3f + out * 4e-3f * ((sp - 1) * 9.8e-3f + all * 1.64e-4f);
+      if (us < best.us) best = Q8TilePlan{i, t.bm, nb, mb, sp, per, sp > 1 ? Q8_SPLIT_WGS * 4 + (size_t)all * t.bm * t.un * 128 : 0, us};
+    }
   }
   return best;
 }
 
-void launch_q8_stream(const Q8View& w, const Q8GemmArgs& a, hipStream_t st);
+// Subs of a workgroup, for the least that the busiest compute unit has to read (its subs of W, and X once a workgroup) at 34 bytes a nanosecond, up to 50 on a
+// chip that is partly full: within 10 % of what was measured from 512 x 16000 to 37888 x 3584 at 8 and 16 rows
+Q8StreamPlan q8_stream_plan(int M, int units, int K, bool gated) {
+  const int subs = 2 * units, rows = M < Q8_STREAM_ROWS ? M : Q8_STREAM_ROWS;
+  Q8StreamPlan best{2, 1e30f};
+  for (int n = gated ? 2 : 1; n <= (gated || rows > 16 ? 2 : 3); ++n) {
+    const int wgs = (subs + n - 1) / n;
+    const float rate = (n == 3 ? 31e3f : 34e3f) + (wgs < 256 ? 16e3f * (256 - wgs) / 256 : 0.f);
+    const float us = 2.2f + (wgs + 255) / 256 * (16.f * n + rows) * K / rate;
+    if (us < best.us) best = Q8StreamPlan{n, us};
+  }
+  return best;
+}
+
+namespace {
+
+// Few rows are either's, whichever is estimated to take less; rows so far apart that a tile's would be past 32 bits are streamed, however many
+struct Choice {
+  bool stream;
+  Q8StreamPlan s;
+  Q8TilePlan t;
+};
+Choice choose(int M, int units, int K, bool gated, int64_t x_stride) {
+  Choice c{};
+  const bool far = x_stride > 1 << 22;
+  if (M <= Q8_STREAM_ROWS || far) c.s = q8_stream_plan(M, units, K, gated);
+  if (!far) c.t = q8_tile_plan(M, units, K);
+  c.stream = far || (M <= Q8_STREAM_ROWS && c.s.us <= c.t.us);
+  return c;
+}
+
+}  // namespace
+
+size_t q8_gemm_workspace(int rows, int n, int k, int gated) {
+  // (a tile's plan depends on the rows through their blocks of 32, and one that splits K has at most Q8_SPLIT_WGS / 2 tiles, of at least 32 x 64)
+  const int units = q8_units(n, gated), most = units <= Q8_SPLIT_WGS ? Q8_SPLIT_WGS / 2 * 256 : 0;
+  size_t bytes = 0;
+  for (int m = 1; m <= rows && m <= most; m += 32) {
+    const size_t need = q8_tile_plan(m, units, k).workspace;
+    if (need > bytes) bytes = need;
+  }
+  return bytes;
+}
+
+size_t q8_gemm_need(const Q8View& w, const Q8GemmArgs& a) {
+  const Choice c = choose(a.M, w.units, w.k, w.gated, a.x_stride);
+  return c.stream ? 0 : c.t.workspace;
+}
+
 void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, hipStream_t st) {
-  // few rows; or rows so far apart that a tile's would be past 32 bits
-  if (a.M <= 64 || a.x_stride > 1 << 22) return launch_q8_stream(w, a, st);
-  const Q8TilePlan p = q8_tile_plan(a.M, w.units, w.k);
-  if (a.out_dtype == DLM_BF16) w.gated ? launch_q8_tile<true, bf16_t>(w, a, p, st) : launch_q8_tile<false, bf16_t>(w, a, p, st);
-  else w.gated ? launch_q8_tile<true, float>(w, a, p, st) : launch_q8_tile<false, float>(w, a, p, st);
+  const Choice c = choose(a.M, w.units, w.k, w.gated, a.x_stride);
+  if (c.stream) return launch_q8_stream(w, a, c.s, st);
+  c.t.rows >= 128 ? launch_q8_tiles<true>(w, a, c.t, st) : launch_q8_tiles<false>(w, a, c.t, st);
 }

@@ -1,0 +1,37 @@
+// Which launch serves a product in 8-bit integers.
+#pragma once
+#include "q8.h"
+
+// The shape of a tile {WM, WN, RW, CW, KB, NT, ns}: see q8_tile.h.  NT: a W that one row block reads is read non-temporally, past the memory-side cache, in
+// which the weights of a model do not stay from pass to pass (5 % of launches of up to 64 rows; nothing beyond).  ns: nanoseconds per k-tile of 64 that a workgroup alone on the
+// chip takes.  15 of 24 shapes that were timed (17319 launches, 29 row counts from 8 to 2822, 15 weights from 640 x 640 to 3584 x 18944): with all 24 the choices
+// lose 3.0 % to the best of each, with these 2.8 %, with 10 of them 3.2 %.
+#define Q8_TILES(X)                                                                                                    \
+  X(4, 2, 2, 4, 1, false, 577) X(3, 3, 2, 4, 1, false, 644) X(3, 2, 2, 4, 1, false, 459) X(2, 3, 2, 4, 1, false, 462) \
+  X(2, 2, 2, 4, 2, false, 291) X(5, 1, 1, 5, 1, false, 389) X(1, 2, 4, 2, 2, false, 209) X(3, 1, 1, 6, 1, false, 279) \
+  X(3, 1, 1, 4, 1, false, 232) X(1, 1, 2, 5, 1, true, 249) X(1, 1, 2, 4, 2, true, 159) X(1, 1, 2, 2, 2, true, 132)    \
+  X(1, 1, 1, 5, 1, true, 186) X(1, 1, 1, 4, 2, true, 131) X(1, 1, 1, 2, 2, true, 120)
+// rows x packed rows: 256 x 256, 192 x 384, 192 x 256, 128 x 384, 128 x 256, 160 x 160, 128 x 128, 96 x 192, 96 x 128, 64 x 160, 64 x 128, 64 x 64, 32 x 160, 32 x 128, 32 x 64
+
+struct Q8TilePlan {
+  int tile;  // index into Q8_TILES
+  int rows;  // of a tile
+  int nblocks, mblocks;
+  int splits, stages;  // workgroups that share a tile's K, and how many stages each has
+  size_t workspace;    // bytes of a launch that splits K: Q8_SPLIT_WGS counters (zeros before and after it), then a partial tile for each workgroup
+  float us;            // estimated
+};
+// K is split only over tiles whose wavefronts have at most this many fragments (the last workgroup holds two tiles of them), in at most Q8_SPLIT_WGS
+// workgroups: one round, and a counter each
+constexpr int Q8_SPLIT_FRAGS = 6, Q8_SPLIT_WGS = 256, Q8_MAX_SPLITS = 8;
+Q8TilePlan q8_tile_plan(int M, int units, int K);
+template <bool WIDE>
+void launch_q8_tiles(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);
+
+constexpr int Q8_STREAM_ROWS = 32;  // up to as many rows may be the streamed product's (q8_stream.h)
+struct Q8StreamPlan {
+  int subs;  // of a workgroup: 1, 2 or 3
+  float us;  // estimated
+};
+Q8StreamPlan q8_stream_plan(int M, int units, int K, bool gated);
+void launch_q8_stream(const Q8View& w, const Q8GemmArgs& a, const Q8StreamPlan& p, hipStream_t st);

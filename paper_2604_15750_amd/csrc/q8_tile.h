@@ -8,30 +8,9 @@
 //   * one barrier a stage, in front of its last step: by then every wavefront has the stage's last fragments in registers, and the copies of
 //     stage s + S go out over the steps that follow.
 #pragma once
-#include <type_traits>
-
 #include "q8_gemm.h"
+#include "q8_plan.h"
 
-// {WM, WN, RW, CW, KB, ns4, ns2, ns1}: nanoseconds per k-tile of 64 on a chip full of such workgroups, one each a compute unit, where four or more, two, or one
-// row block share a W that comes from HBM (random codes; slopes between K = 2048 and 8192 of 256 workgroups)
-#define Q8_TILES(X)                                                                          \
-  X(4, 2, 2, 4, 1, 859, 1048, 972) X(3, 3, 2, 4, 1, 861, 996, 1066) X(3, 2, 2, 4, 1, 631, 693, 795) \
-  X(2, 3, 2, 4, 1, 669, 871, 917) X(2, 2, 2, 4, 2, 445, 476, 633) X(5, 1, 1, 8, 1, 563, 652, 710)   \
-  X(5, 1, 1, 4, 1, 371, 371, 430) X(3, 1, 2, 4, 1, 393, 393, 561) X(1, 2, 4, 2, 2, 257, 257, 320)   \
-  X(1, 2, 2, 4, 2, 266, 381, 635) X(1, 2, 2, 2, 2, 178, 178, 287) X(3, 1, 1, 8, 1, 377, 496, 614)   \
-  X(3, 1, 1, 4, 1, 250, 250, 316) X(1, 1, 2, 2, 2, 145, 147, 148)
-// rows: 256 (x 256 packed rows), 192 (x 384, 256, 128), 128 (x 384, 256, 128), 160 (x 256, 128), 64 (x 256, 128, 64), 96 (x 256, 128)
-
-struct Q8TilePlan {
-  int tile;  // index into Q8_TILES
-  int nblocks, mblocks;
-  float us;  // estimated
-};
-Q8TilePlan q8_tile_plan(int M, int units, int K);
-template <bool GATED, typename TO>
-void launch_q8_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);  // q8_tile_<form>_<type>.hip
-
-#ifdef Q8_TILE_INSTANTIATE
 namespace {
 
 // 1 KiB, 16 bytes a lane, from a buffer to LDS (dst: the wavefront's)
@@ -42,6 +21,16 @@ __device__ inline void copy_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* d
   else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, lane_at, at, 0, 0);
 }
 
+// 16 bytes a lane at device scope (past the XCD's L2)
+constexpr int SC1 = 16;
+__device__ inline void store_device(char* base, int bytes, int at, i32x4 v) {
+  typedef unsigned u32x4_ __attribute__((ext_vector_type(4)));
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_, v), __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000), at, 0, SC1);
+}
+__device__ inline i32x4 load_device(const char* base, int bytes, int at) {
+  return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000), at, 0, SC1));
+}
+
 template <int WM, int WN, int RW, int CW, int KB>
 struct Q8Tile {
   static constexpr int NW = RW * CW, TPB = NW * 64, BM = 32 * RW * WM, UN = CW * WN;  // rows of X, units of W
@@ -50,13 +39,13 @@ struct Q8Tile {
   static constexpr int W_BYTES = W_LOADS * 1024, STAGE = W_BYTES + X_LOADS * 1024;
   static constexpr int S_FIT = 160 * 1024 / STAGE, S_CNT = 63 / LPS + 1, S_ = S_FIT < S_CNT ? S_FIT : S_CNT, S = S_ > 6 ? 6 : S_;
   static constexpr int LDS_BYTES = S * STAGE;
-  static_assert(W_LOADS % NW == 0 && (KB == 1 || X_LOADS % NW == 0) && S >= 2 && (KB == 1 || KB == 2), "tile shape");
+  static_assert(W_LOADS % NW == 0 && (KB == 1 || X_LOADS % NW == 0) && S >= 2 && (KB == 1 || KB == 2) && LDS_BYTES <= 160 * 1024, "tile shape");
 };
 
-template <int WM, int WN, int RW, int CW, int KB, bool GATED, typename TO>
+template <int WM, int WN, int RW, int CW, int KB, bool NT>
 __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kernel(const unsigned char* __restrict__ wt, const int8_t* __restrict__ x, int x_stride, int M, int K, int units,
-                                                                      int nblocks, int mblocks, const float* __restrict__ wscale, const float* __restrict__ x_scale,
-                                                                      TO* __restrict__ out, int64_t out_stride, int outputs) {
+                                                                      int nblocks, int mblocks, int splits, int split_stages, const float* __restrict__ wscale, const float* __restrict__ x_scale,
+                                                                      void* __restrict__ out, int64_t out_stride, int outputs, int form, int* counters) {
   typedef Q8Tile<WM, WN, RW, CW, KB> SH;
   constexpr int NW = SH::NW, BM = SH::BM, UN = SH::UN, LPS = SH::LPS, STAGE = SH::STAGE, S = SH::S, W_LOADS = SH::W_LOADS, LOADS = W_LOADS + SH::X_LOADS;
   constexpr int STEPS = 2 * KB;  // of 32 k, a stage
@@ -64,13 +53,15 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
 
   // Workgroup id -> tile: ids congruent mod 8 share an XCD, which gets one contiguous eighth of the tiles; in groups of 8 row blocks, row blocks fastest, so that
   // the tiles an XCD works on at a time share both operands in its L2
-  const int tiles = nblocks * mblocks, lin = (blockIdx.x & 7) * ((tiles + 7) >> 3) + (blockIdx.x >> 3);
-  if (lin >= tiles) return;  // (the whole workgroup)
-  const int group = lin / (8 * nblocks), rows_in = min(8, mblocks - 8 * group), at = lin - group * 8 * nblocks;
+  const int tiles = nblocks * mblocks, lin = (blockIdx.x & 7) * ((tiles * splits + 7) >> 3) + (blockIdx.x >> 3);
+  if (lin >= tiles * splits) return;  // (the whole workgroup)
+  const int split = lin / tiles, tile = lin - split * tiles;
+  const int group = tile / (8 * nblocks), rows_in = min(8, mblocks - 8 * group), at = tile - group * 8 * nblocks;
   const int cb = at / rows_in, rb = 8 * group + at - cb * rows_in;
 
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / CW, wn = wave % CW;
-  const int KTP = (K + 127) >> 7 << 1, nst = ((K + 63) / 64 + KB - 1) / KB;  // k-tiles of a unit in memory; stages
+  const int KTP = (K + 127) >> 7 << 1;                                       // k-tiles of a unit in memory
+  const int s0 = split * split_stages, nst = min(((K + 63) / 64 + KB - 1) / KB - s0, split_stages);  // this workgroup's stages s0 .. s0 + nst - 1
   const int u0 = cb * UN, m0 = rb * BM, mrows = min(BM, M - m0), nunits = min(UN, units - u0);
 
   // Direct-to-LDS loads, 1 KiB each: wavefront w moves the ones congruent w mod NW, W's first.  Rows and units past the end are the last one again, chunks
@@ -93,12 +84,12 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
   const int my_chunk = ((lane % CPR) ^ (KB == 2 ? my_row >> 1 : my_row >> 2)) * 16;
   const int k_last = (K + 15) / 16 * 16 - 16;
   auto issue = [&](int s, int buf, int lo, int hi) __attribute__((always_inline)) {
-    const int t = min(s, nst - 1);
+    const int t = s0 + min(s, nst - 1);
     const int chunk = min(my_chunk, k_last - t * (64 * KB));
 #pragma unroll
     for (int i = lo; i < hi; ++i) {
       unsigned char* dst = lds + buf * STAGE + min(i * NW + wave, LOADS - 1) * 1024;
-      if (i * NW < W_LOADS) copy_to_lds<false>(wr, dst, off[i], t * (KB * 2048));
+      if (i * NW < W_LOADS) copy_to_lds<NT>(wr, dst, off[i], t * (KB * 2048));
       else copy_to_lds<false>(xr, dst, off[i] + chunk, t * (64 * KB));
     }
   };
@@ -180,51 +171,101 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last stages land before the workgroup's LDS is another's
 
-  // ---- epilogue, straight from the accumulators: a lane has 16 packed rows of a token, neighbours in the output
+  if constexpr (WM * WN <= Q8_SPLIT_FRAGS) if (splits > 1) {
+    // K split: every workgroup but the one that finishes last leaves its sums in the workspace and raises the tile's count; the last adds them up (integers:
+    // in any order) and goes on.  The hand-off crosses XCDs, whose L2s are separate: sums and counts are written and read at device scope, and a wavefront's
+    // stores have been acknowledged before the barrier in front of the count, so neither side needs a fence and nobody waits for anybody.
+    int* s_last = (int*)lds;  // (the loop's LDS is quiet; more than it would not fit)
+    constexpr int PART = SH::BM * UN * 32 * 4;
+    auto part = [&](int sp) { return (char*)(counters + Q8_SPLIT_WGS) + (int64_t)(sp * tiles + tile) * PART; };
+    constexpr int F = WM * WN;
+    auto place = [&](int f, int a) { return (((wave * F + f) * 4 + a) * 64 + lane) * 16; };
+    {
+      char* mine = part(split);
 #pragma unroll
-  for (int i = 0; i < WM; ++i) {
-    const int m = m0 + (wm * WM + i) * 32 + r32;
-    const float xs = x_scale[min(m, M - 1)];
-    TO* row = out + (int64_t)m * out_stride;
+      for (int f = 0; f < F; ++f)
 #pragma unroll
-    for (int j = 0; j < WN; ++j) {
-      const int u = u0 + wn * WN + j;
-      if (u >= units) continue;
-      f32x4 y[4];
+        for (int a = 0; a < 4; ++a) store_device(mine, PART, place(f, a), i32x4{acc[f / WM][f % WM][4 * a], acc[f / WM][f % WM][4 * a + 1], acc[f / WM][f % WM][4 * a + 2], acc[f / WM][f % WM][4 * a + 3]});
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) {
+      const int last = __hip_atomic_fetch_add(counters + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == splits - 1;
+      if (last) __hip_atomic_store(counters + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next launch
+      *s_last = last;
+    }
+    __syncthreads();
+    if (!*s_last) return;
+    asm volatile("" ::: "memory");
+    for (int sp = 0; sp < splits; ++sp) {
+      if (sp == split) continue;
+      const char* theirs = part(sp);
+      i32x4 t[F][4];
 #pragma unroll
-      for (int a = 0; a < 4; ++a)
-        y[a] = scaled(i32x4{acc[j][i][4 * a], acc[j][i][4 * a + 1], acc[j][i][4 * a + 2], acc[j][i][4 * a + 3]}, xs, *(const f32x4*)(wscale + u * 32 + 8 * a + 4 * half));
-      if (m >= M) continue;
-      if (GATED) {
-        store8(row, 16 * u + 8 * half, outputs, gated_unit(y[0], y[2]), gated_unit(y[1], y[3]));
-      } else {
-        store8(row, 32 * u + 16 * half, outputs, y[0], y[1]);
-        store8(row, 32 * u + 16 * half + 8, outputs, y[2], y[3]);
-      }
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int a = 0; a < 4; ++a) t[f][a] = load_device(theirs, PART, place(f, a));
+#pragma unroll
+      for (int f = 0; f < F; ++f)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) acc[f / WM][f % WM][v] += t[f][v >> 2][v & 3];
     }
   }
+
+  // ---- epilogue, straight from the accumulators: a lane has 16 packed rows of a token, neighbours in the output
+  with_form(form, out, [&](auto gated, auto* to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+      const int m = m0 + (wm * WM + i) * 32 + r32;
+      const float xs = x_scale[min(m, M - 1)];
+      auto* row = to + (int64_t)m * out_stride;
+#pragma unroll
+      for (int j = 0; j < WN; ++j) {
+        const int u = u0 + wn * WN + j;
+        if (u >= units) continue;
+        f32x4 y[4];
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+          y[a] = scaled(i32x4{acc[j][i][4 * a], acc[j][i][4 * a + 1], acc[j][i][4 * a + 2], acc[j][i][4 * a + 3]}, xs, *(const f32x4*)(wscale + u * 32 + 8 * a + 4 * half));
+        if (m >= M) continue;
+        if constexpr (decltype(gated)::value) {
+          store8(row, 16 * u + 8 * half, outputs, gated_unit(y[0], y[2]), gated_unit(y[1], y[3]));
+        } else {
+          store8(row, 32 * u + 16 * half, outputs, y[0], y[1]);
+          store8(row, 32 * u + 16 * half + 8, outputs, y[2], y[3]);
+        }
+      }
+    }
+  });
 }
 
-template <int WM, int WN, int RW, int CW, int KB, bool GATED, typename TO>
+template <int WM, int WN, int RW, int CW, int KB, bool NT>
 void launch_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
   typedef Q8Tile<WM, WN, RW, CW, KB> SH;
   static bool configured = false;  // raise the dynamic LDS limit of this instantiation once
   if (!configured) {
-    (void)hipFuncSetAttribute((const void*)q8_tile_kernel<WM, WN, RW, CW, KB, GATED, TO>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS_BYTES);
+    (void)hipFuncSetAttribute((const void*)q8_tile_kernel<WM, WN, RW, CW, KB, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS_BYTES);
     configured = true;
   }
-  q8_tile_kernel<WM, WN, RW, CW, KB, GATED, TO><<<(p.nblocks * p.mblocks + 7) / 8 * 8, SH::TPB, SH::LDS_BYTES, st>>>(
-      w.codes, a.x, (int)a.x_stride, a.M, w.k, w.units, p.nblocks, p.mblocks, w.scale, a.x_scale, (TO*)a.out, a.out_stride, w.outputs());
+  q8_tile_kernel<WM, WN, RW, CW, KB, NT><<<(p.nblocks * p.mblocks * p.splits + 7) / 8 * 8, SH::TPB, SH::LDS_BYTES, st>>>(
+      w.codes, a.x, (int)a.x_stride, a.M, w.k, w.units, p.nblocks, p.mblocks, p.splits, p.stages, w.scale, a.x_scale, a.out, a.out_stride, w.outputs(), out_form(w, a),
+      (int*)a.workspace);
 }
 
 }  // namespace
 
-template <bool GATED, typename TO>
-void launch_q8_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
+// the launches of the tiles of 128 rows and more, or of those of fewer (q8_tile_wide.hip, q8_tile_narrow.hip)
+template <bool WIDE>
+void launch_q8_tiles(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
   int i = 0;
-#define GO(WM, WN, RW, CW, KB, NS4, NS2, NS1) \
-  if (p.tile == i++) return launch_tile<WM, WN, RW, CW, KB, GATED, TO>(w, a, p, st);
+#define GO(WM, WN, RW, CW, KB, NT, NS)                                             \
+  if constexpr ((RW * WM >= 4) == WIDE) {                                                     \
+    if constexpr (NT) {                                                                       \
+      if (p.tile == i && p.mblocks == 1) return launch_tile<WM, WN, RW, CW, KB, true>(w, a, p, st); \
+    }                                                                                         \
+    if (p.tile == i) return launch_tile<WM, WN, RW, CW, KB, false>(w, a, p, st);              \
+  }                                                                                           \
+  ++i;
   Q8_TILES(GO)
 #undef GO
 }
-#endif  // Q8_TILE_INSTANTIATE
