@@ -344,7 +344,7 @@ int dlm_q8_weight_pack(const dlm_q8_weight* w, const int8_t* codes, int64_t code
  * workspace: DEVICE scratch at a multiple of 16 of dlm_q8_gemm_workspace(r, n, k, gated) bytes for some r >= rows (0: none is needed, it may be NULL),
  * zero-filled before its first use; a call leaves zeros where the next one needs them.  It is in use until the call's work is done: calls that may overlap need one each.
  * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, bad dtype, gated), DLM_ESHAPE (weight, rows < 0), DLM_ECAPACITY (workspace too small,
- * more than 1048576 rows), DLM_EHIP. */
+ * more than 1048576 rows or 2^38 outputs), DLM_EHIP. */
 size_t dlm_q8_gemm_workspace(int rows, int n, int k, int gated);
 int dlm_q8_gemm(const dlm_q8_weight* w, const int8_t* x, int64_t x_stride, const float* x_scale, int rows, void* out, int64_t out_stride, int out_dtype,
                 void* workspace, size_t workspace_bytes, void* stream);
@@ -396,10 +396,14 @@ int dlm_profile_read(dlm_state* s, int n, double* ms_out, int64_t* launches_out,
  * statistics (at most 64 rows).  plan[0] kernel (0 skinny, 1 mid, 2 macro), plan[1], plan[2] rows and columns of
  * a workgroup's tile, plan[3] workgroups that share a tile by splitting K, plan[4] parts K is summed in,
  * plan[5] workgroups, plan[6] chunks of the rows' sums of squares per column block (epilogue 3).
- * Errors: DLM_EINVAL (null, bad dtype or epilogue), DLM_ESHAPE (a size out of range, head_dim not in {32, 64, 128}). */
+ * dlm_plan_q8_gemm: dlm_q8_gemm of `rows` rows (a stride of up to 4 MiB between them) with a weight [n, k].  plan[0] kernel (0 streamed, 1 tiled), plan[1],
+ * plan[2] rows and packed channels of a workgroup's tile, plan[3] workgroups that share a tile by splitting K, plan[4] workgroups, plan[5] KiB of
+ * workspace.
+ * Errors: DLM_EINVAL (null, bad dtype, epilogue or gated), DLM_ESHAPE (a size out of range, head_dim not in {32, 64, 128}). */
 int dlm_plan_vocab_stats(int rows, int vocab, int dtype, int32_t plan[2]);
 int dlm_plan_gemm(int M, int N, int K, int epilogue, int32_t plan[7]);
 int dlm_plan_attention(int max_seq_rows, int n_seqs, int n_q, int head_dim, int32_t plan[3]);
+int dlm_plan_q8_gemm(int rows, int n, int k, int gated, int32_t plan[6]);
 
 #ifdef __cplusplus
 }

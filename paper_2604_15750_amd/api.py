@@ -69,7 +69,7 @@ EXPORTS = ["dlm_last_error", "dlm_model_create", "dlm_model_destroy", "dlm_state
            "dlm_state_fuse_stats", "dlm_vocab_stats_static", "dlm_plan_attention",
            "dlm_plan_vocab_stats", "dlm_plan_gemm", "dlm_qk_norm_rope", "dlm_kv8_bytes", "dlm_kv8_write", "dlm_kv8_read",
            "dlm_kv8_attention_workspace", "dlm_kv8_attention", "dlm_q8_rows", "dlm_add_norm_q8", "dlm_q8_weight_bytes",
-           "dlm_q8_weight_pack", "dlm_q8_gemm_workspace", "dlm_q8_gemm"]
+           "dlm_q8_weight_pack", "dlm_q8_gemm_workspace", "dlm_q8_gemm", "dlm_plan_q8_gemm"]
 
 
 def lib():
@@ -120,6 +120,7 @@ def lib():
         L.dlm_q8_rows.argtypes = [C.c_void_p, C.c_int64] + [C.c_int] * 3 + [C.c_void_p, C.c_int64] + [C.c_void_p] * 2
         L.dlm_add_norm_q8.argtypes = [C.c_void_p, C.c_int64] + [C.c_int] * 3 + [C.c_void_p, C.c_int64] * 2 + [C.c_int, C.c_void_p, C.c_float, C.c_void_p, C.c_int64] + \
                                      [C.c_void_p] * 2
+        L.dlm_plan_q8_gemm.argtypes = [C.c_int] * 4 + [_I32P]
         L.dlm_q8_weight_bytes.argtypes = [C.c_int] * 3
         L.dlm_q8_weight_bytes.restype = C.c_size_t
         L.dlm_q8_weight_pack.argtypes = [C.c_void_p] * 2 + [C.c_int64] + [C.c_void_p] * 2
@@ -827,3 +828,10 @@ def plan_gemm(M, N, K, epilogue):
     out = (C.c_int32 * 7)()
     _check(lib().dlm_plan_gemm(M, N, K, EPILOGUES.index(epilogue), out))
     return dict(zip(("kernel", "rows", "cols", "splits", "k_parts", "workgroups", "ssq_parts"), (("skinny", "mid", "macro")[out[0]], *out[1:])))
+
+
+def plan_q8_gemm(rows, n, k, gated=False):
+    """How a product of 8-bit rows with a Q8Weight [n, k] is launched (include/dlm.h)."""
+    out = (C.c_int32 * 6)()
+    _check(lib().dlm_plan_q8_gemm(rows, n, k, int(gated), out))
+    return dict(zip(("kernel", "rows", "cols", "splits", "workgroups", "workspace_kib"), (("streamed", "tiled")[out[0]], *out[1:])))

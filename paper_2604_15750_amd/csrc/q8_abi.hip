@@ -119,7 +119,7 @@ extern "C" int dlm_q8_gemm(const dlm_q8_weight* w, const int8_t* x, int64_t x_st
   const int outputs = view.outputs();
   REQUIRE(good_code_stride(x_stride, view.k) && good_stride(out_stride, outputs, out_dtype), DLM_EINVAL, "%s: strides %lld and %lld of rows of %d and %d", name,
           (long long)x_stride, (long long)out_stride, view.k, outputs);
-  REQUIRE(rows <= 1 << 20, DLM_ECAPACITY, "%s: too many rows for one launch", name);
+  REQUIRE(rows <= 1 << 20 && (int64_t)rows * outputs <= INT64_C(1) << 38, DLM_ECAPACITY, "%s: too many rows for one launch", name);
   const Rows xr = Rows::of_bytes(x, rows, x_stride, ((int64_t)view.k + 15) / 16 * 16), to(out, rows, out_stride, outputs, out_dtype);
   const wide bytes = weight_bytes(view.n, view.k, view.gated);
   REQUIRE(!overlap(xr, to) && !overlap(out, to.span(), x_scale, (wide)rows * 4) && !overlap(out, to.span(), w->data, bytes), DLM_EINVAL, "%s: out overlaps an array of the call", name);
@@ -132,5 +132,13 @@ extern "C" int dlm_q8_gemm(const dlm_q8_weight* w, const int8_t* x, int64_t x_st
   if (rows == 0) return DLM_OK;
   launch_q8_gemm(view, args, (hipStream_t)stream);
   DLM_HIP(hipGetLastError());
+  return DLM_OK;
+}
+
+extern "C" int dlm_plan_q8_gemm(int rows, int n, int k, int gated, int32_t plan[6]) {
+  REQUIRE(plan, DLM_EINVAL, "dlm_plan_q8_gemm: null plan");
+  REQUIRE(gated == 0 || gated == 1, DLM_EINVAL, "dlm_plan_q8_gemm: gated %d", gated);
+  REQUIRE(rows >= 1 && rows <= 1 << 20 && weight_bytes(n, k, gated), DLM_ESHAPE, "dlm_plan_q8_gemm: %d rows, a weight of %d x %d", rows, n, k);
+  q8_gemm_describe(rows, n, k, gated, plan);
   return DLM_OK;
 }

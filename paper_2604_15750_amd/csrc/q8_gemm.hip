@@ -77,7 +77,7 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
       const float last = (all - 256 * full) / CUS;
       float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 0.6f + 0.057f * t.first_loads + (full + last) * 1.5e-4f * out + (full + 1) * 9.3e-3f * edge;
       if (sp > 1) us += 2.3f + out * 4e-3f * ((sp - 1) * 9.8e-3f + all * 1.64e-4f);
-      if (us < best.us) best = Q8TilePlan{i, t.bm, nb, mb, sp, per, sp > 1 ? Q8_SPLIT_WGS * 4 + (size_t)all * t.bm * t.un * 128 : 0, us};
+      if (us < best.us) best = Q8TilePlan{i, t.bm, t.un * 32, nb, mb, sp, per, sp > 1 ? Q8_SPLIT_WGS * 4 + (size_t)all * t.bm * t.un * 128 : 0, us};
     }
   }
   return best;
@@ -117,8 +117,8 @@ Choice choose(int M, int units, int K, bool gated, int64_t x_stride) {
 }  // namespace
 
 size_t q8_gemm_workspace(int rows, int n, int k, int gated) {
-  // (a tile's plan depends on the rows through their blocks of 32, and one that splits K has at most Q8_SPLIT_WGS / 2 tiles, of at least 32 x 64)
-  const int units = q8_units(n, gated), most = units <= Q8_SPLIT_WGS ? Q8_SPLIT_WGS / 2 * 256 : 0;
+  // (a tile's plan depends on the rows through their blocks of 32, and one that splits K has at most Q8_SPLIT_WGS / 2 tiles, of at most 192 rows x 8 units)
+  const int units = q8_units(n, gated), most = 192 * (Q8_SPLIT_WGS / 2 / ((units + 7) / 8));
   size_t bytes = 0;
   for (int m = 1; m <= rows && m <= most; m += 32) {
     const size_t need = q8_tile_plan(m, units, k).workspace;
@@ -130,6 +130,19 @@ size_t q8_gemm_workspace(int rows, int n, int k, int gated) {
 size_t q8_gemm_need(const Q8View& w, const Q8GemmArgs& a) {
   const Choice c = choose(a.M, w.units, w.k, w.gated, a.x_stride);
   return c.stream ? 0 : c.t.workspace;
+}
+
+void q8_gemm_describe(int rows, int n, int k, int gated, int32_t plan[6]) {
+  const int units = q8_units(n, gated);
+  const Choice c = choose(rows, units, k, gated, 0);
+  const int tile = rows <= 16 ? 16 : 32;
+  if (c.stream) {
+    const int32_t p[6] = {0, tile, 16 * c.s.subs, 1, (2 * units + c.s.subs - 1) / c.s.subs * ((rows + tile - 1) / tile), 0};
+    for (int i = 0; i < 6; ++i) plan[i] = p[i];
+  } else {
+    const int32_t p[6] = {1, c.t.rows, c.t.cols, c.t.splits, c.t.nblocks * c.t.mblocks * c.t.splits, (int32_t)(c.t.workspace >> 10)};
+    for (int i = 0; i < 6; ++i) plan[i] = p[i];
+  }
 }
 
 void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, hipStream_t st) {

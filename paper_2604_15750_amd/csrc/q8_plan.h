@@ -15,7 +15,7 @@
 
 struct Q8TilePlan {
   int tile;  // index into Q8_TILES
-  int rows;  // of a tile
+  int rows, cols;  // of a tile
   int nblocks, mblocks;
   int splits, stages;  // workgroups that share a tile's K, and how many stages each has
   size_t workspace;    // bytes of a launch that splits K: Q8_SPLIT_WGS counters (zeros before and after it), then a partial tile for each workgroup

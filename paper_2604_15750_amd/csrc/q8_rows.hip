@@ -28,29 +28,6 @@ template <> struct V8<float> {
   __device__ inline void set(int i, float x) { v[i >> 2][i & 3] = x; }
   __device__ inline void store(float* p) const { *(f32x4*)p = v[0]; *(f32x4*)(p + 4) = v[1]; }
 };
-// values d .. d + 7 of a row of `width` (those past its end are zeros, and are not stored)
-template <typename T>
-__device__ inline V8<T> load8(const T* row, int d, int width) {
-  V8<T> r;
-  if (d + 8 <= width) {
-    r.load(row + d);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) r.set(i, d + i < width ? (float)row[d + i] : 0.f);
-  }
-  return r;
-}
-template <typename T>
-__device__ inline void store8(const V8<T>& v, T* row, int d, int width) {
-  if (d + 8 <= width) {
-    v.store(row + d);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (d + i < width) row[d + i] = (T)v.get(i);
-  }
-}
-
 // The code of t where the row's largest magnitude is top: inv = 127 / top in fp32
 __device__ inline int code(float t, float top, float inv) {
   const float q = t * inv, k = rintf(q), r = q - k;
@@ -77,30 +54,44 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void q8_rows_kernel(const TX* x,
   TH* ph = RES ? h_out + row * h_stride : nullptr;
   int8_t* pc = codes + row * codes_stride;
 
-  float t[ITERS][8];
+  // The last width % 8 values of a row are a thread's own, one each, so that eights have no bounds; their loads go out first
+  const int whole = width & ~7, e = whole + (int)(threadIdx.x % T);
+  const bool odd = e < width;  // (T > 7)
+  TX ox, og;
+  TH orr;
+  if (odd) {
+    ox = px[e];
+    if (RES) orr = pr[e];
+    if (NORM) og = gain[e];
+  }
+  float t[ITERS][8], ot = 0.f;
   unsigned top = 0;
   float ss = 0.f;
   auto take = [&](int d, float (&v)[8], bool first) __attribute__((always_inline)) {  // the t's of d .. d + 7
     if (RES && !first) {
-      const V8<TH> h = load8(ph, d, width);
+      V8<TH> h;
+      h.load(ph + d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = h.get(i);
     } else {
-      const V8<TX> a = load8(px, d, width);
+      V8<TX> a;
+      a.load(px + d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = a.get(i);
       if (RES) {
-        V8<TH> h = load8(pr, d, width);
+        V8<TH> h;
+        h.load(pr + d);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           h.set(i, h.get(i) + v[i]);
           v[i] = h.get(i);
         }
-        store8(h, ph, d, width);
+        h.store(ph + d);
       }
     }
     if (NORM) {
-      const V8<TX> g = load8(gain, d, width);
+      V8<TX> g;
+      g.load(gain + d);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         if (first) ss += v[i] * v[i];
@@ -112,11 +103,24 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void q8_rows_kernel(const TX* x,
       for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7FFFFFFFu);  // (a NaN is above infinity here)
   };
   if (LOOP) {
-    for (int d = d0; d < width; d += STEP) take(d, t[0], true);
+    for (int d = d0; d < whole; d += STEP) take(d, t[0], true);
   } else {
 #pragma unroll
     for (int j = 0; j < ITERS; ++j)
-      if (d0 + j * STEP < width) take(d0 + j * STEP, t[j], true);
+      if (d0 + j * STEP < whole) take(d0 + j * STEP, t[j], true);
+  }
+  if (odd) {
+    ot = (float)ox;
+    if (RES) {
+      const TH h = (TH)((float)orr + ot);
+      ph[e] = h;
+      ot = (float)h;
+    }
+    if (NORM) {
+      ss += ot * ot;
+      ot *= (float)og;
+    }
+    top = max(top, __float_as_uint(ot) & 0x7FFFFFFFu);
   }
   struct BitsUMax { __device__ unsigned operator()(unsigned a, unsigned b) const { return max(a, b); } };
   top = butterfly(top, BitsUMax());
@@ -150,24 +154,19 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void q8_rows_kernel(const TX* x,
     union { signed char c[8]; uint64_t w; } o;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o.c[i] = (signed char)(bad ? 0 : code(v[i] * up, big, inv));
-    if (d + 8 <= width) {
-      *(uint64_t*)(pc + d) = o.w;
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (d + i < width) pc[d + i] = o.c[i];
-    }
+    *(uint64_t*)(pc + d) = o.w;
   };
   if (LOOP) {
-    for (int d = d0; d < width; d += STEP) {
+    for (int d = d0; d < whole; d += STEP) {
       take(d, t[0], false);
       put(d, t[0]);
     }
   } else {
 #pragma unroll
     for (int j = 0; j < ITERS; ++j)
-      if (d0 + j * STEP < width) put(d0 + j * STEP, t[j]);
+      if (d0 + j * STEP < whole) put(d0 + j * STEP, t[j]);
   }
+  if (odd) pc[e] = (int8_t)(bad ? 0 : code(ot * up, big, inv));
 }
 
 template <typename TX, typename TH, bool NORM, bool RES>
@@ -179,9 +178,10 @@ void launch(const Q8RowsArgs& a, hipStream_t st) {
   };
 #define GO(T, ITERS, LOOP) go(q8_rows_kernel<TX, TH, NORM, RES, T, ITERS, LOOP>, T)
   if (a.width <= 512) GO(64, 1, false);
+  else if (a.width <= 1024) GO(64, 2, false);
   else if (a.width <= 2048) GO(256, 1, false);
   else if (a.width <= 4096) GO(256, 2, false);
-  else if (a.width <= 8192) GO(256, 4, false);
+  else if (a.width <= 8192) GO(512, 2, false);
   else if (a.width <= 16384) GO(1024, 2, false);
   else if (a.width <= 32768) GO(1024, 4, false);
   else GO(1024, 1, true);

@@ -229,6 +229,38 @@ def test_wide_product(device, dtype, rows, n, k, gated):
         assert (np.abs(_np64(out) - want) <= off).all() and _untouched(wide, weight.outputs)
 
 
+# shapes whose plain product is a launch of each streamed form and of each tile, with and without a K split
+VARIANTS = [(8, 64, 128), (8, 5000, 128), (8, 10000, 128), (24, 64, 128), (24, 5000, 128),
+            (35, 6256, 4100), (43, 182, 4100), (66, 9206, 1300), (69, 3025, 4100), (66, 9211, 128), (1847, 141, 8200), (39, 341, 128), (34, 2020, 4100), (34, 17358, 128),
+            (168, 2712, 4100), (33, 30191, 128), (2624, 157, 16400), (66, 20747, 128), (69, 5543, 16400), (65, 33241, 128), (280, 3626, 8200), (194, 10396, 128),
+            (198, 4169, 8200), (195, 16557, 128), (194, 8232, 16400), (195, 33691, 128), (129, 25332, 128), (129, 16768, 8200), (165, 27676, 128), (321, 33667, 128),
+            (394, 24874, 128)]
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows,n,k", VARIANTS)
+def test_every_variant(device, rows, n, k, gated):
+    n += gated and n % 2
+    g = _gen(rows, n, k)
+    (q, s), (c, w) = _coded(g, rows, k, 0.3), _coded(g, n, k, 0.3)
+    w = w * 30
+    weight = api.Q8Weight(_columns(c, device)[0], w.to(device), gated=gated)
+    qd = _columns(q, device)[0]
+    # (the sums in 64 bits on the GPU: exact, as they are below 2^53)
+    y = (q.to(device).double() @ c.to(device).double().t().contiguous()).cpu().numpy() * _np64(s)[:, None] * _np64(w)
+    want, off = y, 3 * U * np.abs(y)
+    if gated:
+        want = o_q8.gated(y)
+        off = (13 + 6 * np.abs(y[:, :n // 2])) * U * np.abs(want) + 2.0 ** -125 * np.abs(y[:, :n // 2] * y[:, n // 2:])
+    for dtype in (F32, BF16):
+        out, wide = _columns(torch.full((rows, weight.outputs), 9.0, dtype=dtype), device)
+        ws = weight.workspace(rows)
+        for _ in range(3):  # (a call finds what the one before left in the workspace)
+            out.fill_(9)
+            api.dlm_q8_gemm(weight, qd, s.to(device), out=out, workspace=ws)
+        assert (np.abs(_np64(out) - want) <= off * (1 + 2.0 ** -7) + HALF_STEP[dtype] * np.abs(want) + 2.0 ** -149).all() and _untouched(wide, weight.outputs)
+
+
 def test_the_largest_sums(device):
     """Every product -128 x -128, and 127 x -128: the longest sums that 32 bits hold."""
     k = 131071
@@ -358,8 +390,50 @@ def test_a_captured_layer_replays(device, rows):
         assert torch.equal(got[0], L.out) and torch.equal(got[1], L.h)
 
 
+def test_captured_products_share_a_workspace_or_have_none_given(device):
+    """Two graphs whose products split K, replayed in turn on one workspace; and a third that makes a workspace of its own each time."""
+    rows, n, k = 64, 512, 8192
+    assert api.plan_q8_gemm(rows, n, k)["splits"] > 1
+    made = []
+    for i in range(2):
+        g = _gen(i, 23)
+        (q, s), (c, w) = _coded(g, rows, k), _coded(g, n, k)
+        made.append((api.Q8Weight(c.to(device), w.to(device)), q.to(device), s.to(device)))
+    ws = made[0][0].workspace(rows)
+    want = [api.dlm_q8_gemm(*m, dtype=F32) for m in made]
+    outs = [torch.empty_like(y) for y in want + want[:1]]
+    graphs = []
+    torch.cuda.synchronize()
+    for i, m in enumerate(made + made[:1]):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            api.dlm_q8_gemm(*m, out=outs[i], workspace=ws if i < 2 else None)
+    for _ in range(4):
+        for y in outs:
+            y.fill_(7)
+        for graph in graphs:
+            graph.replay()
+        api.dlm_q8_gemm(*made[0], workspace=ws)
+        torch.cuda.synchronize()
+        for y, z in zip(outs, want + want[:1]):
+            assert torch.equal(y, z)
+    assert int(ws[:1024].max()) == 0
+
+
+def test_rows_far_apart(device):
+    """A stride whose tiles would be past 32 bits."""
+    rows, k, stride = 150, 100, (1 << 22) + 16
+    g = _gen(29)
+    (q, s), (c, w) = _coded(g, rows, k), _coded(g, 70, k)
+    far = torch.zeros(rows * stride, dtype=I8, device=device).as_strided((rows, k), (stride, 1))
+    far.copy_(q)
+    weight = api.Q8Weight(_columns(c, device)[0], w.to(device))
+    assert torch.equal(api.dlm_q8_gemm(weight, far, s.to(device), dtype=F32), api.dlm_q8_gemm(weight, _columns(q, device)[0], s.to(device), dtype=F32))
+
+
 def test_two_streams_with_a_workspace_each(device):
-    layers = [Layer(device, 300, 512, 1536, seed) for seed in (1, 2)]
+    layers = [Layer(device, 64, 512, 4096, seed) for seed in (1, 2)]
+    assert layers[0].ws[1] is not None
     want = [L.run().clone() for L in layers]
     torch.cuda.synchronize()
     streams = [torch.cuda.Stream() for _ in layers]

@@ -107,12 +107,39 @@ def test_gemm_refusals():
     assert call(rows=0) == 0 and call(_weight(gated=1), os=32, rows=0) == 0
     n, k = 4096, 12288
     for rows in (1, 100, 486):
-        need = api.lib().dlm_q8_gemm_workspace(rows, n, k, 0)
+        need = api.plan_q8_gemm(rows, n, k)["workspace_kib"] << 10
+        assert need <= api.lib().dlm_q8_gemm_workspace(rows, n, k, 0)
         if need:
             big = _weight(n, k)
             args = dict(w=big, stride=k, os=n, rows=rows)
             assert call(**args) == call(ws=S, size=need - 16, **args) == ECAPACITY and "workspace" in _err()
             assert call(ws=P, size=need, **args) == call(ws=R, size=need, **args) == call(ws=T, size=need, **args) == EINVAL and "workspace" in _err()
+
+
+def test_plans():
+    """What is asked for is what is launched; a workspace for more rows serves fewer."""
+    f = api.lib().dlm_plan_q8_gemm
+    out = (C.c_int32 * 6)()
+    assert f(8, 64, 64, 0, None) == EINVAL and f(8, 64, 64, 2, out) == EINVAL
+    for bad in ((0, 64, 64), (8, 0, 64), (8, 64, 131072), ((1 << 20) + 1, 64, 64)):
+        assert f(*bad, 0, out) == ESHAPE
+    for n, k, gated in ((4096, 12288, False), (640, 131071, False), (1000, 3000, True), (12288, 4096, False), (33, 65, False), (8232, 16400, False), (30000, 131071, False)):
+        for rows in (1, 16, 17, 32, 33, 64, 96, 130, 194, 300, 700, 2000, 20000):
+            p = api.plan_q8_gemm(rows, n, k, gated)
+            assert (p["kernel"] == "tiled" or rows <= 32) and p["splits"] >= 1 and p["workgroups"] >= p["splits"]
+            assert (p["workspace_kib"] > 0) == (p["splits"] > 1)
+            for more in (rows, rows + 1, rows + 500):
+                assert p["workspace_kib"] << 10 <= api.lib().dlm_q8_gemm_workspace(more, n, k, int(gated))
+
+
+def test_every_variant_is_reached_by_a_test():
+    from test_gpu_q8 import VARIANTS
+
+    have = {(p["kernel"], p["rows"], p["cols"], p["splits"] > 1) for p in (api.plan_q8_gemm(*v) for v in VARIANTS)}
+    split = {(32, 64), (32, 128), (32, 160), (64, 64), (64, 128), (64, 160), (96, 128), (96, 192), (128, 128), (128, 256), (160, 160)}
+    tiles = split | {(128, 384), (192, 256), (192, 384), (256, 256)}
+    assert have == {("tiled", *t, False) for t in tiles} | {("tiled", *t, True) for t in split} | \
+        {("streamed", 16, c, False) for c in (16, 32, 48)} | {("streamed", 32, c, False) for c in (16, 32)}
 
 
 def test_python_refusals(monkeypatch):
