@@ -28,16 +28,44 @@ template <> struct V8<float> {
   __device__ inline void set(int i, float x) { v[i >> 2][i & 3] = x; }
   __device__ inline void store(float* p) const { *(f32x4*)p = v[0]; *(f32x4*)(p + 4) = v[1]; }
 };
-// The code of t where the row's largest magnitude is top: inv = 127 / top in fp32
-__device__ inline int code(float t, float top, float inv) {
-  const float q = t * inv, k = rintf(q), r = q - k;
-  int c = (int)k;
-  if (fabsf(r) > 0.4999f) {
-    const double border = (double)k + (r > 0.f ? 0.5 : -0.5), e = fma(-border, (double)top, 127.0 * (double)t);
-    const int below = (int)floor(border);
-    c = e > 0.0 ? below + 1 : e < 0.0 ? below : below + (below & 1);
+// The code of t where the row's largest magnitude is top, in the low byte: inv is 127 / top rounded up to fp32.  Added to 1.5 2^23 a product is rounded to an
+// integer; what that leaves of t inv (at most 127 x 2^-23 of which is inv's rounding) says whether the quotient may be on the other side of a border
+constexpr float SHIFT = 12582912.f, NEAR = 0.49998f;
+__device__ inline unsigned rounded(float t, float inv, float* left) {
+  const float f = fmaf(t, inv, SHIFT);
+  *left = fmaf(t, inv, SHIFT - f);
+  return __float_as_uint(f);
+}
+__device__ inline unsigned exact_code(unsigned f, float left, float t, float top) {
+  const float k = __uint_as_float(f) - SHIFT;
+  const double border = (double)k + (left > 0.f ? 0.5 : -0.5), e = fma(-border, (double)top, 127.0 * (double)t);
+  const int below = (int)k - (left > 0.f ? 0 : 1);
+  return (unsigned)(e > 0.0 ? below + 1 : e < 0.0 ? below : below + (below & 1));
+}
+// ... of eight, with one check for all.  t = +-top / 2, which one in 600 bf16 values is, is the border 63.5 itself: it belongs to 64, where a product that is
+// no smaller than the quotient takes it.  One in 25000 others is looked at in 64 bits.
+__device__ inline uint64_t codes8(const float (&t)[8], float top, float inv) {
+  unsigned y[8];
+  float left[8], most = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    y[i] = rounded(t[i], inv, &left[i]);
+    most = fmaxf(most, fabsf(left[i]));
   }
-  return c;
+  if (most > NEAR) {
+    most = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = fmaxf(most, fabsf(t[i]) == 0.5f * top ? 0.f : fabsf(left[i]));
+    if (most > NEAR)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (fabsf(left[i]) > NEAR) y[i] = exact_code(y[i], left[i], t[i], top);
+  }
+  unsigned w[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    w[i] = __builtin_amdgcn_perm(y[4 * i + 1], y[4 * i], 0x0c0c0400u) | __builtin_amdgcn_perm(y[4 * i + 3], y[4 * i + 2], 0x04000c0cu);
+  return (uint64_t)w[1] << 32 | w[0];
 }
 
 // T threads a row; a thread keeps ITERS times eight values, T x 8 of the row apart.  LOOP: rows of any length, read (or, of a sum, read back from h)
@@ -148,13 +176,20 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void q8_rows_kernel(const TX* x,
     const float s = NORM && a > 0.f ? a * rsqrtf(ss / (float)width + eps) / 127.f : a / 127.f;
     scale[row] = bad ? __builtin_nanf("") : s;
   }
-  // a row of zeros: every quotient 0 x 0; a tiny maximum: its quotient would be past fp32's range, so the row is scaled by a power of two first
-  const float up = a < 0x1p-60f ? 0x1p64f : 1.f, big = a * up, inv = bad || big == 0.f ? 0.f : 127.f / big;
-  auto put = [&](int d, const float (&v)[8]) __attribute__((always_inline)) {
-    union { signed char c[8]; uint64_t w; } o;
+  // a row of zeros: every quotient 0 x 0; a tiny maximum: 127 / max would be past fp32's range, so the row is scaled by a power of two first
+  const bool tiny = a < 0x1p-100f;
+  const float big = tiny ? a * 0x1p64f : a;
+  float inv = 0.f;
+  if (!bad && big != 0.f) {
+    inv = 127.f / big;
+    if (fmaf(inv, big, -127.f) < 0.f) inv = __uint_as_float(__float_as_uint(inv) + 1);
+  }
+  auto put = [&](int d, float (&v)[8]) __attribute__((always_inline)) {
+    if (tiny)  // (the whole row)
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.c[i] = (signed char)(bad ? 0 : code(v[i] * up, big, inv));
-    *(uint64_t*)(pc + d) = o.w;
+      for (int i = 0; i < 8; ++i) v[i] *= 0x1p64f;
+    const uint64_t w = codes8(v, big, inv);
+    *(uint64_t*)(pc + d) = bad || big == 0.f ? 0 : w;
   };
   if (LOOP) {
     for (int d = d0; d < whole; d += STEP) {
@@ -166,7 +201,13 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void q8_rows_kernel(const TX* x,
     for (int j = 0; j < ITERS; ++j)
       if (d0 + j * STEP < whole) put(d0 + j * STEP, t[j]);
   }
-  if (odd) pc[e] = (int8_t)(bad ? 0 : code(ot * up, big, inv));
+  if (odd) {
+    const float v = tiny ? ot * 0x1p64f : ot;
+    float left;
+    unsigned f = rounded(v, inv, &left);
+    if (fabsf(left) > NEAR) f = exact_code(f, left, v, big);
+    pc[e] = (int8_t)(bad || big == 0.f ? 0 : f);
+  }
 }
 
 template <typename TX, typename TH, bool NORM, bool RES>
