@@ -40,10 +40,10 @@ void launch_q8_pack(const int8_t* codes, int64_t stride, const float* scale, con
 }
 
 // The tile and K split with the least estimated time.  A round is what 256 compute units take together.  A k-tile takes what a workgroup alone on the chip
-// takes (ns), or what the chip's power leaves the matrix cores (2.7 PFLOP/s), what the L2s (23.7 TB/s) or, for W, HBM (6.0 TB/s, shared by up to 8
+// takes (ns), or what the chip's power leaves the matrix cores (2.8 POP/s), what the L2s (22.7 TB/s) or, for W, HBM (5.7 TB/s, shared by up to 8
 // row blocks) give to all of the round's workgroups, whichever is most, joined by a 4-norm; a round pays for its copies' start and its
 // epilogue; a K split adds the hand-off, the partial tiles' traffic, and those that the last workgroup reads.  Constants fitted to the launches named
-// at Q8_TILES: 9 % off in the mean square.
+// at Q8_TILES: 9 % off in the root mean square.
 Q8TilePlan q8_tile_plan(int M, int units, int K) {
   struct Shape {
     int frags, bm, un, kb, first_loads;  // first_loads: copies of a wavefront before the loop
@@ -55,7 +55,7 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
     const int bm = 32 * rw * wm, un = cw * wn, loads = un * kb * 2 + bm * kb / 16, lps = (loads + rw * cw - 1) / (rw * cw), fit = 160 / loads, count = 63 / lps + 1;
     const int stages = fit < count ? (fit < 6 ? fit : 6) : (count < 6 ? count : 6);
     auto p4 = [](float x) { return x * x * x * x; };
-    return Shape{wm * wn, bm, un, kb, lps * stages, p4(ns), p4(bm * un * 32 * 128 * CUS / 2.73e6f) + p4((bm + un * 32) * 64 * CUS / 23.7e3f), un * 2048 * CUS / 6.0e3f};
+    return Shape{wm * wn, bm, un, kb, lps * stages, p4(ns), p4(bm * un * 32 * 128 * CUS / 2.8e6f) + p4((bm + un * 32) * 64 * CUS / 22.7e3f), un * 2048 * CUS / 5.7e3f};
   };
   static const Shape shapes[] = {Q8_TILES(ROW)};
 #undef ROW
@@ -75,8 +75,8 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
       if ((stages + per - 1) / per != sp) continue;  // (a split without stages)
       const int64_t all = wgs * sp, full = (all - 1) / 256;
       const float last = (all - 256 * full) / CUS;
-      float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 0.6f + 0.057f * t.first_loads + (full + last) * 1.5e-4f * out + (full + 1) * 9.3e-3f * edge;
-      if (sp > 1) us += 2.3f + out * 4e-3f * ((sp - 1) * 9.8e-3f + all * 1.64e-4f);
+      float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 1.1f + 0.028f * t.first_loads + (full + last) * 1.3e-4f * out + (full + 1) * 9.3e-3f * edge;
+      if (sp > 1) us += 2.3f + out * 4e-3f * ((sp - 1) * 9.7e-3f + all * 1.7e-4f);
       if (us < best.us) best = Q8TilePlan{i, t.bm, t.un * 32, nb, mb, sp, per, sp > 1 ? Q8_SPLIT_WGS * 4 + (size_t)all * t.bm * t.un * 128 : 0, us};
     }
   }

@@ -35,11 +35,11 @@ template <int WM, int WN, int RW, int CW, int KB>
 struct Q8Tile {
   static constexpr int NW = RW * CW, TPB = NW * 64, BM = 32 * RW * WM, UN = CW * WN;  // rows of X, units of W
   static constexpr int W_LOADS = UN * KB * 2, X_LOADS = BM * KB / 16;                 // of 1 KiB, a stage
-  static constexpr int LPS = (W_LOADS + X_LOADS + NW - 1) / NW;                       // ... of a wavefront (surplus ones repeat the last)
+  static constexpr int LPS = (W_LOADS + X_LOADS + NW - 1) / NW;                       // ... of a wavefront (some have surplus ones)
   static constexpr int W_BYTES = W_LOADS * 1024, STAGE = W_BYTES + X_LOADS * 1024;
   static constexpr int S_FIT = 160 * 1024 / STAGE, S_CNT = 63 / LPS + 1, S_ = S_FIT < S_CNT ? S_FIT : S_CNT, S = S_ > 6 ? 6 : S_;
   static constexpr int LDS_BYTES = S * STAGE;
-  static_assert(W_LOADS % NW == 0 && (KB == 1 || X_LOADS % NW == 0) && S >= 2 && (KB == 1 || KB == 2) && LDS_BYTES <= 160 * 1024, "tile shape");
+  static_assert(W_LOADS % NW == 0 && X_LOADS % 2 == 0 && S >= 2 && (KB == 1 || KB == 2) && LDS_BYTES <= 160 * 1024, "tile shape");
 };
 
 template <int WM, int WN, int RW, int CW, int KB, bool NT>
@@ -69,28 +69,30 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
   const __amdgpu_buffer_rsrc_t wr = __builtin_amdgcn_make_buffer_rsrc((void*)(wt + (int64_t)u0 * KTP * 2048), 0, nunits * KTP * 2048, 0x00020000);
   const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc((void*)(x + (int64_t)m0 * x_stride), 0, (mrows - 1) * x_stride + (K + 15) / 16 * 16, 0x00020000);
   constexpr int CPR = 4 * KB, RPL = 64 / CPR;  // chunks of a row, rows of a load
+  auto load_of = [&](int i) { const int f = i * NW + wave; return f < LOADS ? f : LOADS - 2 + (f & 1); };  // (surplus ones repeat one of the last two)
   int off[LPS];
 #pragma unroll
   for (int i = 0; i < LPS; ++i) {
-    const int f = min(i * NW + wave, LOADS - 1);
+    const int f = load_of(i);
     if (i * NW < W_LOADS) {
       off[i] = min(f / (2 * KB), nunits - 1) * (KTP * 2048) + f % (2 * KB) * 1024 + lane * 16;
     } else {
       off[i] = min((f - W_LOADS) * RPL + lane / CPR, mrows - 1) * x_stride;
     }
   }
-  const int my_row = (wave * RPL + lane / CPR) & 15;  // (of 16: the same in all of a lane's loads, or NW is odd)
-  static_assert(NW * RPL % 16 == 0 && W_LOADS % NW == 0, "a lane's rows are congruent mod 16");
-  const int my_chunk = ((lane % CPR) ^ (KB == 2 ? my_row >> 1 : my_row >> 2)) * 16;
+  // (a load's rows begin at a multiple of RPL: their numbers mod 16 are a lane's own, or one of two where RPL is 8)
+  auto chunk_of = [&](int odd) { const int row = odd * 8 + lane / CPR; return ((lane % CPR) ^ (KB == 2 ? row >> 1 : row >> 2)) * 16; };
+  const int my_chunk = chunk_of(RPL == 8 ? wave & 1 : 0), other_chunk = my_chunk ^ 64;  // (of the loads i NW + wave with i NW even, and odd)
+  static_assert(W_LOADS % 2 == 0, "X's loads are counted from an even number");
   const int k_last = (K + 15) / 16 * 16 - 16;
   auto issue = [&](int s, int buf, int lo, int hi) __attribute__((always_inline)) {
     const int t = s0 + min(s, nst - 1);
-    const int chunk = min(my_chunk, k_last - t * (64 * KB));
+    const int left = k_last - t * (64 * KB), chunk = min(my_chunk, left), chunk2 = min(other_chunk, left);
 #pragma unroll
     for (int i = lo; i < hi; ++i) {
-      unsigned char* dst = lds + buf * STAGE + min(i * NW + wave, LOADS - 1) * 1024;
+      unsigned char* dst = lds + buf * STAGE + load_of(i) * 1024;
       if (i * NW < W_LOADS) copy_to_lds<NT>(wr, dst, off[i], t * (KB * 2048));
-      else copy_to_lds<false>(xr, dst, off[i] + chunk, t * (64 * KB));
+      else copy_to_lds<false>(xr, dst, off[i] + (RPL == 8 && (i * NW) % 2 ? chunk2 : chunk), t * (64 * KB));
     }
   };
 

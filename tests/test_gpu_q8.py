@@ -230,11 +230,11 @@ def test_wide_product(device, dtype, rows, n, k, gated):
 
 
 # shapes whose plain product is a launch of each streamed form and of each tile, with and without a K split
-VARIANTS = [(8, 64, 128), (8, 5000, 128), (8, 10000, 128), (24, 64, 128), (24, 5000, 128),
-            (35, 6256, 4100), (43, 182, 4100), (66, 9206, 1300), (69, 3025, 4100), (66, 9211, 128), (1847, 141, 8200), (39, 341, 128), (34, 2020, 4100), (34, 17358, 128),
-            (168, 2712, 4100), (33, 30191, 128), (2624, 157, 16400), (66, 20747, 128), (69, 5543, 16400), (65, 33241, 128), (280, 3626, 8200), (194, 10396, 128),
-            (198, 4169, 8200), (195, 16557, 128), (194, 8232, 16400), (195, 33691, 128), (129, 25332, 128), (129, 16768, 8200), (165, 27676, 128), (321, 33667, 128),
-            (394, 24874, 128)]
+VARIANTS = [(8, 64, 128), (8, 5000, 128), (8, 10000, 128), (24, 64, 128), (24, 5000, 128), (88, 82, 256), (46, 65, 4100), (66, 9211, 128), (69, 3025, 4100),
+            (68, 10941, 128), (1847, 141, 8200), (121, 84, 128), (33, 3051, 4100), (33, 16973, 128), (1648, 70, 16400), (65, 16768, 128), (2257, 131, 8200),
+            (66, 20747, 128), (72, 5447, 8200), (65, 33241, 128), (268, 3622, 16400), (98, 20570, 128), (198, 4169, 8200), (98, 33516, 128),
+            (194, 8232, 16400), (194, 33018, 128), (130, 29642, 128), (305, 5395, 16400), (133, 16522, 128), (153, 5611, 16400), (165, 33014, 128),
+            (291, 33266, 128), (394, 24874, 128)]
 
 
 @pytest.mark.parametrize("gated", [False, True])
