@@ -773,7 +773,7 @@ class Q8Weight:
     def workspace(self, rows):
         """A new workspace for products of up to `rows` rows, or None where they need none."""
         size = lib().dlm_q8_gemm_workspace(rows, self.n, self.k, int(self.gated)) if 0 < rows < 2**31 else 0
-        return torch.zeros(size, dtype=torch.uint8, device=self._data.device) if size else None
+        return torch.empty(size, dtype=torch.uint8, device=self._data.device) if size else None
 
 
 def dlm_q8_gemm(weight, x, x_scale, out=None, dtype=torch.bfloat16, workspace=None):

@@ -31,6 +31,28 @@ __global__ __launch_bounds__(256) void q8_pack_scale_kernel(const float* __restr
   out[i] = channel < n ? scale[channel] : 0.f;
 }
 
+// The sums of a launch that splits K, added up and finished: a wavefront has a unit's 32 packed rows of 32 tokens
+__global__ __launch_bounds__(256) void q8_join_kernel(const i32x4* __restrict__ parts, int splits, int M, int units, const float* __restrict__ wscale, const float* __restrict__ x_scale,
+                                                      void* __restrict__ out, int64_t out_stride, int outputs, int form) {
+  const int lane = threadIdx.x & 63, blocks = (M + 31) >> 5, frag = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (frag >= units * blocks) return;
+  const int u = frag / blocks, m = (frag - u * blocks) * 32 + (lane & 31);
+  const i32x4* from = parts + (int64_t)frag * 256 + lane;
+  i32x4 t[4];
+#pragma unroll
+  for (int a = 0; a < 4; ++a) t[a] = from[a * 64];
+#pragma unroll 4
+  for (int sp = 1; sp < splits; ++sp) {
+    from += (int64_t)units * blocks * 256;
+#pragma unroll
+    for (int a = 0; a < 4; ++a) t[a] += from[a * 64];
+  }
+  const float xs = x_scale[min(m, M - 1)];
+  with_form(form, out, [&](auto gated, auto* to) __attribute__((always_inline)) {
+    finish16<decltype(gated)::value>(t, xs, wscale, to + (int64_t)m * out_stride, u, lane >> 5, outputs, m < M);
+  });
+}
+
 }  // namespace
 
 void launch_q8_pack(const int8_t* codes, int64_t stride, const float* scale, const Q8View& w, void* data, hipStream_t st) {
@@ -39,24 +61,28 @@ void launch_q8_pack(const int8_t* codes, int64_t stride, const float* scale, con
   q8_pack_scale_kernel<<<(w.units * 32 + 255) / 256, 256, 0, st>>>(scale, w.n, w.gated, w.units, (float*)w.scale);
 }
 
+void launch_q8_join(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
+  q8_join_kernel<<<(w.units * ((a.M + 31) / 32) + 3) / 4, 256, 0, st>>>((const i32x4*)a.workspace, p.splits, a.M, w.units, w.scale, a.x_scale, a.out, a.out_stride, w.outputs(),
+                                                                        out_form(w, a));
+}
+
 // The tile and K split with the least estimated time.  A round is what 256 compute units take together.  A k-tile takes what a workgroup alone on the chip
-// takes (ns), or what the chip's power leaves the matrix cores (2.8 POP/s), what the L2s (22.7 TB/s) or, for W, HBM (5.7 TB/s, shared by up to 8
+// takes (ns), or what the chip's power leaves the matrix cores (3.3 POP/s), what the L2s (19 TB/s) or, for W, HBM (5.5 TB/s, shared by up to 8
 // row blocks) give to all of the round's workgroups, whichever is most, joined by a 4-norm; a round pays for its copies' start and its
-// epilogue; a K split adds the hand-off, the partial tiles' traffic, and those that the last workgroup reads.  Constants fitted to the launches named
+// epilogue; a K split adds a launch, and the sums' way to memory and back.  Constants fitted to the launches named
 // at Q8_TILES: 9 % off in the root mean square.
 Q8TilePlan q8_tile_plan(int M, int units, int K) {
   struct Shape {
-    int frags, bm, un, kb, first_loads;  // first_loads: copies of a wavefront before the loop
-    float ns_4, chip_4, hbm;             // 4th powers of ns, and of what power and the L2s allow on a full chip; ns that HBM allows where one row block reads W
+    int bm, un, kb;
+    float ns_4, chip_4, hbm;  // 4th powers of ns, and of what power and the L2s allow on a full chip; ns that HBM allows where one row block reads W
   };
   constexpr float CUS = 256.f;
-#define ROW(WM, WN, RW, CW, KB, NT, NS) q8_shape(WM, WN, RW, CW, KB, NS),
-  static const auto q8_shape = [](int wm, int wn, int rw, int cw, int kb, float ns) {
-    const int bm = 32 * rw * wm, un = cw * wn, loads = un * kb * 2 + bm * kb / 16, lps = (loads + rw * cw - 1) / (rw * cw), fit = 160 / loads, count = 63 / lps + 1;
-    const int stages = fit < count ? (fit < 6 ? fit : 6) : (count < 6 ? count : 6);
+  static const auto shape = [](int wm, int wn, int rw, int cw, int kb, float ns) {
+    const int bm = 32 * rw * wm, un = cw * wn;
     auto p4 = [](float x) { return x * x * x * x; };
-    return Shape{wm * wn, bm, un, kb, lps * stages, p4(ns), p4(bm * un * 32 * 128 * CUS / 2.8e6f) + p4((bm + un * 32) * 64 * CUS / 22.7e3f), un * 2048 * CUS / 5.7e3f};
+    return Shape{bm, un, kb, p4(ns), p4(bm * un * 32 * 128 * CUS / 3.33e6f) + p4((bm + un * 32) * 64 * CUS / 19.0e3f), un * 2048 * CUS / 5.5e3f};
   };
+#define ROW(WM, WN, RW, CW, KB, NT, NS) shape(WM, WN, RW, CW, KB, NS),
   static const Shape shapes[] = {Q8_TILES(ROW)};
 #undef ROW
   const int KT = (K + 63) / 64;
@@ -69,15 +95,15 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
     const float out = t.bm * t.un * 32.f, edge = t.bm + t.un * 32.f, hbm = t.hbm / (mb < 8 ? mb : 8), full_4 = t.chip_4 + hbm * hbm * hbm * hbm;
     auto ns = [&](float share) { return sqrtf(sqrtf(t.ns_4 + full_4 * (share * share) * (share * share))); };
     const int64_t wgs = (int64_t)mb * nb;
-    for (int sp = 1; sp <= (t.frags <= Q8_SPLIT_FRAGS ? Q8_MAX_SPLITS : 1); ++sp) {
+    for (int sp = 1; sp <= Q8_MAX_SPLITS; ++sp) {
       if (sp > 1 && (wgs * sp > Q8_SPLIT_WGS || stages < 4 * sp)) break;
       const int per = (stages + sp - 1) / sp;
       if ((stages + per - 1) / per != sp) continue;  // (a split without stages)
       const int64_t all = wgs * sp, full = (all - 1) / 256;
       const float last = (all - 256 * full) / CUS;
-      float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 1.1f + 0.028f * t.first_loads + (full + last) * 1.3e-4f * out + (full + 1) * 9.3e-3f * edge;
-      if (sp > 1) us += 2.3f + out * 4e-3f * ((sp - 1) * 9.7e-3f + all * 1.7e-4f);
-      if (us < best.us) best = Q8TilePlan{i, t.bm, t.un * 32, nb, mb, sp, per, sp > 1 ? Q8_SPLIT_WGS * 4 + (size_t)all * t.bm * t.un * 128 : 0, us};
+      float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 2.4f + (full + last) * 1.76e-4f * out + (full + 1) * 5e-3f * edge;
+      if (sp > 1) us += 2.1f + sp * (0.1f + 7e-4f * units * ((M + 31) / 32));
+      if (us < best.us) best = Q8TilePlan{i, t.bm, t.un * 32, nb, mb, sp, per, sp > 1 ? (size_t)sp * units * ((M + 31) / 32) * 4096 : 0, us};
     }
   }
   return best;
@@ -117,8 +143,8 @@ Choice choose(int M, int units, int K, bool gated, int64_t x_stride) {
 }  // namespace
 
 size_t q8_gemm_workspace(int rows, int n, int k, int gated) {
-  // (a tile's plan depends on the rows through their blocks of 32, and one that splits K has at most Q8_SPLIT_WGS / 2 tiles, of at most 192 rows x 8 units)
-  const int units = q8_units(n, gated), most = 192 * (Q8_SPLIT_WGS / 2 / ((units + 7) / 8));
+  // (a tile's plan depends on the rows through their blocks of 32, and one that splits K has at most Q8_SPLIT_WGS / 2 tiles, of at most 256 rows or 12 units)
+  const int units = q8_units(n, gated), most = 256 * (Q8_SPLIT_WGS / 2 / ((units + 11) / 12));
   size_t bytes = 0;
   for (int m = 1; m <= rows && m <= most; m += 32) {
     const size_t need = q8_tile_plan(m, units, k).workspace;
@@ -149,4 +175,5 @@ void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, hipStream_t st) {
   const Choice c = choose(a.M, w.units, w.k, w.gated, a.x_stride);
   if (c.stream) return launch_q8_stream(w, a, c.s, st);
   c.t.rows >= 128 ? launch_q8_tiles<true>(w, a, c.t, st) : launch_q8_tiles<false>(w, a, c.t, st);
+  if (c.t.splits > 1) launch_q8_join(w, a, c.t, st);
 }

@@ -5,12 +5,12 @@
 // The shape of a tile {WM, WN, RW, CW, KB, NT, ns}: see q8_tile.h.  NT: a W that one row block reads is read non-temporally, past the memory-side cache, in
 // which the weights of a model do not stay from pass to pass (5 % of launches of up to 64 rows; nothing beyond).  ns: nanoseconds per k-tile of 64 that a workgroup alone on the
 // chip takes.  16 of 36 shapes that were timed (30000 launches: 29 row counts from 8 to 2822, 15 weights from 640 x 640 to 3584 x 18944), chosen by leaving out, one by
-// one, the shape whose absence costs least: what the planner takes is 1.8 % behind the best of these in the mean.
+// one, the shape whose absence costs least: what the planner takes is 1.5 % behind the best of these in the mean.
 #define Q8_TILES(X) \
-  X(4, 2, 2, 4, 1, false, 584) X(3, 3, 2, 4, 1, false, 651) X(3, 2, 2, 4, 1, false, 469) X(2, 3, 2, 4, 1, false, 476) \
-  X(2, 2, 2, 4, 2, false, 289) X(5, 1, 1, 6, 2, false, 345) X(3, 1, 2, 4, 2, false, 233) X(1, 2, 4, 2, 2, false, 203) \
-  X(3, 1, 1, 4, 2, false, 184) X(3, 1, 1, 8, 2, false, 246) X(1, 1, 2, 5, 2, true, 180) X(1, 1, 2, 4, 2, true, 158) \
-  X(1, 1, 2, 2, 2, true, 132) X(1, 1, 1, 5, 1, true, 180) X(1, 1, 1, 4, 2, true, 132) X(1, 1, 1, 2, 2, true, 117)
+  X(4, 2, 2, 4, 1, false, 588) X(3, 3, 2, 4, 1, false, 622) X(3, 2, 2, 4, 1, false, 460) X(2, 3, 2, 4, 1, false, 464) \
+  X(2, 2, 2, 4, 2, false, 303) X(5, 1, 1, 6, 2, false, 349) X(3, 1, 2, 4, 2, false, 233) X(1, 2, 4, 2, 2, false, 198) \
+  X(3, 1, 1, 4, 2, false, 182) X(3, 1, 1, 8, 2, false, 245) X(1, 1, 2, 5, 2, true, 182) X(1, 1, 2, 4, 2, true, 155) \
+  X(1, 1, 2, 2, 2, true, 129) X(1, 1, 1, 5, 1, true, 180) X(1, 1, 1, 4, 2, true, 132) X(1, 1, 1, 2, 2, true, 117)
 // rows x packed rows: 256 x 256, 192 x 384, 192 x 256, 128 x 384, 128 x 256, 160 x 192, 192 x 128, 128 x 128, 96 x 128, 96 x 256, 64 x 160, 64 x 128, 64 x 64, 32 x 160,
 // 32 x 128, 32 x 64
 
@@ -19,15 +19,15 @@ struct Q8TilePlan {
   int rows, cols;  // of a tile
   int nblocks, mblocks;
   int splits, stages;  // workgroups that share a tile's K, and how many stages each has
-  size_t workspace;    // bytes of a launch that splits K: Q8_SPLIT_WGS counters (zeros before and after it), then a partial tile for each workgroup
+  size_t workspace;    // bytes: the sums of every split of a launch that splits K, 4 KiB a unit and 32 rows
   float us;            // estimated
 };
-// K is split only over tiles whose wavefronts have at most this many fragments (the last workgroup holds two tiles of them), in at most Q8_SPLIT_WGS
-// workgroups: one round, and a counter each
-constexpr int Q8_SPLIT_FRAGS = 6, Q8_SPLIT_WGS = 256, Q8_MAX_SPLITS = 8;
+constexpr int Q8_SPLIT_WGS = 256, Q8_MAX_SPLITS = 16;  // (a launch that splits K is one round)
 Q8TilePlan q8_tile_plan(int M, int units, int K);
 template <bool WIDE>
 void launch_q8_tiles(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);
+
+void launch_q8_join(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);  // behind one that splits K
 
 constexpr int Q8_STREAM_ROWS = 32;  // up to as many rows may be the streamed product's (q8_stream.h)
 struct Q8StreamPlan {

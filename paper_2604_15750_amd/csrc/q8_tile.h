@@ -21,16 +21,6 @@ __device__ inline void copy_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* d
   else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, lane_at, at, 0, 0);
 }
 
-// 16 bytes a lane at device scope (past the XCD's L2)
-constexpr int SC1 = 16;
-__device__ inline void store_device(char* base, int bytes, int at, i32x4 v) {
-  typedef unsigned u32x4_ __attribute__((ext_vector_type(4)));
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_, v), __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000), at, 0, SC1);
-}
-__device__ inline i32x4 load_device(const char* base, int bytes, int at) {
-  return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(__builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00020000), at, 0, SC1));
-}
-
 template <int WM, int WN, int RW, int CW, int KB>
 struct Q8Tile {
   static constexpr int NW = RW * CW, TPB = NW * 64, BM = 32 * RW * WM, UN = CW * WN;  // rows of X, units of W
@@ -45,7 +35,7 @@ struct Q8Tile {
 template <int WM, int WN, int RW, int CW, int KB, bool NT>
 __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kernel(const unsigned char* __restrict__ wt, const int8_t* __restrict__ x, int x_stride, int M, int K, int units,
                                                                       int nblocks, int mblocks, int splits, int split_stages, const float* __restrict__ wscale, const float* __restrict__ x_scale,
-                                                                      void* __restrict__ out, int64_t out_stride, int outputs, int form, int* counters) {
+                                                                      void* __restrict__ out, int64_t out_stride, int outputs, int form, i32x4* __restrict__ parts) {
   typedef Q8Tile<WM, WN, RW, CW, KB> SH;
   constexpr int NW = SH::NW, BM = SH::BM, UN = SH::UN, LPS = SH::LPS, STAGE = SH::STAGE, S = SH::S, W_LOADS = SH::W_LOADS, LOADS = W_LOADS + SH::X_LOADS;
   constexpr int STEPS = 2 * KB;  // of 32 k, a stage
@@ -173,45 +163,25 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last stages land before the workgroup's LDS is another's
 
-  if constexpr (WM * WN <= Q8_SPLIT_FRAGS) if (splits > 1) {
-    // K split: every workgroup but the one that finishes last leaves its sums in the workspace and raises the tile's count; the last adds them up (integers:
-    // in any order) and goes on.  The hand-off crosses XCDs, whose L2s are separate: sums and counts are written and read at device scope, and a wavefront's
-    // stores have been acknowledged before the barrier in front of the count, so neither side needs a fence and nobody waits for anybody.
-    int* s_last = (int*)lds;  // (the loop's LDS is quiet; more than it would not fit)
-    constexpr int PART = SH::BM * UN * 32 * 4;
-    auto part = [&](int sp) { return (char*)(counters + Q8_SPLIT_WGS) + (int64_t)(sp * tiles + tile) * PART; };
-    constexpr int F = WM * WN;
-    auto place = [&](int f, int a) { return (((wave * F + f) * 4 + a) * 64 + lane) * 16; };
-    {
-      char* mine = part(split);
+  auto sums = [&](int j, int i, i32x4 (&t)[4]) __attribute__((always_inline)) {
 #pragma unroll
-      for (int f = 0; f < F; ++f)
+    for (int a = 0; a < 4; ++a) t[a] = i32x4{acc[j][i][4 * a], acc[j][i][4 * a + 1], acc[j][i][4 * a + 2], acc[j][i][4 * a + 3]};
+  };
+  if (splits > 1) {  // K split: the sums go to the workspace, [split][unit][block of 32 rows][4][lane], which a second launch adds up and finishes
+    const int blocks = (M + 31) >> 5;
 #pragma unroll
-        for (int a = 0; a < 4; ++a) store_device(mine, PART, place(f, a), i32x4{acc[f / WM][f % WM][4 * a], acc[f / WM][f % WM][4 * a + 1], acc[f / WM][f % WM][4 * a + 2], acc[f / WM][f % WM][4 * a + 3]});
-    }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    if (tid == 0) {
-      const int last = __hip_atomic_fetch_add(counters + tile, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == splits - 1;
-      if (last) __hip_atomic_store(counters + tile, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // ready for the next launch
-      *s_last = last;
-    }
-    __syncthreads();
-    if (!*s_last) return;
-    asm volatile("" ::: "memory");
-    for (int sp = 0; sp < splits; ++sp) {
-      if (sp == split) continue;
-      const char* theirs = part(sp);
-      i32x4 t[F][4];
+    for (int j = 0; j < WN; ++j)
 #pragma unroll
-      for (int f = 0; f < F; ++f)
+      for (int i = 0; i < WM; ++i) {
+        const int u = u0 + wn * WN + j, block = (m0 >> 5) + wm * WM + i;
+        if (u >= units || block >= blocks) continue;
+        i32x4 t[4];
+        sums(j, i, t);
+        i32x4* to = parts + ((int64_t)split * units + u) * blocks * 256 + block * 256 + lane;
 #pragma unroll
-        for (int a = 0; a < 4; ++a) t[f][a] = load_device(theirs, PART, place(f, a));
-#pragma unroll
-      for (int f = 0; f < F; ++f)
-#pragma unroll
-        for (int v = 0; v < 16; ++v) acc[f / WM][f % WM][v] += t[f][v >> 2][v & 3];
-    }
+        for (int a = 0; a < 4; ++a) to[a * 64] = t[a];
+      }
+    return;
   }
 
   // ---- epilogue, straight from the accumulators: a lane has 16 packed rows of a token, neighbours in the output
@@ -220,22 +190,13 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
     for (int i = 0; i < WM; ++i) {
       const int m = m0 + (wm * WM + i) * 32 + r32;
       const float xs = x_scale[min(m, M - 1)];
-      auto* row = to + (int64_t)m * out_stride;
 #pragma unroll
       for (int j = 0; j < WN; ++j) {
         const int u = u0 + wn * WN + j;
         if (u >= units) continue;
-        f32x4 y[4];
-#pragma unroll
-        for (int a = 0; a < 4; ++a)
-          y[a] = scaled(i32x4{acc[j][i][4 * a], acc[j][i][4 * a + 1], acc[j][i][4 * a + 2], acc[j][i][4 * a + 3]}, xs, *(const f32x4*)(wscale + u * 32 + 8 * a + 4 * half));
-        if (m >= M) continue;
-        if constexpr (decltype(gated)::value) {
-          store8(row, 16 * u + 8 * half, outputs, gated_unit(y[0], y[2]), gated_unit(y[1], y[3]));
-        } else {
-          store8(row, 32 * u + 16 * half, outputs, y[0], y[1]);
-          store8(row, 32 * u + 16 * half + 8, outputs, y[2], y[3]);
-        }
+        i32x4 t[4];
+        sums(j, i, t);
+        finish16<decltype(gated)::value>(t, xs, wscale, to + (int64_t)m * out_stride, u, half, outputs, m < M);
       }
     }
   });
@@ -251,7 +212,7 @@ void launch_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipS
   }
   q8_tile_kernel<WM, WN, RW, CW, KB, NT><<<(p.nblocks * p.mblocks * p.splits + 7) / 8 * 8, SH::TPB, SH::LDS_BYTES, st>>>(
       w.codes, a.x, (int)a.x_stride, a.M, w.k, w.units, p.nblocks, p.mblocks, p.splits, p.stages, w.scale, a.x_scale, a.out, a.out_stride, w.outputs(), out_form(w, a),
-      (int*)a.workspace);
+      (i32x4*)a.workspace);
 }
 
 }  // namespace

@@ -230,11 +230,11 @@ def test_wide_product(device, dtype, rows, n, k, gated):
 
 
 # shapes whose plain product is a launch of each streamed form and of each tile, with and without a K split
-VARIANTS = [(8, 64, 128), (8, 5000, 128), (8, 10000, 128), (24, 64, 128), (24, 5000, 128), (88, 82, 256), (46, 65, 4100), (66, 9211, 128), (69, 3025, 4100),
-            (68, 10941, 128), (1847, 141, 8200), (121, 84, 128), (33, 3051, 4100), (33, 16973, 128), (1648, 70, 16400), (65, 16768, 128), (2257, 131, 8200),
-            (66, 20747, 128), (72, 5447, 8200), (65, 33241, 128), (268, 3622, 16400), (98, 20570, 128), (198, 4169, 8200), (98, 33516, 128),
-            (194, 8232, 16400), (194, 33018, 128), (130, 29642, 128), (305, 5395, 16400), (133, 16522, 128), (153, 5611, 16400), (165, 33014, 128),
-            (291, 33266, 128), (394, 24874, 128)]
+VARIANTS = [(8, 64, 128), (8, 5000, 128), (8, 10000, 128), (24, 64, 128), (24, 5000, 128), (87, 106, 128), (46, 65, 4100), (65, 7407, 128), (68, 2503, 4100),
+            (67, 11033, 128), (36, 8331, 128), (33, 2729, 4100), (33, 16973, 128), (2800, 91, 4100), (34, 33132, 128), (3000, 131, 4100), (65, 14393, 128),
+            (66, 2958, 8200), (65, 33241, 128), (260, 5378, 8200), (98, 20570, 128), (198, 2077, 8200), (195, 16557, 128), (197, 5550, 16400),
+            (194, 33018, 128), (130, 16868, 128), (292, 4025, 16400), (164, 16572, 128), (291, 3697, 8200), (165, 33014, 128), (321, 33667, 128),
+            (968, 9606, 128)]
 
 
 @pytest.mark.parametrize("gated", [False, True])
@@ -255,8 +255,10 @@ def test_every_variant(device, rows, n, k, gated):
     for dtype in (F32, BF16):
         out, wide = _columns(torch.full((rows, weight.outputs), 9.0, dtype=dtype), device)
         ws = weight.workspace(rows)
-        for _ in range(3):  # (a call finds what the one before left in the workspace)
+        for fill in (255, 127, None):  # (whatever a workspace holds)
             out.fill_(9)
+            if ws is not None and fill:
+                ws.fill_(fill)
             api.dlm_q8_gemm(weight, qd, s.to(device), out=out, workspace=ws)
         assert (np.abs(_np64(out) - want) <= off * (1 + 2.0 ** -7) + HALF_STEP[dtype] * np.abs(want) + 2.0 ** -149).all() and _untouched(wide, weight.outputs)
 
@@ -417,7 +419,6 @@ def test_captured_products_share_a_workspace_or_have_none_given(device):
         torch.cuda.synchronize()
         for y, z in zip(outs, want + want[:1]):
             assert torch.equal(y, z)
-    assert int(ws[:1024].max()) == 0
 
 
 def test_rows_far_apart(device):
