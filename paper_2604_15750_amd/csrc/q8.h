@@ -68,7 +68,4 @@ struct Q8GemmArgs {
   int out_dtype;
   void* workspace;
 };
-size_t q8_gemm_workspace(int rows, int n, int k, int gated);      // most bytes that a launch of up to that many rows needs
-size_t q8_gemm_need(const Q8View& w, const Q8GemmArgs& a);        // what this one needs
-void q8_gemm_describe(int rows, int n, int k, int gated, int32_t plan[6]);  // dlm_plan_q8_gemm
-void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, hipStream_t st);
+size_t q8_gemm_workspace(int rows, int n, int k, int gated);  // most bytes that a launch of up to that many rows needs

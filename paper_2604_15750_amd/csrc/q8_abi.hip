@@ -1,6 +1,6 @@
 // C ABI of the linear layers in 8-bit integers: argument validation.  No kernel code here.
 #include "abi_args.h"
-#include "q8.h"
+#include "q8_plan.h"
 
 namespace {
 
@@ -124,13 +124,14 @@ extern "C" int dlm_q8_gemm(const dlm_q8_weight* w, const int8_t* x, int64_t x_st
   const wide bytes = weight_bytes(view.n, view.k, view.gated);
   REQUIRE(!overlap(xr, to) && !overlap(out, to.span(), x_scale, (wide)rows * 4) && !overlap(out, to.span(), w->data, bytes), DLM_EINVAL, "%s: out overlaps an array of the call", name);
   const Q8GemmArgs args{x, x_stride, x_scale, rows, out, out_stride, out_dtype, workspace};
-  const size_t need = rows ? q8_gemm_need(view, args) : 0;
+  if (rows == 0) return DLM_OK;
+  const Q8Plan plan = q8_plan(rows, view.units, view.k, view.gated, x_stride);
+  const size_t need = plan.workspace;
   REQUIRE(!need || (workspace && workspace_bytes >= need), DLM_ECAPACITY, "%s: workspace of %zu bytes < %zu", name, workspace ? workspace_bytes : 0, need);
   REQUIRE(!need || !(overlap(workspace, need, x, xr.span()) || overlap(workspace, need, out, to.span()) || overlap(workspace, need, x_scale, (wide)rows * 4) ||
                      overlap(workspace, need, w->data, bytes)),
           DLM_EINVAL, "%s: the workspace overlaps an array of the call", name);
-  if (rows == 0) return DLM_OK;
-  launch_q8_gemm(view, args, (hipStream_t)stream);
+  launch_q8_gemm(view, args, plan, (hipStream_t)stream);
   DLM_HIP(hipGetLastError());
   return DLM_OK;
 }
@@ -139,6 +140,14 @@ extern "C" int dlm_plan_q8_gemm(int rows, int n, int k, int gated, int32_t plan[
   REQUIRE(plan, DLM_EINVAL, "dlm_plan_q8_gemm: null plan");
   REQUIRE(gated == 0 || gated == 1, DLM_EINVAL, "dlm_plan_q8_gemm: gated %d", gated);
   REQUIRE(rows >= 1 && rows <= 1 << 20 && weight_bytes(n, k, gated), DLM_ESHAPE, "dlm_plan_q8_gemm: %d rows, a weight of %d x %d", rows, n, k);
-  q8_gemm_describe(rows, n, k, gated, plan);
+  const int units = q8_units(n, gated), tile = rows <= 16 ? 16 : 32;
+  const Q8Plan p = q8_plan(rows, units, k, gated, 0);
+  if (p.streamed) {
+    const int32_t v[6] = {0, tile, 16 * p.stream.subs, 1, (2 * units + p.stream.subs - 1) / p.stream.subs * ((rows + tile - 1) / tile), 0};
+    for (int i = 0; i < 6; ++i) plan[i] = v[i];
+  } else {
+    const int32_t v[6] = {1, p.tile.rows, p.tile.cols, p.tile.splits, p.tile.nblocks * p.tile.mblocks * p.tile.splits, (int32_t)(p.tile.workspace >> 10)};
+    for (int i = 0; i < 6; ++i) plan[i] = v[i];
+  }
   return DLM_OK;
 }

@@ -123,24 +123,16 @@ Q8StreamPlan q8_stream_plan(int M, int units, int K, bool gated) {
   return best;
 }
 
-namespace {
-
 // Few rows are either's, whichever is estimated to take less; rows so far apart that a tile's would be past 32 bits are streamed, however many
-struct Choice {
-  bool stream;
-  Q8StreamPlan s;
-  Q8TilePlan t;
-};
-Choice choose(int M, int units, int K, bool gated, int64_t x_stride) {
-  Choice c{};
+Q8Plan q8_plan(int M, int units, int K, bool gated, int64_t x_stride) {
+  Q8Plan c{};
   const bool far = x_stride > 1 << 22;
-  if (M <= Q8_STREAM_ROWS || far) c.s = q8_stream_plan(M, units, K, gated);
-  if (!far) c.t = q8_tile_plan(M, units, K);
-  c.stream = far || (M <= Q8_STREAM_ROWS && c.s.us <= c.t.us);
+  if (M <= Q8_STREAM_ROWS || far) c.stream = q8_stream_plan(M, units, K, gated);
+  if (!far) c.tile = q8_tile_plan(M, units, K);
+  c.streamed = far || (M <= Q8_STREAM_ROWS && c.stream.us <= c.tile.us);
+  c.workspace = c.streamed ? 0 : c.tile.workspace;
   return c;
 }
-
-}  // namespace
 
 size_t q8_gemm_workspace(int rows, int n, int k, int gated) {
   // (a tile's plan depends on the rows through their blocks of 32, and one that splits K has at most Q8_SPLIT_WGS / 2 tiles, of at most 256 rows or 12 units)
@@ -153,27 +145,8 @@ size_t q8_gemm_workspace(int rows, int n, int k, int gated) {
   return bytes;
 }
 
-size_t q8_gemm_need(const Q8View& w, const Q8GemmArgs& a) {
-  const Choice c = choose(a.M, w.units, w.k, w.gated, a.x_stride);
-  return c.stream ? 0 : c.t.workspace;
-}
-
-void q8_gemm_describe(int rows, int n, int k, int gated, int32_t plan[6]) {
-  const int units = q8_units(n, gated);
-  const Choice c = choose(rows, units, k, gated, 0);
-  const int tile = rows <= 16 ? 16 : 32;
-  if (c.stream) {
-    const int32_t p[6] = {0, tile, 16 * c.s.subs, 1, (2 * units + c.s.subs - 1) / c.s.subs * ((rows + tile - 1) / tile), 0};
-    for (int i = 0; i < 6; ++i) plan[i] = p[i];
-  } else {
-    const int32_t p[6] = {1, c.t.rows, c.t.cols, c.t.splits, c.t.nblocks * c.t.mblocks * c.t.splits, (int32_t)(c.t.workspace >> 10)};
-    for (int i = 0; i < 6; ++i) plan[i] = p[i];
-  }
-}
-
-void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, hipStream_t st) {
-  const Choice c = choose(a.M, w.units, w.k, w.gated, a.x_stride);
-  if (c.stream) return launch_q8_stream(w, a, c.s, st);
-  c.t.rows >= 128 ? launch_q8_tiles<true>(w, a, c.t, st) : launch_q8_tiles<false>(w, a, c.t, st);
-  if (c.t.splits > 1) launch_q8_join(w, a, c.t, st);
+void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, const Q8Plan& c, hipStream_t st) {
+  if (c.streamed) return launch_q8_stream(w, a, c.stream, st);
+  c.tile.rows >= 128 ? launch_q8_tiles<true>(w, a, c.tile, st) : launch_q8_tiles<false>(w, a, c.tile, st);
+  if (c.tile.splits > 1) launch_q8_join(w, a, c.tile, st);
 }

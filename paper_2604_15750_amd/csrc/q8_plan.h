@@ -36,3 +36,12 @@ struct Q8StreamPlan {
 };
 Q8StreamPlan q8_stream_plan(int M, int units, int K, bool gated);
 void launch_q8_stream(const Q8View& w, const Q8GemmArgs& a, const Q8StreamPlan& p, hipStream_t st);
+
+struct Q8Plan {
+  bool streamed;
+  Q8StreamPlan stream;
+  Q8TilePlan tile;
+  size_t workspace;  // bytes that the launch needs
+};
+Q8Plan q8_plan(int M, int units, int K, bool gated, int64_t x_stride);
+void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, const Q8Plan& p, hipStream_t st);
