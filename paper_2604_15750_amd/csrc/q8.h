@@ -5,14 +5,14 @@
 // for K up to Q8_MAX_K.
 //
 // Packed weight: units of 32 channels ("packed rows" R = 0 .. 31) by 64 k, 2 KiB each, [unit][k-tile][sub][chunk][16 rows][16 bytes]: packed row
-// R = 16 sub + row, k = 64 k-tile + 16 chunk + byte.  A sub is one operand of a 16x16x64 product, lane by lane (row = lane % 16, chunk =
-// lane / 16), and both subs together are the two operands of 32x32x32 products.  Behind the codes lie the scales, [unit][R] fp32.
-// k-tiles come in pairs; channels and k's past the end are zeros, so that whatever stands behind the last k of a row of activations is multiplied by zero.
+// R = 16 sub + row, k = 64 k-tile + 16 chunk + byte.  A sub is one operand of a 16x16x64 product, lane by lane (row = lane % 16, chunk = lane / 16).  Behind the codes
+// lie the scales, [unit][R] fp32.  k-tiles come in pairs; channels and k's past the end are zeros, so that whatever stands behind the last k of a row of
+// activations is multiplied by zero.
 //
-// Which channel packed row R = 8a + 4b + c (a, c = 0..3, b = 0, 1) is: the products leave a lane 4 (16x16) or 16 (32x32: b = lane / 32) packed
-// rows of a token, and these are to be neighbours in the output:
-//   plain  channel 32 unit + 16b + 4a + c
-//   gated  a < 2: gate, a >= 2: up, of output 16 unit + 8b + 4 (a % 2) + c, so that a lane holds both parts of each of its outputs
+// Which channel packed row R = 16 s + 4 g + c (s = 0, 1; g, c = 0 .. 3) is: the products leave a lane of group g four packed rows of each sub, and these are
+// to be neighbours in the output:
+//   plain  channel 32 unit + 8 g + 4 s + c
+//   gated  s = 0: gate, s = 1: up, of output 16 unit + 4 g + c, so that a lane holds both parts of each of its outputs
 #pragma once
 #include "common.h"
 
@@ -34,10 +34,10 @@ __host__ __device__ inline int q8_units(int n, int gated) { return gated ? (n / 
 __host__ __device__ constexpr int q8_ktiles(int k) { return (k + 127) / 128 * 2; }
 // the channel of packed row R of a unit (n and more: none)
 __host__ __device__ inline int q8_channel(int unit, int R, int n, int gated) {
-  const int a = R >> 3, b = (R >> 2) & 1, c = R & 3;
-  if (!gated) return 32 * unit + 16 * b + 4 * a + c;
-  const int o = 16 * unit + 8 * b + 4 * (a & 1) + c;
-  return o >= n / 2 ? n : a < 2 ? o : n / 2 + o;
+  const int s = R >> 4, g = (R >> 2) & 3, c = R & 3;
+  if (!gated) return 32 * unit + 8 * g + 4 * s + c;
+  const int o = 16 * unit + 4 * g + c;
+  return o >= n / 2 ? n : s == 0 ? o : n / 2 + o;
 }
 
 struct Q8RowsArgs {

@@ -68,19 +68,13 @@ __device__ inline void with_form(int form, void* out, F f) {
   else f(std::true_type{}, (float*)out);
 }
 
-// The outputs of 16 packed rows of a unit and a token, as a 32x32 product leaves them to a lane (half: lane / 32): neighbours
+// The outputs of 4 packed rows of each sub of a unit and of a token, as 16x16 products leave them to a lane (g: lane / 16): neighbours
 template <bool GATED, typename TO>
-__device__ inline void finish16(const i32x4 (&sum)[4], float token, const float* wscale, TO* row, int u, int half, int outputs, bool there) {
-  f32x4 y[4];
-#pragma unroll
-  for (int a = 0; a < 4; ++a) y[a] = scaled(sum[a], token, *(const f32x4*)(wscale + u * 32 + 8 * a + 4 * half));
+__device__ inline void finish8(i32x4 first, i32x4 second, float token, const float* wscale, TO* row, int u, int g, int outputs, bool there) {
+  const f32x4 y0 = scaled(first, token, *(const f32x4*)(wscale + u * 32 + 4 * g)), y1 = scaled(second, token, *(const f32x4*)(wscale + u * 32 + 16 + 4 * g));
   if (!there) return;
-  if constexpr (GATED) {
-    store8(row, 16 * u + 8 * half, outputs, gated_unit(y[0], y[2]), gated_unit(y[1], y[3]));
-  } else {
-    store8(row, 32 * u + 16 * half, outputs, y[0], y[1]);
-    store8(row, 32 * u + 16 * half + 8, outputs, y[2], y[3]);
-  }
+  if constexpr (GATED) store4(row, 16 * u + 4 * g, outputs, gated_unit(y0, y1));
+  else store8(row, 32 * u + 8 * g, outputs, y0, y1);
 }
 
 }  // namespace

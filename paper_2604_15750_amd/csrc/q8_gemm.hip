@@ -36,7 +36,7 @@ __global__ __launch_bounds__(256) void q8_join_kernel(const i32x4* __restrict__ 
                                                       void* __restrict__ out, int64_t out_stride, int outputs, int form) {
   const int lane = threadIdx.x & 63, blocks = (M + 31) >> 5, frag = blockIdx.x * 4 + (threadIdx.x >> 6);
   if (frag >= units * blocks) return;
-  const int u = frag / blocks, m = (frag - u * blocks) * 32 + (lane & 31);
+  const int u = frag / blocks, m = (frag - u * blocks) * 32 + (lane & 15);
   const i32x4* from = parts + (int64_t)frag * 256 + lane;
   i32x4 t[4];
 #pragma unroll
@@ -47,9 +47,11 @@ __global__ __launch_bounds__(256) void q8_join_kernel(const i32x4* __restrict__ 
 #pragma unroll
     for (int a = 0; a < 4; ++a) t[a] += from[a * 64];
   }
-  const float xs = x_scale[min(m, M - 1)];
+  const float xs[2] = {x_scale[min(m, M - 1)], x_scale[min(m + 16, M - 1)]};
   with_form(form, out, [&](auto gated, auto* to) __attribute__((always_inline)) {
-    finish16<decltype(gated)::value>(t, xs, wscale, to + (int64_t)m * out_stride, u, lane >> 5, outputs, m < M);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      finish8<decltype(gated)::value>(t[2 * i], t[2 * i + 1], xs[i], wscale, to + (int64_t)(m + 16 * i) * out_stride, u, lane >> 4, outputs, m + 16 * i < M);
   });
 }
 
@@ -67,22 +69,22 @@ void launch_q8_join(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, h
 }
 
 // The tile and K split with the least estimated time.  A round is what 256 compute units take together.  A k-tile takes what a workgroup alone on the chip
-// takes (ns), or what the chip's power leaves the matrix cores (3.3 POP/s), what the L2s (19 TB/s) or, for W, HBM (5.5 TB/s, shared by up to 8
+// takes (ns), or what the chip's power leaves the matrix cores (3.7 POP/s in 16x16x64 products, 2.8 in 32x32x32), what the L2s (24 TB/s) or, for W, HBM (5.9 TB/s, shared by up to 8
 // row blocks) give to all of the round's workgroups, whichever is most, joined by a 4-norm; a round pays for its copies' start and its
 // epilogue; a K split adds a launch, and the sums' way to memory and back.  Constants fitted to the launches named
-// at Q8_TILES: 9 % off in the root mean square.
+// at Q8_TILES: 10 % off in the root mean square.
 Q8TilePlan q8_tile_plan(int M, int units, int K) {
   struct Shape {
     int bm, un, kb;
     float ns_4, chip_4, hbm;  // 4th powers of ns, and of what power and the L2s allow on a full chip; ns that HBM allows where one row block reads W
   };
   constexpr float CUS = 256.f;
-  static const auto shape = [](int wm, int wn, int rw, int cw, int kb, float ns) {
+  static const auto shape = [](int wm, int wn, int rw, int cw, int kb, int mf, float ns) {
     const int bm = 32 * rw * wm, un = cw * wn;
     auto p4 = [](float x) { return x * x * x * x; };
-    return Shape{bm, un, kb, p4(ns), p4(bm * un * 32 * 128 * CUS / 3.33e6f) + p4((bm + un * 32) * 64 * CUS / 19.0e3f), un * 2048 * CUS / 5.5e3f};
+    return Shape{bm, un, kb, p4(ns), p4(bm * un * 32 * 128 * CUS / (mf == 16 ? 3.7e6f : 2.8e6f)) + p4((bm + un * 32) * 64 * CUS / 24.3e3f), un * 2048 * CUS / 5.9e3f};
   };
-#define ROW(WM, WN, RW, CW, KB, NT, NS) shape(WM, WN, RW, CW, KB, NS),
+#define ROW(WM, WN, RW, CW, KB, MF, NT, NS) shape(WM, WN, RW, CW, KB, MF, NS),
   static const Shape shapes[] = {Q8_TILES(ROW)};
 #undef ROW
   const int KT = (K + 63) / 64;
@@ -101,8 +103,8 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
       if ((stages + per - 1) / per != sp) continue;  // (a split without stages)
       const int64_t all = wgs * sp, full = (all - 1) / 256;
       const float last = (all - 256 * full) / CUS;
-      float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 2.4f + (full + last) * 1.76e-4f * out + (full + 1) * 5e-3f * edge;
-      if (sp > 1) us += 2.1f + sp * (0.1f + 7e-4f * units * ((M + 31) / 32));
+      float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 2.2f + (full + last) * 1.25e-4f * out + (full + 1) * 7.3e-3f * edge;
+      if (sp > 1) us += 2.f + sp * (0.16f + 5.4e-4f * units * ((M + 31) / 32));
       if (us < best.us) best = Q8TilePlan{i, t.bm, t.un * 32, nb, mb, sp, per, sp > 1 ? (size_t)sp * units * ((M + 31) / 32) * 4096 : 0, us};
     }
   }

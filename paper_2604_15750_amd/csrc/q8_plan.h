@@ -2,16 +2,16 @@
 #pragma once
 #include "q8.h"
 
-// The shape of a tile {WM, WN, RW, CW, KB, NT, ns}: see q8_tile.h.  NT: a W that one row block reads is read non-temporally, past the memory-side cache, in
+// The shape of a tile {WM, WN, RW, CW, KB, MF, NT, ns}: see q8_tile.h.  NT: a W that one row block reads is read non-temporally, past the memory-side cache, in
 // which the weights of a model do not stay from pass to pass (5 % of launches of up to 64 rows; nothing beyond).  ns: nanoseconds per k-tile of 64 that a workgroup alone on the
-// chip takes.  16 of 36 shapes that were timed (30000 launches: 29 row counts from 8 to 2822, 15 weights from 640 x 640 to 3584 x 18944), chosen by leaving out, one by
-// one, the shape whose absence costs least: what the planner takes is 1.5 % behind the best of these in the mean.
+// chip takes.  16 of 60 shapes that were timed (29 row counts from 8 to 2822, 15 weights from 640 x 640 to 3584 x 18944, random codes), chosen by leaving out, one by
+// one, the shape whose absence costs least: what the planner takes is 2 % behind the best of these in the mean.
 #define Q8_TILES(X) \
-  X(4, 2, 2, 4, 1, false, 588) X(3, 3, 2, 4, 1, false, 622) X(3, 2, 2, 4, 1, false, 460) X(2, 3, 2, 4, 1, false, 464) \
-  X(2, 2, 2, 4, 2, false, 303) X(5, 1, 1, 6, 2, false, 349) X(3, 1, 2, 4, 2, false, 233) X(1, 2, 4, 2, 2, false, 198) \
-  X(3, 1, 1, 4, 2, false, 182) X(3, 1, 1, 8, 2, false, 245) X(1, 1, 2, 5, 2, true, 182) X(1, 1, 2, 4, 2, true, 155) \
-  X(1, 1, 2, 2, 2, true, 129) X(1, 1, 1, 5, 1, true, 180) X(1, 1, 1, 4, 2, true, 132) X(1, 1, 1, 2, 2, true, 117)
-// rows x packed rows: 256 x 256, 192 x 384, 192 x 256, 128 x 384, 128 x 256, 160 x 192, 192 x 128, 128 x 128, 96 x 128, 96 x 256, 64 x 160, 64 x 128, 64 x 64, 32 x 160,
+  X(4, 2, 2, 4, 2, 16, false, 586) X(3, 3, 2, 4, 1, 16, false, 675) X(3, 2, 2, 4, 2, 16, false, 506) X(2, 3, 2, 4, 1, 16, false, 499) \
+  X(2, 2, 2, 4, 2, 16, false, 325) X(5, 1, 1, 6, 2, 32, false, 348) X(5, 1, 1, 8, 2, 32, false, 351) X(3, 1, 2, 4, 2, 32, false, 231) \
+  X(1, 2, 4, 2, 2, 16, false, 202) X(3, 1, 1, 4, 2, 32, false, 190) X(1, 1, 2, 5, 2, 16, true, 173) X(1, 1, 2, 4, 2, 16, true, 149) \
+  X(1, 1, 2, 2, 2, 16, true, 121) X(1, 1, 1, 5, 1, 16, true, 151) X(1, 1, 1, 4, 2, 16, true, 128) X(1, 1, 1, 2, 2, 16, true, 114)
+// rows x packed rows: 256 x 256, 192 x 384, 192 x 256, 128 x 384, 128 x 256, 160 x 192, 160 x 256, 192 x 128, 128 x 128, 96 x 128, 64 x 160, 64 x 128, 64 x 64, 32 x 160,
 // 32 x 128, 32 x 64
 
 struct Q8TilePlan {

@@ -101,9 +101,9 @@ __global__ __launch_bounds__(64 * NWV) void q8_stream_kernel(const i32x4* __rest
         auto* row = to + (int64_t)m * out_stride;
         if constexpr (GATED) {
           const f32x4 gate = scaled(sum(c * MT + j), xs, channels(s)), up = scaled(sum((c + 1) * MT + j), xs, channels(s + 1));
-          store4(row, 8 * s + 8 * (g & 1) + 4 * (g >> 1), outputs, gated_unit(gate, up));
+          store4(row, 8 * s + 4 * g, outputs, gated_unit(gate, up));
         } else {
-          store4(row, 32 * (s >> 1) + 16 * (g & 1) + 8 * (s & 1) + 4 * (g >> 1), outputs, scaled(sum(c * MT + j), xs, channels(s)));
+          store4(row, 32 * (s >> 1) + 8 * g + 4 * (s & 1), outputs, scaled(sum(c * MT + j), xs, channels(s)));
         }
       }
     }

@@ -4,7 +4,10 @@
 //   * W's units lie in memory as the products take them, so a stage of them is copied to LDS as it is; X's rows are 64 KB bytes of each of the tile's
 //     rows, in 16-byte chunks whose place in the row is turned by the row's number, so that 16 lanes that read the same chunk of 16 rows
 //     meet 16 different banks' groups.  Both by direct-to-LDS loads, S stages of them in flight or in use;
-//   * a wavefront multiplies WM x WN fragments (v_mfma_i32_32x32x32_i8) of a step of 32 k while it reads the next step's from LDS;
+//   * a wavefront multiplies its fragments of a step while it reads the next step's from LDS.  MF = 16: v_mfma_i32_16x16x64_i8, a step of 64 k; MF = 32:
+//     v_mfma_i32_32x32x32_i8, a step of 32 k.  Operands, cycles and LDS reads are the same.  16x16x64 takes less power, which is what bounds launches that fill
+//     the chip (4096 x 8192 x 8192 in 256 x 256 tiles 233 us with MF = 32, 210 with 16); the smaller steps of 32 leave a stage's copies a quarter of a stage longer, which is
+//     worth more where W comes from HBM in tiles that are waited for (152 x 37888 x 3584 in 160 x 192 tiles 33.1 us, 37.5 with 16);
 //   * one barrier a stage, in front of its last step: by then every wavefront has the stage's last fragments in registers, and the copies of
 //     stage s + S go out over the steps that follow.
 #pragma once
@@ -32,13 +35,13 @@ struct Q8Tile {
   static_assert(W_LOADS % NW == 0 && X_LOADS % 2 == 0 && S >= 2 && (KB == 1 || KB == 2) && LDS_BYTES <= 160 * 1024, "tile shape");
 };
 
-template <int WM, int WN, int RW, int CW, int KB, bool NT>
-__global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kernel(const unsigned char* __restrict__ wt, const int8_t* __restrict__ x, int x_stride, int M, int K, int units,
+template <int WM, int WN, int RW, int CW, int KB, int MF, bool NT>
+__global__ __launch_bounds__(RW * CW * 64, RW * CW > 4 ? (RW * CW + 3) / 4 : 2) void q8_tile_kernel(const unsigned char* __restrict__ wt, const int8_t* __restrict__ x, int x_stride, int M, int K, int units,
                                                                       int nblocks, int mblocks, int splits, int split_stages, const float* __restrict__ wscale, const float* __restrict__ x_scale,
                                                                       void* __restrict__ out, int64_t out_stride, int outputs, int form, i32x4* __restrict__ parts) {
   typedef Q8Tile<WM, WN, RW, CW, KB> SH;
   constexpr int NW = SH::NW, BM = SH::BM, UN = SH::UN, LPS = SH::LPS, STAGE = SH::STAGE, S = SH::S, W_LOADS = SH::W_LOADS, LOADS = W_LOADS + SH::X_LOADS;
-  constexpr int STEPS = 2 * KB;  // of 32 k, a stage
+  constexpr int STEPS = MF == 16 ? KB : 2 * KB;  // of a stage
   extern __shared__ __align__(16) unsigned char lds[];
 
   // Workgroup id -> tile: ids congruent mod 8 share an XCD, which gets one contiguous eighth of the tiles; in groups of 8 row blocks, row blocks fastest, so that
@@ -86,28 +89,35 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
     }
   };
 
-  i32x16 acc[WN][WM];
+  constexpr int PER = MF == 16 ? 2 : 1, FM = PER * WM, FN = PER * WN;  // fragments of 16 or 32 rows
+  typedef typename std::conditional<MF == 16, i32x4, i32x16>::type Acc;
+  Acc acc[FN][FM];
+  i32x4 xf[2][FM], wf[2][FN];
 #pragma unroll
-  for (int j = 0; j < WN; ++j)
+  for (int j = 0; j < FN; ++j)
 #pragma unroll
-    for (int i = 0; i < WM; ++i)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) acc[j][i][v] = 0;
-  i32x4 xf[2][WM], wf[2][WN];
-  const int half = lane >> 5, r32 = lane & 31;
-  const int w_at = (r32 >> 4) * 1024 + half * 256 + (r32 & 15) * 16, turn = KB == 2 ? (r32 >> 1) & 7 : (r32 >> 2) & 3;
+    for (int i = 0; i < FM; ++i) acc[j][i] = Acc(0);
+  // lane -> row of a fragment, and which of a k-tile's chunks (of step q) it has
+  const int row = lane % MF, part = lane / MF, turn = KB == 2 ? (row >> 1) & 7 : (row >> 2) & 3;
+  const int w_at = MF == 16 ? lane * 16 : (row >> 4) * 1024 + part * 256 + (row & 15) * 16;
   auto read_frags = [&](int set, int buf, int q) __attribute__((always_inline)) {
     const unsigned char* st = lds + buf * STAGE;
 #pragma unroll
-    for (int j = 0; j < WN; ++j) wf[set][j] = *(const i32x4*)(st + ((wn * WN + j) * KB + (q >> 1)) * 2048 + (q & 1) * 512 + w_at);
+    for (int j = 0; j < FN; ++j) {
+      if constexpr (MF == 16) wf[set][j] = *(const i32x4*)(st + ((wn * WN + j / 2) * KB + q) * 2048 + (j & 1) * 1024 + w_at);
+      else wf[set][j] = *(const i32x4*)(st + ((wn * WN + j) * KB + (q >> 1)) * 2048 + (q & 1) * 512 + w_at);
+    }
 #pragma unroll
-    for (int i = 0; i < WM; ++i) xf[set][i] = *(const i32x4*)(st + SH::W_BYTES + ((wm * WM + i) * 32 + r32) * (64 * KB) + (((2 * q + half) ^ turn) << 4));
+    for (int i = 0; i < FM; ++i) xf[set][i] = *(const i32x4*)(st + SH::W_BYTES + (wm * WM * 32 + i * MF + row) * (64 * KB) + (((64 / MF * q + part) ^ turn) << 4));
   };
   auto multiply = [&](int set) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < WN; ++j)
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int i = 0; i < WM; ++i) acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[set][j], xf[set][i], acc[j][i], 0, 0, 0);
+      for (int i = 0; i < FM; ++i) {
+        if constexpr (MF == 16) acc[j][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[set][j], xf[set][i], acc[j][i], 0, 0, 0);
+        else acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[set][j], xf[set][i], acc[j][i], 0, 0, 0);
+      }
   };
 
   // stages 0 .. S - 2 and the first part of S - 1 go out at once; the rest of it during stage 0, as for every later stage
@@ -119,8 +129,9 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
   asm volatile("" ::: "memory");
   read_frags(0, 0, 0);
   __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
-  auto step = [&](auto Qc, int s, int buf, int nbuf) __attribute__((always_inline)) {
-    constexpr int Q = decltype(Qc)::value, SET = Q & 1;
+  // step Q of stage s (in LDS buffer buf), whose operands are in register set SET
+  auto step = [&](auto Qc, auto SETc, int s, int buf, int nbuf) __attribute__((always_inline)) {
+    constexpr int Q = decltype(Qc)::value, SET = decltype(SETc)::value;
     constexpr bool LAST = Q == STEPS - 1;
     constexpr int LO = LAST ? 0 : LPS * (Q + 1) / STEPS, HI = LAST ? LPS / STEPS : LPS * (Q + 2) / STEPS;
     if (LAST) {
@@ -133,7 +144,7 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
     else issue(s + S - 1, buf == 0 ? S - 1 : buf - 1, LO, HI);
     read_frags(SET ^ 1, LAST ? nbuf : buf, LAST ? 0 : Q + 1);
     multiply(SET);
-    constexpr int NM = WN * WM, RF = WM + WN, LI = HI - LO;
+    constexpr int NM = FN * FM, RF = FM + FN, LI = HI - LO;
     constexpr int OPS = 2 * (LI + RF) <= NM ? 1 : LI + RF <= NM ? 2 : 4;
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
 #pragma unroll
@@ -150,24 +161,38 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
     __builtin_amdgcn_sched_barrier(0);
     __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the reads have had the products' time to complete
   };
+  typedef std::integral_constant<int, 0> Zero;
+  typedef std::integral_constant<int, 1> One;
+  auto next = [](int b) { return b + 1 == S ? 0 : b + 1; };
   int buf = 0;
-  for (int s = 0; s < nst; ++s) {
-    const int nbuf = buf + 1 == S ? 0 : buf + 1;
-    step(std::integral_constant<int, 0>{}, s, buf, nbuf);
-    step(std::integral_constant<int, 1>{}, s, buf, nbuf);
-    if constexpr (KB == 2) {
-      step(std::integral_constant<int, 2>{}, s, buf, nbuf);
-      step(std::integral_constant<int, 3>{}, s, buf, nbuf);
+  if constexpr (STEPS > 1) {
+    for (int s = 0; s < nst; ++s, buf = next(buf)) {
+      step(Zero{}, Zero{}, s, buf, next(buf));
+      step(One{}, One{}, s, buf, next(buf));
+      if constexpr (STEPS == 4) {
+        step(std::integral_constant<int, 2>{}, Zero{}, s, buf, next(buf));
+        step(std::integral_constant<int, 3>{}, One{}, s, buf, next(buf));
+      }
     }
-    buf = nbuf;
+  } else {  // two stages a trip, so that each register set has its place
+    int s = 0;
+    for (; s + 1 < nst; s += 2, buf = next(buf)) {
+      step(Zero{}, Zero{}, s, buf, next(buf));
+      buf = next(buf);
+      step(Zero{}, One{}, s + 1, buf, next(buf));
+    }
+    if (s < nst) step(Zero{}, Zero{}, s, buf, next(buf));
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last stages land before the workgroup's LDS is another's
 
-  auto sums = [&](int j, int i, i32x4 (&t)[4]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int a = 0; a < 4; ++a) t[a] = i32x4{acc[j][i][4 * a], acc[j][i][4 * a + 1], acc[j][i][4 * a + 2], acc[j][i][4 * a + 3]};
+  // Of a unit and 32 rows of X a lane has two pieces p: four packed rows of each sub (s = 0, 1) of group_of(p), of row token_of(p)
+  auto sums = [&](int j, int i, int p, int s) __attribute__((always_inline)) {
+    if constexpr (MF == 16) return acc[2 * j + s][2 * i + p];
+    else return i32x4{acc[j][i][4 * (p + 2 * s)], acc[j][i][4 * (p + 2 * s) + 1], acc[j][i][4 * (p + 2 * s) + 2], acc[j][i][4 * (p + 2 * s) + 3]};
   };
-  if (splits > 1) {  // K split: the sums go to the workspace, [split][unit][block of 32 rows][4][lane], which a second launch adds up and finishes
+  auto group_of = [&](int p) { return MF == 16 ? part : 2 * p + part; };
+  auto token_of = [&](int p) { return MF == 16 ? 16 * p + row : row; };
+  if (splits > 1) {  // K split: the sums go to the workspace, [split][unit][32 rows][sub + 2 (row / 16)][group][row % 16], which a second launch adds up and finishes
     const int blocks = (M + 31) >> 5;
 #pragma unroll
     for (int j = 0; j < WN; ++j)
@@ -175,42 +200,41 @@ __global__ __launch_bounds__(RW * CW * 64, (RW * CW + 3) / 4) void q8_tile_kerne
       for (int i = 0; i < WM; ++i) {
         const int u = u0 + wn * WN + j, block = (m0 >> 5) + wm * WM + i;
         if (u >= units || block >= blocks) continue;
-        i32x4 t[4];
-        sums(j, i, t);
-        i32x4* to = parts + ((int64_t)split * units + u) * blocks * 256 + block * 256 + lane;
+        i32x4* to = parts + ((int64_t)split * units + u) * blocks * 256 + block * 256;
 #pragma unroll
-        for (int a = 0; a < 4; ++a) to[a * 64] = t[a];
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) to[(s + 2 * (token_of(p) >> 4)) * 64 + group_of(p) * 16 + (token_of(p) & 15)] = sums(j, i, p, s);
       }
     return;
   }
 
-  // ---- epilogue, straight from the accumulators: a lane has 16 packed rows of a token, neighbours in the output
+  // ---- epilogue, straight from the accumulators
   with_form(form, out, [&](auto gated, auto* to) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < WM; ++i) {
-      const int m = m0 + (wm * WM + i) * 32 + r32;
-      const float xs = x_scale[min(m, M - 1)];
+    for (int i = 0; i < WM; ++i)
 #pragma unroll
-      for (int j = 0; j < WN; ++j) {
-        const int u = u0 + wn * WN + j;
-        if (u >= units) continue;
-        i32x4 t[4];
-        sums(j, i, t);
-        finish16<decltype(gated)::value>(t, xs, wscale, to + (int64_t)m * out_stride, u, half, outputs, m < M);
+      for (int p = 0; p < 2; ++p) {
+        const int m = m0 + (wm * WM + i) * 32 + token_of(p);
+        const float xs = x_scale[min(m, M - 1)];
+#pragma unroll
+        for (int j = 0; j < WN; ++j) {
+          const int u = u0 + wn * WN + j;
+          if (u < units) finish8<decltype(gated)::value>(sums(j, i, p, 0), sums(j, i, p, 1), xs, wscale, to + (int64_t)m * out_stride, u, group_of(p), outputs, m < M);
+        }
       }
-    }
   });
 }
 
-template <int WM, int WN, int RW, int CW, int KB, bool NT>
+template <int WM, int WN, int RW, int CW, int KB, int MF, bool NT>
 void launch_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
   typedef Q8Tile<WM, WN, RW, CW, KB> SH;
   static bool configured = false;  // raise the dynamic LDS limit of this instantiation once
   if (!configured) {
-    (void)hipFuncSetAttribute((const void*)q8_tile_kernel<WM, WN, RW, CW, KB, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS_BYTES);
+    (void)hipFuncSetAttribute((const void*)q8_tile_kernel<WM, WN, RW, CW, KB, MF, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS_BYTES);
     configured = true;
   }
-  q8_tile_kernel<WM, WN, RW, CW, KB, NT><<<(p.nblocks * p.mblocks * p.splits + 7) / 8 * 8, SH::TPB, SH::LDS_BYTES, st>>>(
+  q8_tile_kernel<WM, WN, RW, CW, KB, MF, NT><<<(p.nblocks * p.mblocks * p.splits + 7) / 8 * 8, SH::TPB, SH::LDS_BYTES, st>>>(
       w.codes, a.x, (int)a.x_stride, a.M, w.k, w.units, p.nblocks, p.mblocks, p.splits, p.stages, w.scale, a.x_scale, a.out, a.out_stride, w.outputs(), out_form(w, a),
       (i32x4*)a.workspace);
 }
@@ -221,12 +245,12 @@ void launch_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipS
 template <bool WIDE>
 void launch_q8_tiles(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
   int i = 0;
-#define GO(WM, WN, RW, CW, KB, NT, NS)                                             \
+#define GO(WM, WN, RW, CW, KB, MF, NT, NS)                                             \
   if constexpr ((RW * WM >= 4) == WIDE) {                                                     \
     if constexpr (NT) {                                                                       \
-      if (p.tile == i && p.mblocks == 1) return launch_tile<WM, WN, RW, CW, KB, true>(w, a, p, st); \
+      if (p.tile == i && p.mblocks == 1) return launch_tile<WM, WN, RW, CW, KB, MF, true>(w, a, p, st); \
     }                                                                                         \
-    if (p.tile == i) return launch_tile<WM, WN, RW, CW, KB, false>(w, a, p, st);              \
+    if (p.tile == i) return launch_tile<WM, WN, RW, CW, KB, MF, false>(w, a, p, st);              \
   }                                                                                           \
   ++i;
   Q8_TILES(GO)

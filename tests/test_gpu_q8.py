@@ -230,11 +230,11 @@ def test_wide_product(device, dtype, rows, n, k, gated):
 
 
 # shapes whose plain product is a launch of each streamed form and of each tile, with and without a K split
-VARIANTS = [(8, 64, 128), (8, 5000, 128), (8, 10000, 128), (24, 64, 128), (24, 5000, 128), (87, 106, 128), (46, 65, 4100), (65, 7407, 128), (68, 2503, 4100),
-            (67, 11033, 128), (36, 8331, 128), (33, 2729, 4100), (33, 16973, 128), (2800, 91, 4100), (34, 33132, 128), (3000, 131, 4100), (65, 14393, 128),
-            (66, 2958, 8200), (65, 33241, 128), (260, 5378, 8200), (98, 20570, 128), (198, 2077, 8200), (195, 16557, 128), (197, 5550, 16400),
-            (194, 33018, 128), (130, 16868, 128), (292, 4025, 16400), (164, 16572, 128), (291, 3697, 8200), (165, 33014, 128), (321, 33667, 128),
-            (968, 9606, 128)]
+VARIANTS = [(8, 64, 128), (8, 5000, 128), (8, 10000, 128), (24, 64, 128), (24, 5000, 128), (87, 106, 128), (46, 65, 4100), (66, 9211, 128), (71, 2707, 4100),
+            (67, 11033, 128), (74, 2696, 8200), (36, 8331, 128), (33, 2729, 4100), (33, 16973, 128), (2800, 91, 4100), (34, 33132, 128), (1847, 141, 8200),
+            (65, 16768, 128), (67, 5438, 8200), (98, 20570, 128), (195, 2810, 8200), (65, 33241, 128), (388, 2716, 16400), (194, 33018, 128),
+            (129, 23367, 128), (267, 4025, 16400), (257, 24682, 128), (260, 5414, 16400), (130, 16868, 128), (136, 4212, 16400), (165, 33014, 128),
+            (259, 33058, 128), (390, 24714, 128)]
 
 
 @pytest.mark.parametrize("gated", [False, True])
