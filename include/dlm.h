@@ -396,8 +396,8 @@ int dlm_profile_read(dlm_state* s, int n, double* ms_out, int64_t* launches_out,
  * statistics (at most 64 rows).  plan[0] kernel (0 skinny, 1 mid, 2 macro), plan[1], plan[2] rows and columns of
  * a workgroup's tile, plan[3] workgroups that share a tile by splitting K, plan[4] parts K is summed in,
  * plan[5] workgroups, plan[6] chunks of the rows' sums of squares per column block (epilogue 3).
- * dlm_plan_q8_gemm: dlm_q8_gemm of `rows` rows (a stride of up to 4 MiB between them) with a weight [n, k].  plan[0] kernel (0 streamed, 1 tiled), plan[1],
- * plan[2] rows and packed channels of a workgroup's tile, plan[3] workgroups that share a tile by splitting K, plan[4] workgroups, plan[5] KiB of
+ * dlm_plan_q8_gemm: dlm_q8_gemm of `rows` rows (a stride of up to 4 MiB between them) with a weight [n, k].  plan[0] kernel (0 streamed, 1 tiled, 2 banded),
+ * plan[1], plan[2] rows and packed channels of a workgroup's tile, plan[3] workgroups that share a tile by splitting K, plan[4] workgroups, plan[5] KiB of
  * workspace.
  * Errors: DLM_EINVAL (null, bad dtype, epilogue or gated), DLM_ESHAPE (a size out of range, head_dim not in {32, 64, 128}). */
 int dlm_plan_vocab_stats(int rows, int vocab, int dtype, int32_t plan[2]);

@@ -834,4 +834,4 @@ def plan_q8_gemm(rows, n, k, gated=False):
     """How a product of 8-bit rows with a Q8Weight [n, k] is launched (include/dlm.h)."""
     out = (C.c_int32 * 6)()
     _check(lib().dlm_plan_q8_gemm(rows, n, k, int(gated), out))
-    return dict(zip(("kernel", "rows", "cols", "splits", "workgroups", "workspace_kib"), (("streamed", "tiled")[out[0]], *out[1:])))
+    return dict(zip(("kernel", "rows", "cols", "splits", "workgroups", "workspace_kib"), (("streamed", "tiled", "banded")[out[0]], *out[1:])))

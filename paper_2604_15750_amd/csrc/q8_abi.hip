@@ -146,7 +146,7 @@ extern "C" int dlm_plan_q8_gemm(int rows, int n, int k, int gated, int32_t plan[
     const int32_t v[6] = {0, tile, 16 * p.stream.subs, 1, (2 * units + p.stream.subs - 1) / p.stream.subs * ((rows + tile - 1) / tile), 0};
     for (int i = 0; i < 6; ++i) plan[i] = v[i];
   } else {
-    const int32_t v[6] = {1, p.tile.rows, p.tile.cols, p.tile.splits, p.tile.nblocks * p.tile.mblocks * p.tile.splits, (int32_t)(p.tile.workspace >> 10)};
+    const int32_t v[6] = {p.tile.tile < Q8_TILE_COUNT ? 1 : 2, p.tile.rows, p.tile.cols, p.tile.splits, p.tile.nblocks * p.tile.mblocks * p.tile.splits, (int32_t)(p.tile.workspace >> 10)};
     for (int i = 0; i < 6; ++i) plan[i] = v[i];
   }
   return DLM_OK;

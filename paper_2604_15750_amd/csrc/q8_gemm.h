@@ -17,7 +17,7 @@ __device__ inline f32x4 scaled(i32x4 sum, float token, f32x4 channel) {
   for (int i = 0; i < 4; ++i) y[i] = (float)sum[i] * token * channel[i];
   return y;
 }
-// silu(g) u: the exponential and the reciprocal within a few units of fp32's last place
+// silu(g) u: the exponential's argument is rounded (2 |g| 2^-24 of the result), the exponential and the reciprocal are within a few units of fp32's last place
 __device__ inline f32x4 gated_unit(f32x4 g, f32x4 u) {
   f32x4 y;
 #pragma unroll
@@ -75,6 +75,60 @@ __device__ inline void finish8(i32x4 first, i32x4 second, float token, const flo
   if (!there) return;
   if constexpr (GATED) store4(row, 16 * u + 4 * g, outputs, gated_unit(y0, y1));
   else store8(row, 32 * u + 8 * g, outputs, y0, y1);
+}
+
+// 1 KiB, 16 bytes a lane, from a buffer to LDS (dst: the wavefront's)
+__device__ inline void copy_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* dst, int lane_at, int at) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (__attribute__((address_space(3))) void*)dst, 16, lane_at, at, 0, 0);
+}
+
+// Workgroup id -> tile and share of K: ids congruent mod 8 share an XCD, which gets one contiguous eighth of the tiles; in groups of 8 row blocks, row blocks
+// fastest, so that the tiles an XCD works on at a time share both operands in its L2
+struct Q8At {
+  int split, rb, cb;  // split < 0: none
+};
+__device__ inline Q8At tile_of(int id, int nblocks, int mblocks, int splits) {
+  const int tiles = nblocks * mblocks, lin = (id & 7) * ((tiles * splits + 7) >> 3) + (id >> 3);
+  if (lin >= tiles * splits) return Q8At{-1, 0, 0};
+  const int split = lin / tiles, tile = lin - split * tiles;
+  const int group = tile / (8 * nblocks), rows_in = min(8, mblocks - 8 * group), at = tile - group * 8 * nblocks;
+  const int cb = at / rows_in;
+  return Q8At{split, 8 * group + at - cb * rows_in, cb};
+}
+
+// The end of a tile: WN units from u0 on by WM x 32 rows from m0 on of a wavefront, acc[2 unit + sub][2 (rows / 32) + half] as 16x16 products leave them.
+// A launch that splits K leaves its sums in the workspace, [split][unit][32 rows][sub + 2 (row / 16)][group][row % 16], where a second launch adds them up
+// and finishes; any other finishes straight from the accumulators.
+template <int WN, int WM>
+__device__ inline __attribute__((always_inline)) void finish_tile(const i32x4 (&acc)[2 * WN][2 * WM], int u0, int m0, int lane, int split, int splits, int M, int units, const float* wscale,
+                                                                  const float* x_scale, void* out, int64_t out_stride, int outputs, int form, i32x4* parts) {
+  const int g = lane >> 4;
+  if (splits > 1) {
+    const int blocks = (M + 31) >> 5;
+#pragma unroll
+    for (int j = 0; j < WN; ++j)
+#pragma unroll
+      for (int i = 0; i < WM; ++i) {
+        const int u = u0 + j, block = (m0 >> 5) + i;
+        if (u >= units || block >= blocks) continue;
+        i32x4* to = parts + ((int64_t)split * units + u) * blocks * 256 + block * 256 + lane;
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) to[(s + 2 * p) * 64] = acc[2 * j + s][2 * i + p];
+      }
+    return;
+  }
+  with_form(form, out, [&](auto gated, auto* to) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 2 * WM; ++i) {
+      const int m = m0 + 16 * i + (lane & 15);
+      const float xs = x_scale[min(m, M - 1)];
+#pragma unroll
+      for (int j = 0; j < WN; ++j)
+        if (u0 + j < units) finish8<decltype(gated)::value>(acc[2 * j][i], acc[2 * j + 1][i], xs, wscale, to + (int64_t)m * out_stride, u0 + j, g, outputs, m < M);
+    }
+  });
 }
 
 }  // namespace

@@ -68,25 +68,25 @@ void launch_q8_join(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, h
                                                                         out_form(w, a));
 }
 
-// The tile and K split with the least estimated time.  A round is what 256 compute units take together.  A k-tile takes what a workgroup alone on the chip
-// takes (ns), or what the chip's power leaves the matrix cores (3.7 POP/s in 16x16x64 products, 2.8 in 32x32x32), what the L2s (24 TB/s) or, for W, HBM (5.9 TB/s, shared by up to 8
-// row blocks) give to all of the round's workgroups, whichever is most, joined by a 4-norm; a round pays for its copies' start and its
-// epilogue; a K split adds a launch, and the sums' way to memory and back.  Constants fitted to the launches named
-// at Q8_TILES: 10 % off in the root mean square.
+// The shape and K split with the least estimated time.  A k-tile takes what a workgroup alone on the chip takes (ns), or what the chip's power leaves the matrix cores (3.24
+// POP/s), what the L2s (25.3 TB/s) or, for W, HBM (5.33 TB/s, shared by up to 8 row blocks) give to all of the workgroups that run at a time, whichever is most, joined
+// by a 4-norm; 256 further workgroups add `more` to that, and their epilogues; a K split adds a launch, and the sums' way to memory and back.  Constants
+// fitted to the launches named at Q8_TILES: 10 % off in the root mean square.
 Q8TilePlan q8_tile_plan(int M, int units, int K) {
   struct Shape {
     int bm, un, kb;
-    float ns_4, chip_4, hbm;  // 4th powers of ns, and of what power and the L2s allow on a full chip; ns that HBM allows where one row block reads W
+    float ns_4, more_4, chip_4, hbm;  // 4th powers of ns, of `more`, and of what power and the L2s allow on a full chip; ns that HBM allows where one row block reads W
   };
   constexpr float CUS = 256.f;
-  static const auto shape = [](int wm, int wn, int rw, int cw, int kb, int mf, float ns) {
-    const int bm = 32 * rw * wm, un = cw * wn;
+  static const auto shape = [](int bm, int un, int kb, float ns, float more) {
     auto p4 = [](float x) { return x * x * x * x; };
-    return Shape{bm, un, kb, p4(ns), p4(bm * un * 32 * 128 * CUS / (mf == 16 ? 3.7e6f : 2.8e6f)) + p4((bm + un * 32) * 64 * CUS / 24.3e3f), un * 2048 * CUS / 5.9e3f};
+    return Shape{bm, un, kb, p4(ns), p4(more), p4(bm * un * 32 * 128 * CUS / 3.24e6f) + p4((bm + un * 32) * 64 * CUS / 25.3e3f), un * 2048 * CUS / 5.33e3f};
   };
-#define ROW(WM, WN, RW, CW, KB, MF, NT, NS) shape(WM, WN, RW, CW, KB, MF, NS),
-  static const Shape shapes[] = {Q8_TILES(ROW)};
-#undef ROW
+#define TILE(WM, WN, KB, NS, MORE) shape(64 * WM, 4 * WN, KB, NS, MORE),
+#define BAND(WM, CW, S, NS, MORE) shape(32 * WM, CW, 2, NS, MORE),
+  static const Shape shapes[] = {Q8_TILES(TILE) Q8_BANDS(BAND)};
+#undef TILE
+#undef BAND
   const int KT = (K + 63) / 64;
   Q8TilePlan best{};
   best.us = 1e30f;
@@ -95,7 +95,7 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
     ++i;
     const int mb = (M + t.bm - 1) / t.bm, nb = (units + t.un - 1) / t.un, stages = (KT + t.kb - 1) / t.kb;
     const float out = t.bm * t.un * 32.f, edge = t.bm + t.un * 32.f, hbm = t.hbm / (mb < 8 ? mb : 8), full_4 = t.chip_4 + hbm * hbm * hbm * hbm;
-    auto ns = [&](float share) { return sqrtf(sqrtf(t.ns_4 + full_4 * (share * share) * (share * share))); };
+    auto ns = [&](float own_4, float share) { return sqrtf(sqrtf(own_4 + full_4 * (share * share) * (share * share))); };
     const int64_t wgs = (int64_t)mb * nb;
     for (int sp = 1; sp <= Q8_MAX_SPLITS; ++sp) {
       if (sp > 1 && (wgs * sp > Q8_SPLIT_WGS || stages < 4 * sp)) break;
@@ -103,8 +103,8 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
       if ((stages + per - 1) / per != sp) continue;  // (a split without stages)
       const int64_t all = wgs * sp, full = (all - 1) / 256;
       const float last = (all - 256 * full) / CUS;
-      float us = per * t.kb * 1e-3f * ((full ? full * ns(1.f) : 0.f) + ns(last)) + 2.2f + (full + last) * 1.25e-4f * out + (full + 1) * 7.3e-3f * edge;
-      if (sp > 1) us += 2.f + sp * (0.16f + 5.4e-4f * units * ((M + 31) / 32));
+      float us = per * t.kb * 1e-3f * ((full ? full * ns(t.more_4, 1.f) : 0.f) + ns(t.ns_4, last)) + 1.67f + (full + last) * 1.336e-4f * out + (0.45f * full + 1) * 9.4e-3f * edge;
+      if (sp > 1) us += 1.8f + sp * (0.166f + 5e-4f * units * ((M + 31) / 32));
       if (us < best.us) best = Q8TilePlan{i, t.bm, t.un * 32, nb, mb, sp, per, sp > 1 ? (size_t)sp * units * ((M + 31) / 32) * 4096 : 0, us};
     }
   }
@@ -149,6 +149,6 @@ size_t q8_gemm_workspace(int rows, int n, int k, int gated) {
 
 void launch_q8_gemm(const Q8View& w, const Q8GemmArgs& a, const Q8Plan& c, hipStream_t st) {
   if (c.streamed) return launch_q8_stream(w, a, c.stream, st);
-  c.tile.rows >= 128 ? launch_q8_tiles<true>(w, a, c.tile, st) : launch_q8_tiles<false>(w, a, c.tile, st);
+  c.tile.tile < Q8_TILE_COUNT ? launch_q8_tiles(w, a, c.tile, st) : launch_q8_bands(w, a, c.tile, st);
   if (c.tile.splits > 1) launch_q8_join(w, a, c.tile, st);
 }

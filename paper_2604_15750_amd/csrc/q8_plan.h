@@ -2,20 +2,22 @@
 #pragma once
 #include "q8.h"
 
-// The shape of a tile {WM, WN, RW, CW, KB, MF, NT, ns}: see q8_tile.h.  NT: a W that one row block reads is read non-temporally, past the memory-side cache, in
-// which the weights of a model do not stay from pass to pass (5 % of launches of up to 64 rows; nothing beyond).  ns: nanoseconds per k-tile of 64 that a workgroup alone on the
-// chip takes.  16 of 60 shapes that were timed (29 row counts from 8 to 2822, 15 weights from 640 x 640 to 3584 x 18944, random codes), chosen by leaving out, one by
-// one, the shape whose absence costs least: what the planner takes is 2 % behind the best of these in the mean.
-#define Q8_TILES(X) \
-  X(4, 2, 2, 4, 2, 16, false, 586) X(3, 3, 2, 4, 1, 16, false, 675) X(3, 2, 2, 4, 2, 16, false, 506) X(2, 3, 2, 4, 1, 16, false, 499) \
-  X(2, 2, 2, 4, 2, 16, false, 325) X(5, 1, 1, 6, 2, 32, false, 348) X(5, 1, 1, 8, 2, 32, false, 351) X(3, 1, 2, 4, 2, 32, false, 231) \
-  X(1, 2, 4, 2, 2, 16, false, 202) X(3, 1, 1, 4, 2, 32, false, 190) X(1, 1, 2, 5, 2, 16, true, 173) X(1, 1, 2, 4, 2, 16, true, 149) \
-  X(1, 1, 2, 2, 2, 16, true, 121) X(1, 1, 1, 5, 1, 16, true, 151) X(1, 1, 1, 4, 2, 16, true, 128) X(1, 1, 1, 2, 2, 16, true, 114)
-// rows x packed rows: 256 x 256, 192 x 384, 192 x 256, 128 x 384, 128 x 256, 160 x 192, 160 x 256, 192 x 128, 128 x 128, 96 x 128, 64 x 160, 64 x 128, 64 x 64, 32 x 160,
-// 32 x 128, 32 x 64
+// The shapes of a tile {WM, WN, KB, ns, more} (see q8_tile.h) and of a band {WM, CW, S, ns, more} (q8_band.h).  ns: nanoseconds per k-tile of 64 that a workgroup
+// alone on the chip takes; more: what one adds that shares its compute unit.  16 of 36 shapes that were timed (29 row counts from 8 to 2822, 15 weights from 640 x 640
+// to 3584 x 18944, random codes), chosen by leaving out, one by one, the shape whose absence costs least (0.8 % in the mean); what the planner takes is 2 % behind the best of these in
+// the mean, 26 % at most.  (W through LDS in tiles of 32, 64 and 96 rows is among those left out: bands are faster by 8 to 16 % from 24 to 340 rows.)
+#define Q8_TILES(X) X(4, 2, 2, 575, 575) X(3, 3, 1, 638, 638) X(2, 3, 1, 472, 472) X(2, 2, 2, 320, 320) X(3, 1, 2, 268, 268) X(2, 1, 2, 200, 200)
+#define Q8_BANDS(X) \
+  X(1, 2, 6, 80, 36) X(1, 3, 6, 90, 62) X(1, 4, 6, 100, 51) X(2, 3, 6, 111, 95) X(2, 4, 5, 124, 108) X(3, 4, 5, 161, 129) X(3, 6, 5, 235, 235) X(4, 4, 4, 210, 122) \
+  X(5, 4, 4, 253, 124) X(5, 6, 4, 374, 374)
+// rows x packed rows: 256 x 256, 192 x 384, 128 x 384, 128 x 256, 192 x 128, 128 x 128; 32 x 64, 32 x 96, 32 x 128, 64 x 96, 64 x 128, 96 x 128, 96 x 192, 128 x 128,
+// 160 x 128, 160 x 192
+#define ONE(...) +1
+constexpr int Q8_TILE_COUNT = 0 Q8_TILES(ONE);
+#undef ONE
 
 struct Q8TilePlan {
-  int tile;  // index into Q8_TILES
+  int tile;  // index into Q8_TILES, or behind those into Q8_BANDS
   int rows, cols;  // of a tile
   int nblocks, mblocks;
   int splits, stages;  // workgroups that share a tile's K, and how many stages each has
@@ -24,8 +26,8 @@ struct Q8TilePlan {
 };
 constexpr int Q8_SPLIT_WGS = 256, Q8_MAX_SPLITS = 16;  // (a launch that splits K is one round)
 Q8TilePlan q8_tile_plan(int M, int units, int K);
-template <bool WIDE>
 void launch_q8_tiles(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);
+void launch_q8_bands(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);
 
 void launch_q8_join(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);  // behind one that splits K
 

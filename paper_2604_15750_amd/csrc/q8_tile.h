@@ -16,17 +16,9 @@
 
 namespace {
 
-// 1 KiB, 16 bytes a lane, from a buffer to LDS (dst: the wavefront's)
-template <bool NT>
-__device__ inline void copy_to_lds(__amdgpu_buffer_rsrc_t from, unsigned char* dst, int lane_at, int at) {
-  __attribute__((address_space(3))) void* to = (__attribute__((address_space(3))) void*)dst;
-  if constexpr (NT) __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, lane_at, at, 0, 2);
-  else __builtin_amdgcn_raw_ptr_buffer_load_lds(from, to, 16, lane_at, at, 0, 0);
-}
-
-template <int WM, int WN, int RW, int CW, int KB>
+template <int WM, int WN, int KB>
 struct Q8Tile {
-  static constexpr int NW = RW * CW, TPB = NW * 64, BM = 32 * RW * WM, UN = CW * WN;  // rows of X, units of W
+  static constexpr int RW = 2, CW = 4, NW = RW * CW, TPB = NW * 64, BM = 32 * RW * WM, UN = CW * WN;  // rows of X, units of W
   static constexpr int W_LOADS = UN * KB * 2, X_LOADS = BM * KB / 16;                 // of 1 KiB, a stage
   static constexpr int LPS = (W_LOADS + X_LOADS + NW - 1) / NW;                       // ... of a wavefront (some have surplus ones)
   static constexpr int W_BYTES = W_LOADS * 1024, STAGE = W_BYTES + X_LOADS * 1024;
@@ -35,27 +27,20 @@ struct Q8Tile {
   static_assert(W_LOADS % NW == 0 && X_LOADS % 2 == 0 && S >= 2 && (KB == 1 || KB == 2) && LDS_BYTES <= 160 * 1024, "tile shape");
 };
 
-template <int WM, int WN, int RW, int CW, int KB, int MF, bool NT>
-__global__ __launch_bounds__(RW * CW * 64, RW * CW > 4 ? (RW * CW + 3) / 4 : 2) void q8_tile_kernel(const unsigned char* __restrict__ wt, const int8_t* __restrict__ x, int x_stride, int M, int K, int units,
-                                                                      int nblocks, int mblocks, int splits, int split_stages, const float* __restrict__ wscale, const float* __restrict__ x_scale,
-                                                                      void* __restrict__ out, int64_t out_stride, int outputs, int form, i32x4* __restrict__ parts) {
-  typedef Q8Tile<WM, WN, RW, CW, KB> SH;
-  constexpr int NW = SH::NW, BM = SH::BM, UN = SH::UN, LPS = SH::LPS, STAGE = SH::STAGE, S = SH::S, W_LOADS = SH::W_LOADS, LOADS = W_LOADS + SH::X_LOADS;
-  constexpr int STEPS = MF == 16 ? KB : 2 * KB;  // of a stage
+template <int WM, int WN, int KB>
+__global__ __launch_bounds__(512, 2) void q8_tile_kernel(const unsigned char* __restrict__ wt, const int8_t* __restrict__ x, int x_stride, int M, int K, int units, int nblocks, int mblocks,
+                                                         int splits, int split_stages, const float* __restrict__ wscale, const float* __restrict__ x_scale, void* __restrict__ out,
+                                                         int64_t out_stride, int outputs, int form, i32x4* __restrict__ parts) {
+  typedef Q8Tile<WM, WN, KB> SH;
+  constexpr int CW = SH::CW, NW = SH::NW, BM = SH::BM, UN = SH::UN, LPS = SH::LPS, STAGE = SH::STAGE, S = SH::S, W_LOADS = SH::W_LOADS, LOADS = W_LOADS + SH::X_LOADS;
   extern __shared__ __align__(16) unsigned char lds[];
 
-  // Workgroup id -> tile: ids congruent mod 8 share an XCD, which gets one contiguous eighth of the tiles; in groups of 8 row blocks, row blocks fastest, so that
-  // the tiles an XCD works on at a time share both operands in its L2
-  const int tiles = nblocks * mblocks, lin = (blockIdx.x & 7) * ((tiles * splits + 7) >> 3) + (blockIdx.x >> 3);
-  if (lin >= tiles * splits) return;  // (the whole workgroup)
-  const int split = lin / tiles, tile = lin - split * tiles;
-  const int group = tile / (8 * nblocks), rows_in = min(8, mblocks - 8 * group), at = tile - group * 8 * nblocks;
-  const int cb = at / rows_in, rb = 8 * group + at - cb * rows_in;
-
+  const Q8At at = tile_of(blockIdx.x, nblocks, mblocks, splits);
+  if (at.split < 0) return;  // (the whole workgroup)
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / CW, wn = wave % CW;
   const int KTP = (K + 127) >> 7 << 1;                                       // k-tiles of a unit in memory
-  const int s0 = split * split_stages, nst = min(((K + 63) / 64 + KB - 1) / KB - s0, split_stages);  // this workgroup's stages s0 .. s0 + nst - 1
-  const int u0 = cb * UN, m0 = rb * BM, mrows = min(BM, M - m0), nunits = min(UN, units - u0);
+  const int s0 = at.split * split_stages, nst = min(((K + 63) / 64 + KB - 1) / KB - s0, split_stages);  // this workgroup's stages s0 .. s0 + nst - 1
+  const int u0 = at.cb * UN, m0 = at.rb * BM, mrows = min(BM, M - m0), nunits = min(UN, units - u0);
 
   // Direct-to-LDS loads, 1 KiB each: wavefront w moves the ones congruent w mod NW, W's first.  Rows and units past the end are the last one again, chunks
   // past a row's last are that one again (W is zero there): every address is one of the operands'.
@@ -84,47 +69,38 @@ __global__ __launch_bounds__(RW * CW * 64, RW * CW > 4 ? (RW * CW + 3) / 4 : 2) 
 #pragma unroll
     for (int i = lo; i < hi; ++i) {
       unsigned char* dst = lds + buf * STAGE + load_of(i) * 1024;
-      if (i * NW < W_LOADS) copy_to_lds<NT>(wr, dst, off[i], t * (KB * 2048));
-      else copy_to_lds<false>(xr, dst, off[i] + (RPL == 8 && (i * NW) % 2 ? chunk2 : chunk), t * (64 * KB));
+      if (i * NW < W_LOADS) copy_to_lds(wr, dst, off[i], t * (KB * 2048));
+      else copy_to_lds(xr, dst, off[i] + (RPL == 8 && (i * NW) % 2 ? chunk2 : chunk), t * (64 * KB));
     }
   };
 
-  constexpr int PER = MF == 16 ? 2 : 1, FM = PER * WM, FN = PER * WN;  // fragments of 16 or 32 rows
-  typedef typename std::conditional<MF == 16, i32x4, i32x16>::type Acc;
-  Acc acc[FN][FM];
+  constexpr int FM = 2 * WM, FN = 2 * WN;  // fragments of 16 rows
+  i32x4 acc[FN][FM];
   i32x4 xf[2][FM], wf[2][FN];
 #pragma unroll
   for (int j = 0; j < FN; ++j)
 #pragma unroll
-    for (int i = 0; i < FM; ++i) acc[j][i] = Acc(0);
-  // lane -> row of a fragment, and which of a k-tile's chunks (of step q) it has
-  const int row = lane % MF, part = lane / MF, turn = KB == 2 ? (row >> 1) & 7 : (row >> 2) & 3;
-  const int w_at = MF == 16 ? lane * 16 : (row >> 4) * 1024 + part * 256 + (row & 15) * 16;
+    for (int i = 0; i < FM; ++i) acc[j][i] = i32x4(0);
+  const int row = lane & 15, part = lane >> 4, turn = KB == 2 ? row >> 1 : row >> 2;  // lane -> row of a fragment, which of a k-tile's chunks it has
   auto read_frags = [&](int set, int buf, int q) __attribute__((always_inline)) {
     const unsigned char* st = lds + buf * STAGE;
 #pragma unroll
-    for (int j = 0; j < FN; ++j) {
-      if constexpr (MF == 16) wf[set][j] = *(const i32x4*)(st + ((wn * WN + j / 2) * KB + q) * 2048 + (j & 1) * 1024 + w_at);
-      else wf[set][j] = *(const i32x4*)(st + ((wn * WN + j) * KB + (q >> 1)) * 2048 + (q & 1) * 512 + w_at);
-    }
+    for (int j = 0; j < FN; ++j) wf[set][j] = *(const i32x4*)(st + ((wn * WN + j / 2) * KB + q) * 2048 + (j & 1) * 1024 + lane * 16);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) xf[set][i] = *(const i32x4*)(st + SH::W_BYTES + (wm * WM * 32 + i * MF + row) * (64 * KB) + (((64 / MF * q + part) ^ turn) << 4));
+    for (int i = 0; i < FM; ++i) xf[set][i] = *(const i32x4*)(st + SH::W_BYTES + (wm * WM * 32 + 16 * i + row) * (64 * KB) + (((4 * q + part) ^ turn) << 4));
   };
   auto multiply = [&](int set) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int i = 0; i < FM; ++i) {
-        if constexpr (MF == 16) acc[j][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[set][j], xf[set][i], acc[j][i], 0, 0, 0);
-        else acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(wf[set][j], xf[set][i], acc[j][i], 0, 0, 0);
-      }
+      for (int i = 0; i < FM; ++i) acc[j][i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[set][j], xf[set][i], acc[j][i], 0, 0, 0);
   };
 
   // stages 0 .. S - 2 and the first part of S - 1 go out at once; the rest of it during stage 0, as for every later stage
 #pragma unroll
   for (int s = 0; s < S - 1; ++s) issue(s, s, 0, LPS);
-  issue(S - 1, S - 1, 0, LPS / STEPS);
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * LPS + LPS / STEPS) : "memory");  // stage 0 has landed (this wavefront's share)
+  issue(S - 1, S - 1, 0, LPS / KB);
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * LPS + LPS / KB) : "memory");  // stage 0 has landed (this wavefront's share)
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
   read_frags(0, 0, 0);
@@ -132,8 +108,8 @@ __global__ __launch_bounds__(RW * CW * 64, RW * CW > 4 ? (RW * CW + 3) / 4 : 2) 
   // step Q of stage s (in LDS buffer buf), whose operands are in register set SET
   auto step = [&](auto Qc, auto SETc, int s, int buf, int nbuf) __attribute__((always_inline)) {
     constexpr int Q = decltype(Qc)::value, SET = decltype(SETc)::value;
-    constexpr bool LAST = Q == STEPS - 1;
-    constexpr int LO = LAST ? 0 : LPS * (Q + 1) / STEPS, HI = LAST ? LPS / STEPS : LPS * (Q + 2) / STEPS;
+    constexpr bool LAST = Q == KB - 1;
+    constexpr int LO = LAST ? 0 : LPS * (Q + 1) / KB, HI = LAST ? LPS / KB : LPS * (Q + 2) / KB;
     if (LAST) {
       asm volatile("s_waitcnt vmcnt(%0)" ::"n"((S - 2) * LPS) : "memory");  // stage s + 1 has landed
       __builtin_amdgcn_s_barrier();  // ... for every wavefront, and every wavefront has read the last of stage s
@@ -165,14 +141,10 @@ __global__ __launch_bounds__(RW * CW * 64, RW * CW > 4 ? (RW * CW + 3) / 4 : 2) 
   typedef std::integral_constant<int, 1> One;
   auto next = [](int b) { return b + 1 == S ? 0 : b + 1; };
   int buf = 0;
-  if constexpr (STEPS > 1) {
+  if constexpr (KB == 2) {
     for (int s = 0; s < nst; ++s, buf = next(buf)) {
       step(Zero{}, Zero{}, s, buf, next(buf));
       step(One{}, One{}, s, buf, next(buf));
-      if constexpr (STEPS == 4) {
-        step(std::integral_constant<int, 2>{}, Zero{}, s, buf, next(buf));
-        step(std::integral_constant<int, 3>{}, One{}, s, buf, next(buf));
-      }
     }
   } else {  // two stages a trip, so that each register set has its place
     int s = 0;
@@ -185,74 +157,20 @@ __global__ __launch_bounds__(RW * CW * 64, RW * CW > 4 ? (RW * CW + 3) / 4 : 2) 
   }
   asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the surplus loads of the last stages land before the workgroup's LDS is another's
 
-  // Of a unit and 32 rows of X a lane has two pieces p: four packed rows of each sub (s = 0, 1) of group_of(p), of row token_of(p)
-  auto sums = [&](int j, int i, int p, int s) __attribute__((always_inline)) {
-    if constexpr (MF == 16) return acc[2 * j + s][2 * i + p];
-    else return i32x4{acc[j][i][4 * (p + 2 * s)], acc[j][i][4 * (p + 2 * s) + 1], acc[j][i][4 * (p + 2 * s) + 2], acc[j][i][4 * (p + 2 * s) + 3]};
-  };
-  auto group_of = [&](int p) { return MF == 16 ? part : 2 * p + part; };
-  auto token_of = [&](int p) { return MF == 16 ? 16 * p + row : row; };
-  if (splits > 1) {  // K split: the sums go to the workspace, [split][unit][32 rows][sub + 2 (row / 16)][group][row % 16], which a second launch adds up and finishes
-    const int blocks = (M + 31) >> 5;
-#pragma unroll
-    for (int j = 0; j < WN; ++j)
-#pragma unroll
-      for (int i = 0; i < WM; ++i) {
-        const int u = u0 + wn * WN + j, block = (m0 >> 5) + wm * WM + i;
-        if (u >= units || block >= blocks) continue;
-        i32x4* to = parts + ((int64_t)split * units + u) * blocks * 256 + block * 256;
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-          for (int s = 0; s < 2; ++s) to[(s + 2 * (token_of(p) >> 4)) * 64 + group_of(p) * 16 + (token_of(p) & 15)] = sums(j, i, p, s);
-      }
-    return;
-  }
-
-  // ---- epilogue, straight from the accumulators
-  with_form(form, out, [&](auto gated, auto* to) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < WM; ++i)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const int m = m0 + (wm * WM + i) * 32 + token_of(p);
-        const float xs = x_scale[min(m, M - 1)];
-#pragma unroll
-        for (int j = 0; j < WN; ++j) {
-          const int u = u0 + wn * WN + j;
-          if (u < units) finish8<decltype(gated)::value>(sums(j, i, p, 0), sums(j, i, p, 1), xs, wscale, to + (int64_t)m * out_stride, u, group_of(p), outputs, m < M);
-        }
-      }
-  });
+  finish_tile<WN, WM>(acc, u0 + wn * WN, m0 + wm * WM * 32, lane, at.split, splits, M, units, wscale, x_scale, out, out_stride, outputs, form, parts);
 }
 
-template <int WM, int WN, int RW, int CW, int KB, int MF, bool NT>
+template <int WM, int WN, int KB>
 void launch_tile(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
-  typedef Q8Tile<WM, WN, RW, CW, KB> SH;
+  typedef Q8Tile<WM, WN, KB> SH;
   static bool configured = false;  // raise the dynamic LDS limit of this instantiation once
   if (!configured) {
-    (void)hipFuncSetAttribute((const void*)q8_tile_kernel<WM, WN, RW, CW, KB, MF, NT>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS_BYTES);
+    (void)hipFuncSetAttribute((const void*)q8_tile_kernel<WM, WN, KB>, hipFuncAttributeMaxDynamicSharedMemorySize, SH::LDS_BYTES);
     configured = true;
   }
-  q8_tile_kernel<WM, WN, RW, CW, KB, MF, NT><<<(p.nblocks * p.mblocks * p.splits + 7) / 8 * 8, SH::TPB, SH::LDS_BYTES, st>>>(
+  q8_tile_kernel<WM, WN, KB><<<(p.nblocks * p.mblocks * p.splits + 7) / 8 * 8, SH::TPB, SH::LDS_BYTES, st>>>(
       w.codes, a.x, (int)a.x_stride, a.M, w.k, w.units, p.nblocks, p.mblocks, p.splits, p.stages, w.scale, a.x_scale, a.out, a.out_stride, w.outputs(), out_form(w, a),
       (i32x4*)a.workspace);
 }
 
 }  // namespace
-
-// the launches of the tiles of 128 rows and more, or of those of fewer (q8_tile_wide.hip, q8_tile_narrow.hip)
-template <bool WIDE>
-void launch_q8_tiles(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st) {
-  int i = 0;
-#define GO(WM, WN, RW, CW, KB, MF, NT, NS)                                             \
-  if constexpr ((RW * WM >= 4) == WIDE) {                                                     \
-    if constexpr (NT) {                                                                       \
-      if (p.tile == i && p.mblocks == 1) return launch_tile<WM, WN, RW, CW, KB, MF, true>(w, a, p, st); \
-    }                                                                                         \
-    if (p.tile == i) return launch_tile<WM, WN, RW, CW, KB, MF, false>(w, a, p, st);              \
-  }                                                                                           \
-  ++i;
-  Q8_TILES(GO)
-#undef GO
-}

@@ -230,11 +230,13 @@ def test_wide_product(device, dtype, rows, n, k, gated):
 
 
 # shapes whose plain product is a launch of each streamed form and of each tile, with and without a K split
-VARIANTS = [(8, 64, 128), (8, 5000, 128), (8, 10000, 128), (24, 64, 128), (24, 5000, 128), (87, 106, 128), (46, 65, 4100), (66, 9211, 128), (71, 2707, 4100),
-            (67, 11033, 128), (74, 2696, 8200), (36, 8331, 128), (33, 2729, 4100), (33, 16973, 128), (2800, 91, 4100), (34, 33132, 128), (1847, 141, 8200),
-            (65, 16768, 128), (67, 5438, 8200), (98, 20570, 128), (195, 2810, 8200), (65, 33241, 128), (388, 2716, 16400), (194, 33018, 128),
-            (129, 23367, 128), (267, 4025, 16400), (257, 24682, 128), (260, 5414, 16400), (130, 16868, 128), (136, 4212, 16400), (165, 33014, 128),
-            (259, 33058, 128), (390, 24714, 128)]
+VARIANTS = [(193, 24601, 128), (774, 4656, 128), (129, 16570, 128), (771, 1154, 16400), (130, 5378, 16400), (289, 16471, 128), (131, 32825, 128),
+            (772, 3213, 16400), (1157, 580, 640), (15, 24578, 2100), (675, 193, 8200), (34, 32, 128), (17, 8205, 640), (33, 33, 4100), (14, 33, 8200),
+            (2725, 129, 128), (21, 16400, 640), (548, 258, 4100), (2711, 483, 128), (33, 24610, 128), (515, 484, 8200), (2340, 385, 128), (33, 16434, 128),
+            (387, 386, 8200), (34, 4098, 16400), (2314, 770, 128), (65, 16443, 128), (771, 881, 8200), (68, 5474, 16400), (258, 11033, 128), (65, 32836, 128),
+            (1035, 910, 16400), (1, 33, 128), (1, 4112, 128), (1, 8193, 128), (17, 33, 128), (17, 4124, 128), (193, 12336, 128), (970, 641, 16400),
+            (193, 21897, 200), (974, 1411, 16400), (197, 32844, 128), (866, 3358, 16400), (518, 8245, 128), (902, 1027, 16400), (513, 24779, 128),
+            (520, 13062, 8200), (1156, 9736, 200), (967, 4530, 16400)]
 
 
 @pytest.mark.parametrize("gated", [False, True])

@@ -126,7 +126,7 @@ def test_plans():
     for n, k, gated in ((4096, 12288, False), (640, 131071, False), (1000, 3000, True), (12288, 4096, False), (33, 65, False), (8232, 16400, False), (30000, 131071, False)):
         for rows in (1, 16, 17, 32, 33, 64, 96, 130, 194, 300, 700, 2000, 20000):
             p = api.plan_q8_gemm(rows, n, k, gated)
-            assert (p["kernel"] == "tiled" or rows <= 32) and p["splits"] >= 1 and p["workgroups"] >= p["splits"]
+            assert (p["kernel"] != "streamed" or rows <= 32) and p["splits"] >= 1 and p["workgroups"] >= p["splits"]
             assert (p["workspace_kib"] > 0) == (p["splits"] > 1)
             for more in (rows, rows + 1, rows + 500):
                 assert p["workspace_kib"] << 10 <= api.lib().dlm_q8_gemm_workspace(more, n, k, int(gated))
@@ -135,11 +135,15 @@ def test_plans():
 def test_every_variant_is_reached_by_a_test():
     from test_gpu_q8 import VARIANTS
 
-    have = {(p["kernel"], p["rows"], p["cols"], p["splits"] > 1) for p in (api.plan_q8_gemm(*v) for v in VARIANTS)}
-    split = {(32, 64), (32, 128), (32, 160), (64, 64), (64, 128), (64, 160), (96, 128), (128, 128), (128, 256), (160, 192), (160, 256), (192, 128)}
-    tiles = split | {(128, 384), (192, 256), (192, 384), (256, 256)}
-    assert have == {("tiled", *t, False) for t in tiles} | {("tiled", *t, True) for t in split} | \
-        {("streamed", 16, c, False) for c in (16, 32, 48)} | {("streamed", 32, c, False) for c in (16, 32)}
+    plans = [(v[0], api.plan_q8_gemm(*v)) for v in VARIANTS]
+    tiles = {(128, 128), (128, 256), (128, 384), (192, 128), (192, 384), (256, 256)}
+    bands = {(32, 64), (32, 96), (32, 128), (64, 96), (64, 128), (96, 128), (96, 192), (128, 128), (160, 128), (160, 192)}
+    assert {(p["kernel"], p["rows"], p["cols"]) for _, p in plans if p["splits"] == 1} == {("tiled", *t) for t in tiles} | {("banded", *b) for b in bands} | \
+        {("streamed", 16, c) for c in (16, 32, 48)} | {("streamed", 32, c) for c in (16, 32)}
+    assert {(p["kernel"], p["rows"], p["cols"]) for _, p in plans if p["splits"] > 1} == {("tiled", *t) for t in tiles} | {("banded", *b) for b in bands - {(128, 128)}}
+    # a band's W is read in another way where one row block reads it
+    for one in (False, True):
+        assert {(p["rows"], p["cols"]) for m, p in plans if p["kernel"] == "banded" and (m <= p["rows"]) == one} >= bands - ({(128, 128)} if one else set())
 
 
 def test_python_refusals(monkeypatch):
