@@ -17,7 +17,6 @@
 #include "common.h"
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 constexpr int Q8_MAX_K = 131071;
 constexpr int Q8_MAX_N = 1 << 24;

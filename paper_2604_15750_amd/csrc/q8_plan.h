@@ -3,14 +3,14 @@
 #include "q8.h"
 
 // The shapes of a tile {WM, WN, KB, ns, more} (see q8_tile.h) and of a band {WM, CW, S, ns, more} (q8_band.h).  ns: nanoseconds per k-tile of 64 that a workgroup
-// alone on the chip takes; more: what one adds that shares its compute unit.  16 of 36 shapes that were timed (29 row counts from 8 to 2822, 15 weights from 640 x 640
-// to 3584 x 18944, random codes), chosen by leaving out, one by one, the shape whose absence costs least (0.8 % in the mean); what the planner takes is 2 % behind the best of these in
-// the mean, 26 % at most.  (W through LDS in tiles of 32, 64 and 96 rows is among those left out: bands are faster by 8 to 16 % from 24 to 340 rows.)
-#define Q8_TILES(X) X(4, 2, 2, 575, 575) X(3, 3, 1, 638, 638) X(2, 3, 1, 472, 472) X(2, 2, 2, 320, 320) X(3, 1, 2, 268, 268) X(2, 1, 2, 200, 200)
+// alone on the chip takes; more: what one adds that shares its compute unit.  15 of 36 shapes that were timed (29 row counts from 8 to 2822, 15 weights from 640 x 640
+// to 3584 x 18944, random codes), chosen by leaving out, one by one, the shape whose absence costs least (0.8 % in the mean); what the planner takes is 1 to 2 % behind the best of
+// these in the mean, a third at most (90 x 4096 x 12288).  (W through LDS in tiles of 32, 64 and 96 rows is among those left out: bands are faster by 8 to 16 % from 24 to 340 rows.)
+#define Q8_TILES(X) X(4, 2, 2, 541, 541) X(3, 3, 1, 638, 638) X(2, 3, 1, 472, 472) X(2, 2, 2, 320, 320) X(3, 1, 2, 272, 272)
 #define Q8_BANDS(X) \
-  X(1, 2, 6, 80, 36) X(1, 3, 6, 90, 62) X(1, 4, 6, 100, 51) X(2, 3, 6, 111, 95) X(2, 4, 5, 124, 108) X(3, 4, 5, 161, 129) X(3, 6, 5, 235, 235) X(4, 4, 4, 210, 122) \
-  X(5, 4, 4, 253, 124) X(5, 6, 4, 374, 374)
-// rows x packed rows: 256 x 256, 192 x 384, 128 x 384, 128 x 256, 192 x 128, 128 x 128; 32 x 64, 32 x 96, 32 x 128, 64 x 96, 64 x 128, 96 x 128, 96 x 192, 128 x 128,
+  X(1, 2, 6, 67, 36) X(1, 3, 6, 90, 62) X(1, 4, 6, 87, 51) X(2, 3, 6, 115, 95) X(2, 4, 5, 133, 108) X(3, 4, 5, 175, 121) X(3, 6, 5, 239, 235) X(4, 4, 4, 199, 122) \
+  X(5, 4, 4, 267, 124) X(5, 6, 4, 374, 374)
+// rows x packed rows: 256 x 256, 192 x 384, 128 x 384, 128 x 256, 192 x 128; 32 x 64, 32 x 96, 32 x 128, 64 x 96, 64 x 128, 96 x 128, 96 x 192, 128 x 128,
 // 160 x 128, 160 x 192
 #define ONE(...) +1
 constexpr int Q8_TILE_COUNT = 0 Q8_TILES(ONE);

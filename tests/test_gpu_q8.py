@@ -229,14 +229,14 @@ def test_wide_product(device, dtype, rows, n, k, gated):
         assert (np.abs(_np64(out) - want) <= off).all() and _untouched(wide, weight.outputs)
 
 
-# shapes whose plain product is a launch of each streamed form and of each tile, with and without a K split
-VARIANTS = [(193, 24601, 128), (774, 4656, 128), (129, 16570, 128), (771, 1154, 16400), (130, 5378, 16400), (289, 16471, 128), (131, 32825, 128),
-            (772, 3213, 16400), (1157, 580, 640), (15, 24578, 2100), (675, 193, 8200), (34, 32, 128), (17, 8205, 640), (33, 33, 4100), (14, 33, 8200),
-            (2725, 129, 128), (21, 16400, 640), (548, 258, 4100), (2711, 483, 128), (33, 24610, 128), (515, 484, 8200), (2340, 385, 128), (33, 16434, 128),
-            (387, 386, 8200), (34, 4098, 16400), (2314, 770, 128), (65, 16443, 128), (771, 881, 8200), (68, 5474, 16400), (258, 11033, 128), (65, 32836, 128),
-            (1035, 910, 16400), (1, 33, 128), (1, 4112, 128), (1, 8193, 128), (17, 33, 128), (17, 4124, 128), (193, 12336, 128), (970, 641, 16400),
-            (193, 21897, 200), (974, 1411, 16400), (197, 32844, 128), (866, 3358, 16400), (518, 8245, 128), (902, 1027, 16400), (513, 24779, 128),
-            (520, 13062, 8200), (1156, 9736, 200), (967, 4530, 16400)]
+# shapes whose plain product is a launch of each streamed form, of each tile and of each band, with and without a K split, with one row block and with more
+VARIANTS = [(193, 12384, 128), (97, 24614, 128), (1364, 641, 8200), (97, 8198, 16400), (773, 4621, 128), (129, 16390, 128), (772, 1158, 16400),
+            (130, 5386, 16400), (290, 16436, 128), (130, 32822, 128), (1418, 1293, 16400), (1159, 581, 640), (9, 24577, 2100), (257, 578, 8200), (34, 32, 128),
+            (17, 8216, 640), (33, 33, 4100), (14, 33, 8200), (2750, 131, 128), (17, 16409, 640), (449, 321, 8200), (2725, 483, 128), (33, 24617, 128),
+            (610, 771, 8200), (2340, 385, 128), (33, 16461, 128), (481, 449, 8200), (35, 5121, 16400), (2305, 782, 128), (65, 16407, 128), (778, 866, 8200),
+            (65, 5446, 16400), (162, 16507, 128), (66, 33284, 128), (1601, 1168, 8200), (1, 33, 128), (1, 4098, 128), (1, 8193, 128), (17, 33, 128),
+            (17, 4099, 128), (97, 36888, 128), (1348, 961, 16400), (193, 33054, 128), (2022, 1413, 16400), (515, 8233, 128), (899, 1033, 16400),
+            (523, 21870, 128), (2313, 3346, 8200), (391, 24580, 200), (2447, 1548, 16400)]
 
 
 @pytest.mark.parametrize("gated", [False, True])

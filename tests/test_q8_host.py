@@ -136,14 +136,14 @@ def test_every_variant_is_reached_by_a_test():
     from test_gpu_q8 import VARIANTS
 
     plans = [(v[0], api.plan_q8_gemm(*v)) for v in VARIANTS]
-    tiles = {(128, 128), (128, 256), (128, 384), (192, 128), (192, 384), (256, 256)}
+    tiles = {(128, 256), (128, 384), (192, 128), (192, 384), (256, 256)}
     bands = {(32, 64), (32, 96), (32, 128), (64, 96), (64, 128), (96, 128), (96, 192), (128, 128), (160, 128), (160, 192)}
     assert {(p["kernel"], p["rows"], p["cols"]) for _, p in plans if p["splits"] == 1} == {("tiled", *t) for t in tiles} | {("banded", *b) for b in bands} | \
         {("streamed", 16, c) for c in (16, 32, 48)} | {("streamed", 32, c) for c in (16, 32)}
-    assert {(p["kernel"], p["rows"], p["cols"]) for _, p in plans if p["splits"] > 1} == {("tiled", *t) for t in tiles} | {("banded", *b) for b in bands - {(128, 128)}}
+    assert {(p["kernel"], p["rows"], p["cols"]) for _, p in plans if p["splits"] > 1} == {("tiled", *t) for t in tiles} | {("banded", *b) for b in bands}
     # a band's W is read in another way where one row block reads it
     for one in (False, True):
-        assert {(p["rows"], p["cols"]) for m, p in plans if p["kernel"] == "banded" and (m <= p["rows"]) == one} >= bands - ({(128, 128)} if one else set())
+        assert {(p["rows"], p["cols"]) for m, p in plans if p["kernel"] == "banded" and (m <= p["rows"]) == one} == bands
 
 
 def test_python_refusals(monkeypatch):
