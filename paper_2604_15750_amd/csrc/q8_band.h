@@ -4,6 +4,11 @@
 // Nobody else in the workgroup uses a wavefront's share of W, so it goes straight to registers, S stages ahead, in the order in which the products take it: a load
 // is 1 KiB of consecutive bytes.  X's rows go through LDS, S stages too, as in q8_tile.h.
 // One barrier a stage, in front of its last step.
+//
+// Bound by W's way from memory and X's from the L2s together: 152 x 37888 x 3584 takes 33 to 35 us for 136 MB of W, 27 to 30 when X is a single row.  Against tiles of the same rows with
+// W through LDS: 152 x 37888 x 3584 35.2 us there, 152 x 12288 x 4096 19.9 (17.6 here), 90 x 37888 x 3584 32.9 (28), 152 x 4096 x 12288 22.4 (20.1).  Where one row block reads W it is read
+// non-temporally, past the memory-side cache, in which the weights of a model do not stay from pass to pass (2 to 3 %); where two do, that costs 7 to 11 %.
+// More stages than S do not help (152 x 37888 x 3584 34.6 us with 4 and with 5).
 #pragma once
 #include "q8_gemm.h"
 #include "q8_plan.h"

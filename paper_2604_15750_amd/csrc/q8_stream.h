@@ -1,14 +1,16 @@
 // Product in 8-bit integers for few rows: the weight's bytes are what it costs.
 //
-// A workgroup of NWV wavefronts owns up to 64 rows of X and CS subs (16 packed channels each) of W and all of K, which its wavefronts share: each
+// A workgroup of NWV wavefronts owns 16 MT rows of X and CS subs (16 packed channels each) of W and all of K, which its wavefronts share: each
 // multiplies its k-tiles (v_mfma_i32_16x16x64_i8) from registers, DEPTH steps of W and X in flight or in use.  No barrier and no LDS in the loop; at the end the
 // wavefronts' sums meet in LDS.  Sums of integers are exact, so their order is free.
+// Bound by W's bytes: 8 x 12288 x 4096 in 9.0 us (5.6 TB/s), 8 x 24576 x 4096, gated, in 16.1 (6.3; a plain non-temporal read of memory reaches 7.1).  With more
+// rows, or a long sum for few outputs, bands are faster (24 x 12288 x 4096 10.8 us, 14.9 here; 8 x 512 x 16000 with K split 8.5, 9.8).
 #pragma once
 #include "q8_gemm.h"
 
 namespace {
 
-template <int MT, int CS, int NWV, int DEPTH, bool NT>
+template <int MT, int CS, int NWV, int DEPTH>
 __global__ __launch_bounds__(64 * NWV) void q8_stream_kernel(const i32x4* __restrict__ wt, const int8_t* __restrict__ x, int64_t x_stride, int M, int K, int subs,
                                                         const float* __restrict__ wscale, const float* __restrict__ x_scale, void* __restrict__ out, int64_t out_stride, int outputs, int form) {
   extern __shared__ __align__(16) i32x4 red[];  // [NWV][CS * MT][64]
@@ -37,10 +39,7 @@ __global__ __launch_bounds__(64 * NWV) void q8_stream_kernel(const i32x4* __rest
 #pragma unroll
     for (int j = 0; j < MT; ++j) v[slot][j] = *(const i32x4*)(xp[j] + 16 * (int64_t)chunk);
 #pragma unroll
-    for (int c = 0; c < CS; ++c) {
-      if constexpr (NT) w[slot][c] = __builtin_nontemporal_load(wp[c] + (int64_t)t * 128);
-      else w[slot][c] = wp[c][(int64_t)t * 128];
-    }
+    for (int c = 0; c < CS; ++c) w[slot][c] = __builtin_nontemporal_load(wp[c] + (int64_t)t * 128);
   };
   auto step = [&](auto Sc, int st) __attribute__((always_inline)) {
     constexpr int S = decltype(Sc)::value;
@@ -110,11 +109,11 @@ __global__ __launch_bounds__(64 * NWV) void q8_stream_kernel(const i32x4* __rest
   });
 }
 
-template <int MT, int CS, int NWV, int DEPTH, bool NT>
+template <int MT, int CS, int NWV, int DEPTH>
 void launch_stream(const Q8View& w, const Q8GemmArgs& a, hipStream_t st) {
   constexpr int LDS = NWV * CS * MT * 1024;
   static_assert(LDS <= 160 * 1024, "the sums' meeting");
-  auto kernel = q8_stream_kernel<MT, CS, NWV, DEPTH, NT>;
+  auto kernel = q8_stream_kernel<MT, CS, NWV, DEPTH>;
   static bool configured = false;
   if (!configured) {
     (void)hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, LDS);

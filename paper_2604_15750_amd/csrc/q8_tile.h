@@ -1,15 +1,18 @@
 // Product in 8-bit integers for many rows: tiles of the output, both operands through LDS.
 //
-// A workgroup of RW x CW wavefronts owns 32 RW WM rows of X (tokens) x 32 CW WN packed rows of W and walks K in stages of KB k-tiles of 64:
+// A workgroup of RW x CW wavefronts owns 32 RW WM rows of X (tokens) x 32 CW WN packed rows of W (RW = 2, CW = 4) and walks K in stages of KB k-tiles of
+// 64:
 //   * W's units lie in memory as the products take them, so a stage of them is copied to LDS as it is; X's rows are 64 KB bytes of each of the tile's
 //     rows, in 16-byte chunks whose place in the row is turned by the row's number, so that 16 lanes that read the same chunk of 16 rows
 //     meet 16 different banks' groups.  Both by direct-to-LDS loads, S stages of them in flight or in use;
-//   * a wavefront multiplies its fragments of a step while it reads the next step's from LDS.  MF = 16: v_mfma_i32_16x16x64_i8, a step of 64 k; MF = 32:
-//     v_mfma_i32_32x32x32_i8, a step of 32 k.  Operands, cycles and LDS reads are the same.  16x16x64 takes less power, which is what bounds launches that fill
-//     the chip (4096 x 8192 x 8192 in 256 x 256 tiles 233 us with MF = 32, 210 with 16); the smaller steps of 32 leave a stage's copies a quarter of a stage longer, which is
-//     worth more where W comes from HBM in tiles that are waited for (152 x 37888 x 3584 in 160 x 192 tiles 33.1 us, 37.5 with 16);
+//   * a wavefront multiplies its fragments of a step of 64 k (v_mfma_i32_16x16x64_i8) while it reads the next step's from LDS;
 //   * one barrier a stage, in front of its last step: by then every wavefront has the stage's last fragments in registers, and the copies of
 //     stage s + S go out over the steps that follow.
+//
+// Bound by the chip's power: 2822 x 12288 x 4096 takes 129 us (2.2 POP/s), 2048 x 37888 x 3584, gated, 251 (2.2), with the matrix cores busy for 52 to 55 % of the cycles at a
+// clock of 1.9 to 2.0 of 2.4 GHz; codes that are all zero go at 3.2 to 3.4 POP/s.  Products of 32x32x32 draw more (4096 x 8192 x 8192 233 us, 210 with 16x16x64).  Slower: four
+// wavefronts of 128 x 128 (2048 x 32768 x 3584 287 us, 210 here: the accumulators do not leave the fragments enough registers), K begun
+// elsewhere by each workgroup, X and W in rings of different depth.
 #pragma once
 #include "q8_gemm.h"
 #include "q8_plan.h"
