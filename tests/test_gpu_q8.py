@@ -434,6 +434,66 @@ def test_rows_far_apart(device):
     assert torch.equal(api.dlm_q8_gemm(weight, far, s.to(device), dtype=F32), api.dlm_q8_gemm(weight, _columns(q, device)[0], s.to(device), dtype=F32))
 
 
+@pytest.mark.parametrize("rows,n", [(257, 300), (300, 24600), (40, 200)])
+def test_rows_as_far_apart_as_a_tile_takes_them(device, rows, n):
+    k, stride = 130, 1 << 22
+    g = _gen(31, rows)
+    (q, s), (c, w) = _coded(g, rows, k), _coded(g, n, k)
+    far = torch.zeros(rows * stride, dtype=I8, device=device).as_strided((rows, k), (stride, 1))
+    far.copy_(q)
+    weight = api.Q8Weight(_columns(c, device)[0], w.to(device))
+    assert torch.equal(api.dlm_q8_gemm(weight, far, s.to(device), dtype=F32), api.dlm_q8_gemm(weight, _columns(q, device)[0], s.to(device), dtype=F32))
+
+
+def test_offsets_past_32_bits(device):
+    """Rows 2^24 elements apart, 300 of them, as inputs and as outputs of every operator."""
+    rows, width, stride = 300, 40, 1 << 24
+    g = _gen(37)
+    far = torch.zeros(rows * stride, dtype=BF16, device=device).as_strided((rows, width), (stride, 1))
+    bytes_ = torch.zeros(rows * stride, dtype=I8, device=device).as_strided((rows, width), (stride, 1))
+    x, res, gain = (torch.randn(rows, width, generator=g).to(BF16).to(device) for _ in range(3))
+    far.copy_(x)
+    scale = torch.empty(rows, device=device)
+    want = api.dlm_q8_rows(x)
+    api.dlm_q8_rows(far, codes=bytes_, scale=scale)
+    assert torch.equal(bytes_, want[0]) and torch.equal(scale, want[1])
+    want = api.dlm_add_norm_q8(x, gain[0], res)
+    api.dlm_add_norm_q8(x, gain[0], res, h=far, codes=bytes_, scale=scale)
+    assert all(torch.equal(a, b) for a, b in zip((bytes_, scale, far), want))
+    (c, w) = _coded(g, width, 64)
+    weight = api.Q8Weight(c.to(device), w.to(device))
+    q, s = (t.to(device) for t in _coded(g, rows, 64))
+    api.dlm_q8_gemm(weight, q, s, out=far)
+    assert torch.equal(far, api.dlm_q8_gemm(weight, q, s))
+
+
+@pytest.mark.parametrize("rows", [3, 40, 150])
+def test_the_most_channels(device, rows):
+    """2^24 channels: a packed weight of 2 GiB, outputs past 2^31.  Sums of 16 products are exact in fp32, and the scales are powers of two."""
+    n, k = 1 << 24, 16
+    q = torch.randint(-128, 128, (rows, k), dtype=I8, generator=_gen(41, rows)).to(device)
+    c = torch.randint(-128, 128, (n, k), dtype=I8, device=device, generator=torch.Generator(device=device).manual_seed(3))
+    w = torch.exp2((torch.arange(n, device=device) % 7).float())
+    weight = api.Q8Weight(c, w)
+    out = api.dlm_q8_gemm(weight, q, torch.full((rows,), 0.5, device=device), dtype=F32)
+    for lo in range(0, n, 1 << 20):  # (torch's product of 150 x 16 x 2^22 in fp32, 2.5 GB of output, is wrong in its rows behind 2 GiB: element by element the sums are ours)
+        part = slice(lo, lo + (1 << 20))
+        assert torch.equal(out[:, part], (q.float() @ c[part].float().t().contiguous()) * 0.5 * w[part])
+
+
+@pytest.mark.parametrize("n,k", [(1, 1), (40, 16), (200, 130)])
+def test_the_most_rows(device, n, k):
+    rows = 1 << 20
+    q = torch.zeros(rows, -(-k // 16) * 16, dtype=I8, device=device)
+    q.random_(-128, 128, generator=torch.Generator(device=device).manual_seed(5))
+    c, _ = _coded(_gen(43, n), n, k)
+    weight = api.Q8Weight(_columns(c, device)[0], torch.ones(n, device=device))
+    out = api.dlm_q8_gemm(weight, q[:, :k], torch.ones(rows, device=device), dtype=F32)
+    assert torch.equal(out, q[:, :k].float() @ c.to(device).float().t().contiguous())
+    with pytest.raises(api.DlmError, match="too many rows"):
+        api.dlm_q8_gemm(weight, torch.zeros(rows + 1, q.shape[1], dtype=I8, device=device)[:, :k], torch.ones(rows + 1, device=device))
+
+
 def test_two_streams_with_a_workspace_each(device):
     layers = [Layer(device, 64, 512, 4096, seed) for seed in (1, 2)]
     assert layers[0].ws[1] is not None
