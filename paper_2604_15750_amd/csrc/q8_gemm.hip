@@ -68,8 +68,8 @@ void launch_q8_join(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, h
                                                                         out_form(w, a));
 }
 
-// The shape and K split with the least estimated time.  A k-tile takes what a workgroup alone on the chip takes (ns), or what the chip's power leaves the matrix cores (3.96
-// POP/s), what the L2s (24.8 TB/s) or, for W, HBM (6.36 TB/s, shared by up to 8 row blocks) give to all of the workgroups that run at a time, whichever is most, joined
+// The shape and K split with the least estimated time.  A k-tile takes what a workgroup alone on the chip takes (ns), or what the chip's power leaves the matrix cores (4.04
+// POP/s), what the L2s (25.6 TB/s) or, for W, HBM (7.07 TB/s, shared by up to 8 row blocks, not perfectly: their number to the power 0.633) give to all of the workgroups that run at a time, whichever is most, joined
 // by a 4-norm; 256 further workgroups add `more` to that, and their epilogues; a K split adds a launch, and the sums' way to memory and back.  Constants
 // fitted to the launches named at Q8_TILES: 10 % off in the root mean square.
 Q8TilePlan q8_tile_plan(int M, int units, int K) {
@@ -80,13 +80,14 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
   constexpr float CUS = 256.f;
   static const auto shape = [](int bm, int un, int kb, float ns, float more) {
     auto p4 = [](float x) { return x * x * x * x; };
-    return Shape{bm, un, kb, p4(ns), p4(more), p4(bm * un * 32 * 128 * CUS / 3.96e6f) + p4((bm + un * 32) * 64 * CUS / 24.8e3f), un * 2048 * CUS / 6.36e3f};
+    return Shape{bm, un, kb, p4(ns), p4(more), p4(bm * un * 32 * 128 * CUS / 4.04e6f) + p4((bm + un * 32) * 64 * CUS / 25.6e3f), un * 2048 * CUS / 7.07e3f};
   };
 #define TILE(WM, WN, KB, NS, MORE) shape(64 * WM, 4 * WN, KB, NS, MORE),
 #define BAND(WM, CW, S, NS, MORE) shape(32 * WM, CW, 2, NS, MORE),
   static const Shape shapes[] = {Q8_TILES(TILE) Q8_BANDS(BAND)};
 #undef TILE
 #undef BAND
+  static constexpr float shared[9] = {1, 1, 0.645f, 0.499f, 0.416f, 0.361f, 0.322f, 0.292f, 0.268f};  // n^-0.633
   const int KT = (K + 63) / 64;
   Q8TilePlan best{};
   best.us = 1e30f;
@@ -94,7 +95,7 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
   for (const Shape& t : shapes) {
     ++i;
     const int mb = (M + t.bm - 1) / t.bm, nb = (units + t.un - 1) / t.un, stages = (KT + t.kb - 1) / t.kb;
-    const float out = t.bm * t.un * 32.f, edge = t.bm + t.un * 32.f, hbm = t.hbm / (mb < 8 ? mb : 8), full_4 = t.chip_4 + hbm * hbm * hbm * hbm;
+    const float out = t.bm * t.un * 32.f, edge = t.bm + t.un * 32.f, hbm = t.hbm * shared[mb < 8 ? mb : 8], full_4 = t.chip_4 + hbm * hbm * hbm * hbm;
     auto ns = [&](float own_4, float share) { return sqrtf(sqrtf(own_4 + full_4 * (share * share) * (share * share))); };
     const int64_t wgs = (int64_t)mb * nb;
     for (int sp = 1; sp <= Q8_MAX_SPLITS; ++sp) {
@@ -103,8 +104,8 @@ Q8TilePlan q8_tile_plan(int M, int units, int K) {
       if ((stages + per - 1) / per != sp) continue;  // (a split without stages)
       const int64_t all = wgs * sp, full = (all - 1) / 256;
       const float last = (all - 256 * full) / CUS;
-      float us = per * t.kb * 1e-3f * ((full ? full * ns(t.more_4, 1.f) : 0.f) + ns(t.ns_4, last)) + 1.67f + (full + last) * 1.336e-4f * out + (0.47f * full + 1) * 9.76e-3f * edge;
-      if (sp > 1) us += 1.8f + sp * (0.187f + 5e-4f * units * ((M + 31) / 32));
+      float us = per * t.kb * 1e-3f * ((full ? full * ns(t.more_4, 1.f) : 0.f) + ns(t.ns_4, last)) + 1.67f + (full + last) * 1.336e-4f * out + (0.44f * full + 1) * 9.76e-3f * edge;
+      if (sp > 1) us += 1.8f + sp * (0.194f + 5e-4f * units * ((M + 31) / 32));
       if (us < best.us) best = Q8TilePlan{i, t.bm, t.un * 32, nb, mb, sp, per, sp > 1 ? (size_t)sp * units * ((M + 31) / 32) * 4096 : 0, us};
     }
   }

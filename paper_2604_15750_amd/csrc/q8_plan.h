@@ -5,11 +5,11 @@
 // The shapes of a tile {WM, WN, KB, ns, more} (see q8_tile.h) and of a band {WM, CW, S, ns, more} (q8_band.h).  ns: nanoseconds per k-tile of 64 that a workgroup
 // alone on the chip takes; more: what one adds that shares its compute unit.  15 of 36 shapes that were timed (29 row counts from 8 to 2822, 15 weights from 640 x 640
 // to 3584 x 18944, random codes), chosen by leaving out, one by one, the shape whose absence costs least (0.8 % in the mean); what the planner takes is 1 to 2 % behind the best of
-// these in the mean, a third at most (90 x 4096 x 12288).  (W through LDS in tiles of 32, 64 and 96 rows is among those left out: bands are faster by 8 to 16 % from 24 to 340 rows.)
-#define Q8_TILES(X) X(4, 2, 2, 541, 541) X(3, 3, 1, 638, 638) X(2, 3, 1, 472, 472) X(2, 2, 2, 320, 320) X(3, 1, 2, 272, 272)
+// these in the mean, 21 % at most (768 x 1024 x 8192).  (W through LDS in tiles of 32, 64 and 96 rows is among those left out: bands are faster by 8 to 16 % from 24 to 340 rows.)
+#define Q8_TILES(X) X(4, 2, 2, 531, 531) X(3, 3, 1, 717, 717) X(2, 3, 1, 472, 472) X(2, 2, 2, 314, 314) X(3, 1, 2, 277, 277)
 #define Q8_BANDS(X) \
-  X(1, 2, 6, 67, 36) X(1, 3, 6, 90, 62) X(1, 4, 6, 87, 51) X(2, 3, 6, 115, 95) X(2, 4, 5, 133, 108) X(3, 4, 5, 175, 121) X(3, 6, 5, 239, 235) X(4, 4, 4, 199, 122) \
-  X(5, 4, 4, 267, 124) X(5, 6, 4, 374, 374)
+  X(1, 2, 6, 64, 36) X(1, 3, 6, 90, 62) X(1, 4, 6, 87, 51) X(2, 3, 6, 133, 95) X(2, 4, 5, 133, 108) X(3, 4, 5, 175, 121) X(3, 6, 5, 230, 230) X(4, 4, 4, 208, 122) \
+  X(5, 4, 4, 269, 128) X(5, 6, 4, 374, 374)
 // rows x packed rows: 256 x 256, 192 x 384, 128 x 384, 128 x 256, 192 x 128; 32 x 64, 32 x 96, 32 x 128, 64 x 96, 64 x 128, 96 x 128, 96 x 192, 128 x 128,
 // 160 x 128, 160 x 192
 #define ONE(...) +1

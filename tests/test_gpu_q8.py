@@ -230,13 +230,13 @@ def test_wide_product(device, dtype, rows, n, k, gated):
 
 
 # shapes whose plain product is a launch of each streamed form, of each tile and of each band, with and without a K split, with one row block and with more
-VARIANTS = [(193, 12384, 128), (97, 24614, 128), (1364, 641, 8200), (97, 8198, 16400), (773, 4621, 128), (129, 16390, 128), (772, 1158, 16400),
-            (130, 5386, 16400), (290, 16436, 128), (130, 32822, 128), (1418, 1293, 16400), (1159, 581, 640), (9, 24577, 2100), (257, 578, 8200), (34, 32, 128),
-            (17, 8216, 640), (33, 33, 4100), (14, 33, 8200), (2750, 131, 128), (17, 16409, 640), (449, 321, 8200), (2725, 483, 128), (33, 24617, 128),
-            (610, 771, 8200), (2340, 385, 128), (33, 16461, 128), (481, 449, 8200), (35, 5121, 16400), (2305, 782, 128), (65, 16407, 128), (778, 866, 8200),
-            (65, 5446, 16400), (162, 16507, 128), (66, 33284, 128), (1601, 1168, 8200), (1, 33, 128), (1, 4098, 128), (1, 8193, 128), (17, 33, 128),
-            (17, 4099, 128), (97, 36888, 128), (1348, 961, 16400), (193, 33054, 128), (2022, 1413, 16400), (515, 8233, 128), (899, 1033, 16400),
-            (523, 21870, 128), (2313, 3346, 8200), (391, 24580, 200), (2447, 1548, 16400)]
+VARIANTS = [(193, 12352, 128), (98, 16443, 200), (1364, 641, 8200), (103, 7169, 8200), (770, 4786, 128), (129, 16713, 128), (290, 2181, 16400),
+            (129, 8083, 8200), (290, 16436, 128), (129, 33001, 128), (1412, 1324, 16400), (131, 16407, 8200), (1158, 582, 640), (6, 24621, 2100),
+            (518, 485, 8200), (34, 32, 128), (32, 4130, 1003), (33, 33, 4100), (14, 33, 8200), (2745, 129, 128), (14, 16506, 640), (321, 452, 8200),
+            (2311, 581, 128), (33, 24603, 128), (805, 577, 8200), (34, 12292, 8200), (2733, 323, 128), (33, 16469, 128), (587, 409, 8200), (36, 2691, 16400),
+            (2305, 782, 128), (65, 16407, 128), (778, 769, 8200), (65, 2694, 16400), (257, 10992, 128), (65, 32870, 128), (1667, 513, 8200), (1, 33, 128),
+            (1, 4106, 128), (1, 8195, 128), (17, 33, 128), (17, 4101, 128), (97, 36888, 128), (1347, 974, 16400), (193, 33111, 200), (878, 3339, 16400),
+            (513, 8297, 128), (706, 1352, 16400), (515, 24663, 128), (2321, 3339, 16400), (196, 36534, 200), (978, 2703, 16400)]
 
 
 @pytest.mark.parametrize("gated", [False, True])
