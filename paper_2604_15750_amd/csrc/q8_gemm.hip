@@ -69,9 +69,9 @@ void launch_q8_join(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, h
 }
 
 // The shape and K split with the least estimated time.  A k-tile takes what a workgroup alone on the chip takes (ns), or what the chip's power leaves the matrix cores (4.04
-// POP/s), what the L2s (25.6 TB/s) or, for W, HBM (7.07 TB/s, shared by up to 8 row blocks, not perfectly: their number to the power 0.633) give to all of the workgroups that run at a time, whichever is most, joined
-// by a 4-norm; 256 further workgroups add `more` to that, and their epilogues; a K split adds a launch, and the sums' way to memory and back.  Constants
-// fitted to the launches named at Q8_TILES: 10 % off in the root mean square.
+// POP/s), what the L2s (25.6 TB/s) or, for W, HBM (7.07 TB/s) give to all of the workgroups that run at a time, whichever is most, joined by a 4-norm; row blocks
+// share W, up to 8 of them and not perfectly: their number to the power 0.633.  256 further workgroups add `more` to that, and their epilogues; a K split adds a launch, and the
+// sums' way to memory and back.  Constants fitted to the launches named at Q8_TILES: 10 % off in the root mean square.
 Q8TilePlan q8_tile_plan(int M, int units, int K) {
   struct Shape {
     int bm, un, kb;
