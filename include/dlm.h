@@ -342,7 +342,8 @@ int dlm_q8_weight_pack(const dlm_q8_weight* w, const int8_t* codes, int64_t code
  * scale.  gated: out [rows, n / 2] = g / (1 + exp(-g)) u of the gate's and the up channel's values.  Rounded once to out_dtype; columns behind
  * the outputs are left as they are.  x [rows, k] codes (any int8) and x_scale [rows]; nothing may overlap out.
  * workspace: DEVICE scratch at a multiple of 16 of dlm_q8_gemm_workspace(r, n, k, gated) bytes for some r >= rows (0: none is needed, it may be NULL), for
- * products that share K between workgroups.  It is in use until the call's work is done: calls that may overlap need one each.
+ * products that share K between workgroups (rows up to r; plan[5] KiB of dlm_plan_q8_gemm are enough for those rows alone).  It is in use until the
+ * call's work is done: calls that may overlap need one each.
  * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, bad dtype, gated), DLM_ESHAPE (weight, rows < 0), DLM_ECAPACITY (workspace too small,
  * more than 1048576 rows or 2^38 outputs), DLM_EHIP. */
 size_t dlm_q8_gemm_workspace(int rows, int n, int k, int gated);

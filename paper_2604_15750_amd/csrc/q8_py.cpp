@@ -65,7 +65,7 @@ PyObject* norm(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   return PyLong_FromLong(rc);
 }
 
-// gemm(weight, weight memory, x, x_scale, out, workspace, device, stream) -> status or None.  Declines a call that needs a workspace and has none.
+// gemm(weight, weight memory, x, x_scale, out, workspace, device, stream) -> status or None.  DLM_ECAPACITY without a workspace: it may need one.
 PyObject* gemm(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   int dev;
   Tensor x, scale, out;
@@ -91,7 +91,6 @@ PyObject* gemm(PyObject* self, PyObject* const* a, Py_ssize_t n_args) {
   Py_BEGIN_ALLOW_THREADS
   rc = g_gemm(w, (const int8_t*)x.p, x.stride, (const float*)scale.p, (int)x.shape[0], out.p, out.stride, out.dtype, ws, ws_bytes, stream);
   Py_END_ALLOW_THREADS
-  DECLINE_UNLESS(rc != DLM_ECAPACITY || a[5] != Py_None);  // (nothing has been launched)
   return PyLong_FromLong(rc);
 }
 
