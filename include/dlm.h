@@ -345,7 +345,7 @@ int dlm_q8_weight_pack(const dlm_q8_weight* w, const int8_t* codes, int64_t code
  * products that share K between workgroups (rows up to r; plan[5] KiB of dlm_plan_q8_gemm are enough for those rows alone).  It is in use until the
  * call's work is done: calls that may overlap need one each.
  * Errors: DLM_EINVAL (null pointer, alignment, stride, overlap, bad dtype, gated), DLM_ESHAPE (weight, rows < 0), DLM_ECAPACITY (workspace too small,
- * more than 1048576 rows or 2^38 outputs), DLM_EHIP. */
+ * more than 1048576 rows or 2^38 outputs, or a launch of 2^32 threads: gated, some products of 0.99 x 2^38 outputs and more), DLM_EHIP. */
 size_t dlm_q8_gemm_workspace(int rows, int n, int k, int gated);
 int dlm_q8_gemm(const dlm_q8_weight* w, const int8_t* x, int64_t x_stride, const float* x_scale, int rows, void* out, int64_t out_stride, int out_dtype,
                 void* workspace, size_t workspace_bytes, void* stream);

@@ -126,6 +126,7 @@ extern "C" int dlm_q8_gemm(const dlm_q8_weight* w, const int8_t* x, int64_t x_st
   const Q8GemmArgs args{x, x_stride, x_scale, rows, out, out_stride, out_dtype, workspace};
   if (rows == 0) return DLM_OK;
   const Q8Plan plan = q8_plan(rows, view.units, view.k, view.gated, x_stride);
+  REQUIRE(plan.streamed || q8_tile_threads(plan.tile) < INT64_C(1) << 32, DLM_ECAPACITY, "%s: too many rows and channels for one launch", name);
   const size_t need = plan.workspace;
   REQUIRE(!need || (workspace && workspace_bytes >= need), DLM_ECAPACITY, "%s: workspace of %zu bytes < %zu", name, workspace ? workspace_bytes : 0, need);
   REQUIRE(!need || !(overlap(workspace, need, x, xr.span()) || overlap(workspace, need, out, to.span()) || overlap(workspace, need, x_scale, (wide)rows * 4) ||

@@ -24,6 +24,10 @@ struct Q8TilePlan {
   size_t workspace;    // bytes: the sums of every split of a launch that splits K, 4 KiB a unit and 32 rows
   float us;            // estimated
 };
+// threads of its launch: 8 wavefronts a tile, one a unit of a band; workgroups in eights (see tile_of)
+inline int64_t q8_tile_threads(const Q8TilePlan& p) {
+  return ((int64_t)p.nblocks * p.mblocks * p.splits + 7) / 8 * 8 * (p.tile < Q8_TILE_COUNT ? 512 : p.cols / 32 * 64);
+}
 constexpr int Q8_SPLIT_WGS = 256, Q8_MAX_SPLITS = 16;  // (a launch that splits K is one round)
 Q8TilePlan q8_tile_plan(int M, int units, int K);
 void launch_q8_tiles(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, hipStream_t st);
