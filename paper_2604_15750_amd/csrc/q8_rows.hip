@@ -175,7 +175,16 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void q8_rows_kernel(const TX* x,
   const float a = __uint_as_float(top);
   const bool bad = top >= 0x7F800000u || (NORM && !(ss < __builtin_inff()));
   if (threadIdx.x % T == 0) {
-    const float s = NORM && a > 0.f ? a * rsqrtf(ss / (float)width + eps) / 127.f : a / 127.f;
+    float y = a, up = 1.f;
+    if (NORM && a > 0.f) {
+      const float r = rsqrtf(ss / (float)width + eps);
+      y = a * r;
+      if (y == __builtin_inff()) {  // (the row's largest value may be past fp32's range where its 127th is not)
+        y = a * 0x1p-16f * r;
+        up = 0x1p16f;
+      }
+    }
+    const float s = y / 127.f * up;
     scale[row] = bad ? __builtin_nanf("") : s;
   }
   // a row of zeros: every quotient 0 x 0; a tiny maximum: 127 / max would be past fp32's range, so the row is scaled by a power of two first
