@@ -339,7 +339,8 @@ size_t dlm_q8_weight_bytes(int n, int k, int gated);
 int dlm_q8_weight_pack(const dlm_q8_weight* w, const int8_t* codes, int64_t codes_stride, const float* scale, void* stream);
 
 /* out [rows, n] = x_scale[m] scale[j] sum_k x[m][k] codes[j][k]: the sum exact, converted to fp32 and multiplied by the row's and then the channel's
- * scale.  gated: out [rows, n / 2] = g / (1 + exp(-g)) u of the gate's and the up channel's values.  Rounded once to out_dtype; columns behind
+ * scale.  gated: out [rows, n / 2] = g / (1 + exp(-g)) u of the gate's and the up channel's values.  Before the output's rounding, plain values are off by 3 x 2^-24
+ * of themselves, gated ones by (13 + 6 |g|) x 2^-24, and by 2^-125 |g u| at most below g = -87.3, where they may be zero.  Rounded once to out_dtype; columns behind
  * the outputs are left as they are.  x [rows, k] codes (any int8) and x_scale [rows]; nothing may overlap out.
  * workspace: DEVICE scratch at a multiple of 16 of dlm_q8_gemm_workspace(r, n, k, gated) bytes for some r >= rows (0: none is needed, it may be NULL), for
  * products that share K between workgroups (rows up to r; plan[5] KiB of dlm_plan_q8_gemm are enough for those rows alone).  It is in use until the

@@ -6,7 +6,7 @@ import torch
 
 from oracle import q8 as o_q8
 from paper_2604_15750_amd import api
-from test_gpu_q8 import BF16, F32, U, _columns, _gen, _np64
+from test_gpu_q8 import BF16, F32, HALF_STEP, I8, U, _columns, _gen, _np64
 
 pytestmark = pytest.mark.gpu
 
@@ -28,3 +28,31 @@ def test_a_scale_whose_row_times_the_norm_is_past_fp32(device, dtype, width):
         assert np.isnan(scale[bad]).all() and (s[~bad] < torch.finfo(F32).max).all()
         assert (np.abs(scale - s)[~bad] <= 72 * U * s[~bad]).all(), (gain, scale, s)
         assert (codes.cpu().numpy() == np.where(bad[:, None], 0, q)).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("rows", [4, 60, 700])
+def test_the_gated_unit_where_it_is_large_and_small(device, dtype, rows):
+    """Gates from -115 to 115 with up values from 2^-60 to 2^100: off by (13 + 6 |g|) u of the output and 2^-125 |g u| at most, besides the output's rounding.
+    The latter is the whole of it below g = -87.3, where exp(-g) is past 2^126 and its reciprocal may be taken as zero."""
+    f = 256
+    g = _gen(rows, 71)
+    codes = torch.zeros(2 * f, 16, dtype=I8)
+    codes[:f, 0] = torch.randint(-115, 116, (f,), generator=g, dtype=torch.int16).to(I8)
+    codes[:6, 0] = torch.tensor([-90, -89, -88, -87, 88, 115], dtype=I8)
+    codes[f:, 1] = torch.randint(-127, 128, (f,), generator=g, dtype=torch.int16).to(I8)
+    w = torch.ones(2 * f)
+    w[f:] = torch.exp2(torch.randint(-60, 101, (f,), generator=g).float())
+    w[f:f + 4] = 2.0 ** 100
+    q = torch.zeros(rows, 16, dtype=I8)
+    q[:, :2] = 1
+    s = 1 - torch.rand(rows, generator=g) / 64  # (gates between the whole numbers)
+    s[0] = 1
+    out = api.dlm_q8_gemm(api.Q8Weight(codes.to(device), w.to(device), gated=True), q.to(device), s.to(device), dtype=dtype)
+    y = o_q8.product(q.numpy(), _np64(s), codes.numpy(), _np64(w))
+    want, size = o_q8.gated(y), np.abs(y[:, :f])
+    off = ((13 + 6 * size) * U * np.abs(want) + 2.0 ** -125 * size * np.abs(y[:, f:])) * (1 + 2.0 ** -7)
+    # the output's rounding: half a step, which below 2^-126 is 2^-150 in fp32 and, with 7 bits of fraction, 2^-134 in bf16
+    off += HALF_STEP[dtype] * np.abs(want) + (2.0 ** -134 if dtype == BF16 else 2.0 ** -149)
+    bad = ~(np.abs(_np64(out) - want) <= off)
+    assert not bad.any(), (np.argwhere(bad)[:5], _np64(out)[bad][:5], want[bad][:5])
