@@ -6,7 +6,7 @@ import torch
 
 from oracle import q8 as o_q8
 from paper_2604_15750_amd import api
-from test_gpu_q8 import BF16, F32, HALF_STEP, I8, U, _columns, _gen, _np64
+from test_gpu_q8 import BF16, F32, HALF_STEP, I8, U, _coded, _columns, _gen, _np64
 
 pytestmark = pytest.mark.gpu
 
@@ -28,6 +28,35 @@ def test_a_scale_whose_row_times_the_norm_is_past_fp32(device, dtype, width):
         assert np.isnan(scale[bad]).all() and (s[~bad] < torch.finfo(F32).max).all()
         assert (np.abs(scale - s)[~bad] <= 72 * U * s[~bad]).all(), (gain, scale, s)
         assert (codes.cpu().numpy() == np.where(bad[:, None], 0, q)).all()
+
+
+@pytest.mark.parametrize("rows", [1, 5, 300])
+@pytest.mark.parametrize("width", [200, 4000])
+def test_columns_beside_their_source(device, rows, width):
+    """What is written lies in columns of the matrix that is read: codes beside their values, outputs beside their codes."""
+    step = -(-(3 * width + 64) // 16) * 16  # bytes a row: values, codes, 32 bytes on each side
+    wide = torch.full((rows, step // 2), 3.0, dtype=BF16, device=device)
+    x = wide[:, 16:16 + width]
+    x.copy_(torch.randn(rows, width, generator=_gen(rows, width)))
+    kept = x.clone()
+    codes, scale = wide.view(I8)[:, 32 + 2 * width:32 + 3 * width], torch.empty(rows, device=device)
+    for norm in (False, True):
+        codes.fill_(9)
+        if norm:
+            gain = torch.ones(width, dtype=BF16, device=device)
+            want, want_scale, _ = api.dlm_add_norm_q8(kept, gain)
+            api.dlm_add_norm_q8(x, gain, codes=codes, scale=scale)
+        else:
+            want, want_scale = api.dlm_q8_rows(kept)
+            api.dlm_q8_rows(x, codes=codes, scale=scale)
+        assert torch.equal(codes, want) and torch.equal(scale, want_scale) and torch.equal(x, kept)
+    # a product of the codes, into the columns where the values were
+    c, w = _coded(_gen(width, 5), width, width)
+    weight = api.Q8Weight(_columns(c, device)[0], w.to(device))
+    out = api.dlm_q8_gemm(weight, want, want_scale)
+    api.dlm_q8_gemm(weight, codes, scale, out=x)
+    assert torch.equal(x, out) and torch.equal(codes, want)
+    assert (wide[:, :16] == 3).all() and (wide.view(I8)[:, 32 + 3 * width:] == torch.full((1,), 3.0, dtype=BF16).view(I8).repeat(step)[:step - 32 - 3 * width].to(device)).all()
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
