@@ -6,7 +6,7 @@ import torch
 
 from oracle import q8 as o_q8
 from paper_2604_15750_amd import api
-from test_gpu_q8 import BF16, F32, HALF_STEP, I8, U, _coded, _columns, _gen, _np64
+from test_gpu_q8 import BF16, F32, HALF_STEP, I8, U, VARIANTS, _coded, _columns, _gen, _np64, _untouched
 
 pytestmark = pytest.mark.gpu
 
@@ -57,6 +57,31 @@ def test_columns_beside_their_source(device, rows, width):
     api.dlm_q8_gemm(weight, codes, scale, out=x)
     assert torch.equal(x, out) and torch.equal(codes, want)
     assert (wide[:, :16] == 3).all() and (wide.view(I8)[:, 32 + 3 * width:] == torch.full((1,), 3.0, dtype=BF16).view(I8).repeat(step)[:step - 32 - 3 * width].to(device)).all()
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows,n,k", [v for v in VARIANTS if api.plan_q8_gemm(*v)["splits"] > 1])
+def test_a_split_product_whatever_the_workspace_holds(device, rows, n, k, gated):
+    """Each time against 64 bits, and bit for bit the same: sums of integers have no order."""
+    n += gated and n % 2
+    g = _gen(rows, n, k, 3)
+    (q, s), (c, w) = _coded(g, rows, k, 0.3), _coded(g, n, k, 0.3)
+    w = w * 30
+    weight = api.Q8Weight(_columns(c, device)[0], w.to(device), gated=gated)
+    qd, ws, first = _columns(q, device)[0], weight.workspace(rows), None
+    # (the sums in 64 bits on the GPU: exact, as they are below 2^53)
+    y = (q.to(device).double() @ c.to(device).double().t().contiguous()).cpu().numpy() * _np64(s)[:, None] * _np64(w)
+    want, off = y, 3 * U * np.abs(y)
+    if gated:
+        want = o_q8.gated(y)
+        off = (13 + 6 * np.abs(y[:, :n // 2])) * U * np.abs(want) + 2.0 ** -125 * np.abs(y[:, :n // 2] * y[:, n // 2:])
+    for fill in (255, 127, 128, 0):
+        out, wide = _columns(torch.full((rows, weight.outputs), 9.0), device)
+        ws.fill_(fill)
+        api.dlm_q8_gemm(weight, qd, s.to(device), out=out, workspace=ws)
+        assert (np.abs(_np64(out) - want) <= off * (1 + 2.0 ** -7) + U * np.abs(want) + 2.0 ** -149).all() and _untouched(wide, weight.outputs)
+        first = out if first is None else first
+        assert torch.equal(out, first)
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
