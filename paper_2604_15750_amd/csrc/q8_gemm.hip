@@ -68,14 +68,14 @@ void launch_q8_join(const Q8View& w, const Q8GemmArgs& a, const Q8TilePlan& p, h
                                                                         out_form(w, a));
 }
 
-// The shape and K split with the least estimated time.  A k-tile takes what a workgroup alone on the chip takes (ns), or what the chip's power leaves the matrix cores (4.04
-// POP/s), what the L2s (25.6 TB/s) or, for W, HBM (7.07 TB/s) give to all of the workgroups that run at a time, whichever is most, joined by a 4-norm; row blocks
+// The shape and K split with the least estimated time.  A k-tile takes what a workgroup alone on the chip takes (ns), or what the matrix cores give when all are busy (4.04
+// POP/s, at the 1.93 GHz that power leaves), what the L2s (25.6 TB/s) or, for W, HBM (7.07 TB/s) give to all of the workgroups that run at a time, whichever is most, joined by a 4-norm; row blocks
 // share W, up to 8 of them and not perfectly: their number to the power 0.633.  256 further workgroups add `more` to that, and their epilogues; a K split adds a launch, and the
 // sums' way to memory and back.  Constants fitted to the launches named at Q8_TILES: 10 % off in the root mean square.
 Q8TilePlan q8_tile_plan(int M, int units, int K) {
   struct Shape {
     int bm, un, kb;
-    float ns_4, more_4, chip_4, hbm;  // 4th powers of ns, of `more`, and of what power and the L2s allow on a full chip; ns that HBM allows where one row block reads W
+    float ns_4, more_4, chip_4, hbm;  // 4th powers of ns, of `more`, and of what the matrix cores and the L2s allow on a full chip; ns that HBM allows where one row block reads W
   };
   constexpr float CUS = 256.f;
   static const auto shape = [](int bm, int un, int kb, float ns, float more) {

@@ -9,8 +9,10 @@
 //   * one barrier a stage, in front of its last step: by then every wavefront has the stage's last fragments in registers, and the copies of
 //     stage s + S go out over the steps that follow.
 //
-// Bound by the chip's power: 2822 x 12288 x 4096 takes 129 us (2.2 POP/s), 2048 x 37888 x 3584, gated, 251 (2.2), with the matrix cores busy for 52 to 55 % of the cycles at a
-// clock of 1.9 to 2.0 of 2.4 GHz; codes that are all zero go at 3.2 to 3.4 POP/s.  Products of 32x32x32 draw more (4096 x 8192 x 8192 233 us, 210 with 16x16x64).  Slower: four
+// 2822 x 12288 x 4096 takes 128 us (2.2 POP/s), 2048 x 37888 x 3584, gated, 247 (2.3).  Bound by a workgroup's own cycles, there being one a compute unit: a tile of
+// 256 x 256 takes 2800 for a stage of 128 k, 2048 of which the matrix cores are busy, and 20000 to fill and to finish (4096 x 8192, two tiles a compute unit, 130, 221, 399 and
+// 756 thousand with k of 2048, 4096, 8192 and 16384: 50, 59, 66 and 69 % busy).  Power sets their length: codes that are all zero take as many cycles, at 2.26 to 2.33 GHz
+// instead of 1.93 to 2.01 (108 us for 128).  With products of 32x32x32 4096 x 8192 x 8192 took 233 us (210 with 16x16x64).  Slower: four
 // wavefronts of 128 x 128 (2048 x 32768 x 3584 287 us, 210 here: the accumulators do not leave the fragments enough registers), K begun
 // elsewhere by each workgroup, X and W in rings of different depth.
 #pragma once
